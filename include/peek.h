@@ -340,6 +340,182 @@ size_t peek_offline_order_workspace(int32_t n);
 peek_status peek_offline_order(int32_t n, const int32_t* d_tokens, const int64_t* d_offsets, int32_t depth_limit,
                                int32_t* d_perm, void* d_workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The cache's contents: keys and values of 8 bits in pages, the attention
+ * that reads them, and what attention says may go.
+ *
+ * peek_lpm_batch says how many leading tokens of a prompt are cached (h).
+ * These calls are what the hit is for: the K and V of those tokens in pages
+ * of block_size tokens, attention of the prompt's other tokens over them,
+ * attention of the tokens generated after it, and the eviction of a
+ * sequence's blocks that attention hardly reads.
+ *
+ * Pool: pages[num_pages][2][kv_heads][block_size][head_dim] of 8-bit codes
+ * (K at 0, V at 1), scales[num_pages][2][kv_heads] float32. A value is its
+ * code times its scale. Formats: PEEK_TYPE_F8E4M3 (OCP e4m3) and
+ * PEEK_TYPE_I8. block_size is a power of two in [4, 256], as of a block
+ * table; head_dim is 64 or 128; kv_heads is in [1, 1024].
+ *
+ * Block table: int32[n][max_blocks], rows table_stride entries apart;
+ * sequence r's token t lies in page table[r][t / block_size], at slot
+ * t % block_size. Sequences may share pages (a prefix found by the match);
+ * a page that a call writes must be named by one sequence only.
+ *
+ * Rows of heads (q, k, v, out): element (token t, head j, i) lies at
+ * t * token_stride + j * head_stride + i, in elements of type
+ * PEEK_TYPE_BF16 or PEEK_TYPE_F16, so slices of a fused projection need no
+ * copy. Base pointers are 16-byte aligned, strides multiples of 8 that are
+ * not negative. Query heads are a multiple of the kv heads, at most 65536;
+ * query head j reads kv head j / (q_heads / kv_heads).
+ *
+ * Sums, maxima and weights are held in 32 bits; weights are rounded to the
+ * query's type where they meet the values, the output once at the end.
+ *
+ * Tokens of other sequences, slots past a sequence's end and pages it does
+ * not name may hold anything, NaN included: they do not reach its outputs.
+ * A page id outside the pool is a broken precondition (PEEK_VALIDATE reports
+ * it); memory outside the pool is not touched: peek_kv_append leaves such a
+ * block out, attention reads page 0 in its place. Lengths beyond the table
+ * (max_blocks * block_size tokens) and negative ones are cut to it.
+ * PEEK_VALIDATE checks offsets, lengths and page ids of these calls.
+ * ---------------------------------------------------------------------- */
+typedef enum peek_type {
+  PEEK_TYPE_BF16 = 0,
+  PEEK_TYPE_F16 = 1,
+  PEEK_TYPE_F8E4M3 = 2,
+  PEEK_TYPE_I8 = 3
+} peek_type;
+
+/* A pool of pages: device memory of the caller's, described by value (read
+ * before a call returns). */
+typedef struct peek_kv_pool {
+  void* d_pages;      /* 16-byte aligned */
+  float* d_scales;
+  int64_t num_pages;  /* < 2^31 */
+  int32_t kv_heads;
+  int32_t block_size;
+  int32_t head_dim;
+  int32_t type;       /* PEEK_TYPE_F8E4M3 or PEEK_TYPE_I8 */
+} peek_kv_pool;
+
+/* ------------------------------------------------------------------------
+ * peek_kv_append: quantises the K and V of new tokens into the pool.
+ *
+ * Sequence r has d_context[r] tokens in the cache; its new ones are rows
+ * d_offsets[r] .. d_offsets[r+1] of k and v (num_tokens rows in all) and
+ * get the positions after them. d_context is not changed. For every block
+ * that gets new tokens, for K and for V and for every head:
+ *   a  = the largest finite magnitude among the block's new values
+ *   s' = F8E4M3: the smallest power of two with a <= 448 * s'
+ *        I8:     a / 127
+ *        (both kept within 2^-60 .. 2^60)
+ *   s  = s' if the block's first token is new, else max(s', old scale)
+ *   code = x / s (in 32 bits) to the nearest the format holds, ties to even,
+ *        larger magnitudes (infinities) to the largest; NaN stays NaN in
+ *        F8E4M3 and becomes 0 in I8
+ * If s is larger than the old scale, the block's older tokens (slots before
+ * the first new one) are rounded again to it. Asynchronous on `stream`; no
+ * workspace. n = 0 or num_tokens = 0 is a no-op.
+ * Errors: INVALID_ARGUMENT, DEVICE.
+ * ---------------------------------------------------------------------- */
+peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_tokens, int32_t type, const void* d_k,
+                           int64_t k_token_stride, int64_t k_head_stride, const void* d_v, int64_t v_token_stride,
+                           int64_t v_head_stride, const int64_t* d_offsets, const int32_t* d_context,
+                           const int32_t* d_block_table, int32_t max_blocks, int64_t table_stride, void* stream);
+
+/* ------------------------------------------------------------------------
+ * peek_prefill_attention: attention of packed prompts, causal, each after
+ * its cached prefix.
+ *
+ * Sequence r's rows of q, k and v are d_offsets[r] .. d_offsets[r+1] of
+ * num_tokens; before them stand d_prefix[r] cached tokens (d_prefix, pool
+ * and table may be NULL together: nothing is cached). For its i-th row and
+ * every query head, with key and value j running over the prefix and then
+ * over its own rows 0 .. i:
+ *   x_j = scale * q . k_j
+ *   out = sum_j exp(x_j) v_j / sum_j exp(x_j),   lse = log sum_j exp(x_j)
+ * d_lse (nullable) is float32[num_tokens][q_heads]. Rows in no sequence are
+ * left as they are. A prompt's own later tokens reach none of its rows'
+ * weights, but a NaN or infinity among their values may reach rows of the
+ * same sequence up to 255 tokens before them.
+ * Scratch comes only from d_workspace (device, 256-byte aligned, at least
+ * peek_prefill_attention_workspace bytes for these sizes; max_context =
+ * max_blocks * block_size, 0 without a cache). Asynchronous on `stream`.
+ * Errors: INVALID_ARGUMENT, WORKSPACE_TOO_SMALL, DEVICE.
+ * ---------------------------------------------------------------------- */
+size_t peek_prefill_attention_workspace(int32_t n, int64_t num_tokens, int32_t q_heads, int32_t kv_heads,
+                                        int32_t head_dim, int64_t max_context);
+
+peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t num_tokens, int32_t type,
+                                   int32_t q_heads, int32_t kv_heads, int32_t head_dim, const void* d_q,
+                                   int64_t q_token_stride, int64_t q_head_stride, const void* d_k,
+                                   int64_t k_token_stride, int64_t k_head_stride, const void* d_v,
+                                   int64_t v_token_stride, int64_t v_head_stride, const int64_t* d_offsets,
+                                   const int32_t* d_prefix, const int32_t* d_block_table, int32_t max_blocks,
+                                   int64_t table_stride, float scale, void* d_out, int64_t out_token_stride,
+                                   int64_t out_head_stride, float* d_lse, void* d_workspace, size_t workspace_bytes,
+                                   void* stream);
+
+/* ------------------------------------------------------------------------
+ * peek_decode_attention: attention of one token per sequence over its
+ * cached tokens, the d_context[r] first of its pages (the token's own K and V
+ * appended before the call where it attends to itself). Row r of q and out
+ * is sequence r's; d_lse (nullable) is float32[n][q_heads]. A sequence of no
+ * tokens has out = 0 and lse = -infinity.
+ *
+ * d_mass (nullable) float32[n][kv_heads][max_blocks] receives the weight
+ * that falls on every block, summed over the kv head's query heads, on top
+ * of d_mass_in (same shape; NULL: zeros; may be d_mass itself):
+ *   mass[r][h][b] = mass_in[r][h][b] + sum over those heads and the tokens
+ *                   of block b of exp(x - lse)
+ * Blocks past the sequence's end keep mass_in. Sums run in a fixed order:
+ * equal inputs give equal bits.
+ * Scratch comes only from d_workspace (device, 256-byte aligned, at least
+ * peek_decode_attention_workspace bytes; with_mass = whether d_mass is
+ * given). Asynchronous on `stream`. n = 0 is a no-op.
+ * Errors: INVALID_ARGUMENT, WORKSPACE_TOO_SMALL, DEVICE.
+ * ---------------------------------------------------------------------- */
+size_t peek_decode_attention_workspace(const peek_kv_pool* pool, int32_t n, int32_t q_heads, int32_t max_blocks,
+                                       int32_t with_mass);
+
+peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t type, int32_t q_heads, const void* d_q,
+                                  int64_t q_token_stride, int64_t q_head_stride, const int32_t* d_context,
+                                  const int32_t* d_block_table, int32_t max_blocks, int64_t table_stride, float scale,
+                                  void* d_out, int64_t out_token_stride, int64_t out_head_stride, float* d_lse,
+                                  const float* d_mass_in, float* d_mass, void* d_workspace, size_t workspace_bytes,
+                                  void* stream);
+
+/* ------------------------------------------------------------------------
+ * peek_kv_evict: drops the blocks of least accumulated attention weight from
+ * sequences that hold more than they may keep.
+ *
+ * Sequence r of d_context[r] tokens has nb = ceil(context / block_size)
+ * blocks and may keep d_keep[r]. A block's score is the sum of its masses
+ * over the kv heads (32 bits, heads in ascending order, NaN above all).
+ * Candidates are the blocks b with sink <= b < nb - recent (recent >= 1, so
+ * the last, perhaps unfinished block stays). The nb - keep candidates of
+ * lowest score go (all of them, if there are fewer), equal scores by
+ * position. Entries that stay move up in order, those past nb (pages held
+ * for tokens to come) included:
+ *   d_table_out int32[n][max_blocks], the rest of a row -1
+ *   d_mass_out  float32[n][kv_heads][max_blocks], the rest 0
+ *   d_freed     int32[n][max_blocks]: the evicted pages by position, then -1
+ *   d_num_freed int32[n],  d_context_out[r] = context - block_size * freed
+ * Keys carry their positions already, so attention over what stays needs
+ * nothing else. Input and output arrays must not overlap, but d_context_out
+ * may be d_context. Scratch comes only from d_workspace (device, 256-byte
+ * aligned, at least peek_kv_evict_workspace bytes). Asynchronous on
+ * `stream`. n = 0 is a no-op.
+ * Errors: INVALID_ARGUMENT, WORKSPACE_TOO_SMALL, DEVICE.
+ * ---------------------------------------------------------------------- */
+size_t peek_kv_evict_workspace(int32_t n, int32_t kv_heads, int32_t max_blocks);
+
+peek_status peek_kv_evict(int32_t n, int32_t kv_heads, int32_t block_size, const int32_t* d_context,
+                          const int32_t* d_block_table, int32_t max_blocks, int64_t table_stride, const float* d_mass,
+                          const int32_t* d_keep, int32_t sink, int32_t recent, int32_t* d_context_out,
+                          int32_t* d_table_out, float* d_mass_out, int32_t* d_freed, int32_t* d_num_freed,
+                          void* d_workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,6 +1,7 @@
 """Python binding of libpeek (include/peek.h): batched longest-prefix match of
 a waiting queue against a KV prefix-cache radix tree, plus the queue signals
-(prefix-sharing clusters and per-cache-node pending demand), on MI355X.
+(prefix-sharing clusters and per-cache-node pending demand), and attention over
+the cache's 8-bit pages, on MI355X.
 
 Argument marshalling only: every step runs in the library's HIP kernels.
 Device arrays are torch tensors on the current HIP device (torch is used for
@@ -41,6 +42,8 @@ PEEK_ERR_UNSUPPORTED_DEVICE = -6
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _i64p = ctypes.POINTER(ctypes.c_int64)
 _vp = ctypes.c_void_p
+_i32 = ctypes.c_int32
+_i64 = ctypes.c_int64
 
 # (name, restype, argtypes) of every exported symbol in include/peek.h
 EXPORTS = [
@@ -73,6 +76,20 @@ EXPORTS = [
     ("peek_offline_order_workspace", ctypes.c_size_t, [ctypes.c_int32]),
     ("peek_offline_order", ctypes.c_int,
      [ctypes.c_int32, _vp, _vp, ctypes.c_int32, _vp, _vp, ctypes.c_size_t, _vp]),
+    ("peek_kv_append", ctypes.c_int,
+     [_vp, _i32, _i64, _i32, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _i32, _i64, _vp]),
+    ("peek_prefill_attention_workspace", ctypes.c_size_t, [_i32, _i64, _i32, _i32, _i32, _i64]),
+    ("peek_prefill_attention", ctypes.c_int,
+     [_vp, _i32, _i64, _i32, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _i32,
+      _i64, ctypes.c_float, _vp, _i64, _i64, _vp, _vp, ctypes.c_size_t, _vp]),
+    ("peek_decode_attention_workspace", ctypes.c_size_t, [_vp, _i32, _i32, _i32, _i32]),
+    ("peek_decode_attention", ctypes.c_int,
+     [_vp, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _vp, _i32, _i64, ctypes.c_float, _vp, _i64, _i64, _vp, _vp, _vp,
+      _vp, ctypes.c_size_t, _vp]),
+    ("peek_kv_evict_workspace", ctypes.c_size_t, [_i32, _i32, _i32]),
+    ("peek_kv_evict", ctypes.c_int,
+     [_i32, _i32, _i32, _vp, _vp, _i32, _i64, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t,
+      _vp]),
 ]
 
 for _name, _res, _args in EXPORTS:
@@ -378,3 +395,170 @@ def peek_offline_order(tokens, offsets, depth_limit: int, perm, workspace, strea
     _check(_lib.peek_offline_order(n, _arg(tokens, "tokens", torch.int32), _arg(offsets, "offsets"), int(depth_limit),
                                    _arg(perm, "perm", torch.int32, n), _arg(workspace, "workspace"), ws_bytes,
                                    _stream(stream)))
+
+
+PEEK_TYPE_BF16 = 0
+PEEK_TYPE_F16 = 1
+PEEK_TYPE_F8E4M3 = 2
+PEEK_TYPE_I8 = 3
+
+_ROW_TYPES = {torch.bfloat16: PEEK_TYPE_BF16, torch.float16: PEEK_TYPE_F16}
+_PAGE_TYPES = {torch.float8_e4m3fn: PEEK_TYPE_F8E4M3, torch.int8: PEEK_TYPE_I8}
+
+
+class _PoolStruct(ctypes.Structure):
+    _fields_ = [("d_pages", _vp), ("d_scales", _vp), ("num_pages", _i64), ("kv_heads", _i32), ("block_size", _i32),
+                ("head_dim", _i32), ("type", _i32)]
+
+
+class KVPool:
+    """The cache's contents: pages [num_pages, 2, kv_heads, block_size, head_dim] of 8-bit codes (K at 0, V at 1;
+    torch.float8_e4m3fn or torch.int8) and scales float32 [num_pages, 2, kv_heads], tensors of the caller's."""
+
+    def __init__(self, pages, scales):
+        if pages.dtype not in _PAGE_TYPES:
+            raise TypeError(f"pages must be torch.float8_e4m3fn or torch.int8, got {pages.dtype}")
+        if pages.dim() != 5 or pages.shape[1] != 2:
+            raise ValueError("pages must be [num_pages, 2, kv_heads, block_size, head_dim]")
+        if scales.shape != pages.shape[:3]:
+            raise ValueError(f"scales must be {tuple(pages.shape[:3])}, got {tuple(scales.shape)}")
+        self.pages, self.scales = pages, scales
+        self.num_pages, _, self.kv_heads, self.block_size, self.head_dim = pages.shape
+        p, s = _arg(pages, "pages"), _arg(scales, "scales", torch.float32)
+        self._struct = _PoolStruct(p, s, self.num_pages, self.kv_heads, self.block_size, self.head_dim,
+                                   _PAGE_TYPES[pages.dtype])
+        self._ref = ctypes.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, num_pages: int, kv_heads: int, block_size: int, head_dim: int, dtype=torch.float8_e4m3fn,
+              device="cuda") -> "KVPool":
+        """A pool of new memory. Pages hold nothing until peek_kv_append writes them."""
+        pages = torch.empty((num_pages, 2, kv_heads, block_size, head_dim), dtype=dtype, device=device)
+        return cls(pages, torch.ones((num_pages, 2, kv_heads), dtype=torch.float32, device=device))
+
+
+def _rows(t, name: str, dtype, heads: int | None = None, dim: int | None = None, tokens: int | None = None):
+    """Pointer and strides of rows of heads [tokens, heads, dim], whose last dimension is contiguous."""
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, head_dim]")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    n, h, d = t.shape
+    if (heads is not None and h != heads) or (dim is not None and d != dim) or (tokens is not None and n != tokens):
+        raise ValueError(f"{name} must be [{tokens}, {heads}, {dim}], got {list(t.shape)}")
+    token, head, one = t.stride()
+    if one != 1 and d > 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    # a dimension of one element has no stride that matters
+    return t.data_ptr(), token if n > 1 else 0, head if h > 1 else 0
+
+
+def _row_type(t, name: str) -> int:
+    if t.dtype not in _ROW_TYPES:
+        raise TypeError(f"{name} must be torch.bfloat16 or torch.float16, got {t.dtype}")
+    return _ROW_TYPES[t.dtype]
+
+
+def _table(t, n: int):
+    """Pointer, width and row stride of a block table int32[n, max_blocks]; a view of its leading columns is one too."""
+    if t.dtype != torch.int32:
+        raise TypeError(f"block_table must be torch.int32, got {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != n:
+        raise ValueError(f"block_table must be [{n}, max_blocks], got {list(t.shape)}")
+    width = t.shape[1]
+    if width > 1 and t.stride(1) != 1:
+        raise ValueError("block_table's rows must be contiguous")
+    if not t.is_cuda:
+        raise ValueError("block_table must be a device tensor")
+    return t.data_ptr(), width, max(t.stride(0), width) if n > 1 else width
+
+
+def _ws(workspace):
+    return _arg(workspace, "workspace"), 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def peek_kv_append(pool: KVPool, k, v, offsets, context, block_table, stream=None):
+    """Quantises the K and V of new tokens into the pool. k, v [tokens, kv_heads, head_dim] (bfloat16 or float16, any
+    token and head strides), offsets int64[n+1], context int32[n] (tokens cached before), block_table int32[n, *]."""
+    n = _queue_n(offsets)
+    kind = _row_type(k, "k")
+    table = _table(block_table, n)
+    _check(_lib.peek_kv_append(pool._ref, n, k.shape[0], kind, *_rows(k, "k", k.dtype, pool.kv_heads, pool.head_dim),
+                               *_rows(v, "v", k.dtype, pool.kv_heads, pool.head_dim, k.shape[0]),
+                               _arg(offsets, "offsets"), _arg(context, "context", torch.int32, n), *table,
+                               _stream(stream)))
+
+
+def peek_prefill_attention_workspace(n: int, num_tokens: int, q_heads: int, kv_heads: int, head_dim: int,
+                                     max_context: int) -> int:
+    return int(_lib.peek_prefill_attention_workspace(int(n), int(num_tokens), int(q_heads), int(kv_heads),
+                                                     int(head_dim), int(max_context)))
+
+
+def peek_prefill_attention(q, k, v, offsets, out, workspace, pool: KVPool | None = None, prefix=None,
+                           block_table=None, scale: float | None = None, lse=None, stream=None):
+    """Causal attention of packed prompts, each after its cached prefix. q, out [tokens, q_heads, head_dim], k, v
+    [tokens, kv_heads, head_dim] (any token and head strides), offsets int64[n+1], prefix int32[n] (peek_lpm_batch's
+    h) with the pool and block table that hold it; lse float32[tokens, q_heads] or None. scale: 1 / sqrt(head_dim)."""
+    n = _queue_n(offsets)
+    kind = _row_type(q, "q")
+    tokens, q_heads, dim = q.shape if q.dim() == 3 else (0, 0, 0)
+    kv_heads = k.shape[1] if k.dim() == 3 else 0
+    if (pool is None) != (prefix is None) or (pool is None) != (block_table is None):
+        raise ValueError("pool, prefix and block_table must be given together")
+    table = (None, 0, 0) if pool is None else _table(block_table, n)
+    _check(_lib.peek_prefill_attention(
+        None if pool is None else pool._ref, n, tokens, kind, q_heads, kv_heads, dim, *_rows(q, "q", q.dtype),
+        *_rows(k, "k", q.dtype, None, dim, tokens), *_rows(v, "v", q.dtype, kv_heads, dim, tokens),
+        _arg(offsets, "offsets"), _arg(prefix, "prefix", torch.int32, n), *table,
+        dim ** -0.5 if scale is None else scale, *_rows(out, "out", q.dtype, q_heads, dim, tokens),
+        _arg(lse, "lse", torch.float32, tokens * q_heads), *_ws(workspace), _stream(stream)))
+
+
+def peek_decode_attention_workspace(pool: KVPool, n: int, q_heads: int, max_blocks: int, mass: bool = False) -> int:
+    return int(_lib.peek_decode_attention_workspace(pool._ref, int(n), int(q_heads), int(max_blocks), int(mass)))
+
+
+def peek_decode_attention(pool: KVPool, q, context, block_table, out, workspace, scale: float | None = None, lse=None,
+                          mass_in=None, mass=None, stream=None):
+    """Attention of one token per sequence over the context[r] first tokens of its pages. q, out [n, q_heads,
+    head_dim], context int32[n], block_table int32[n, max_blocks]; lse float32[n, q_heads] or None; mass
+    float32[n, kv_heads, max_blocks] or None receives mass_in (or 0) plus the weight on every block."""
+    n = q.shape[0]
+    kind = _row_type(q, "q")
+    q_heads = q.shape[1] if q.dim() == 3 else 0
+    table = _table(block_table, n)
+    masses = n * pool.kv_heads * table[1]
+    _check(_lib.peek_decode_attention(
+        pool._ref, n, kind, q_heads, *_rows(q, "q", q.dtype, None, pool.head_dim),
+        _arg(context, "context", torch.int32, n), *table, pool.head_dim ** -0.5 if scale is None else scale,
+        *_rows(out, "out", q.dtype, q_heads, pool.head_dim, n), _arg(lse, "lse", torch.float32, n * q_heads),
+        _arg(mass_in, "mass_in", torch.float32, masses), _arg(mass, "mass", torch.float32, masses), *_ws(workspace),
+        _stream(stream)))
+
+
+def peek_kv_evict_workspace(n: int, kv_heads: int, max_blocks: int) -> int:
+    return int(_lib.peek_kv_evict_workspace(int(n), int(kv_heads), int(max_blocks)))
+
+
+def peek_kv_evict(context, block_table, mass, keep, block_size: int, sink: int, recent: int, context_out,
+                  block_table_out, mass_out, freed, num_freed, workspace, stream=None):
+    """Drops the blocks of least mass from sequences with more than keep[r] of them. context, keep, context_out,
+    num_freed int32[n]; block_table int32[n, max_blocks] (rows of any stride), block_table_out and freed the same,
+    contiguous; mass, mass_out float32[n, kv_heads, max_blocks]."""
+    i32 = torch.int32
+    if mass.dim() != 3:
+        raise ValueError("mass must be [n, kv_heads, max_blocks]")
+    n, heads, width = mass.shape
+    table = _table(block_table, n)
+    if table[1] != width:
+        raise ValueError(f"block_table has {table[1]} columns, mass {width}")
+    _check(_lib.peek_kv_evict(n, heads, int(block_size), _arg(context, "context", i32, n), *table,
+                              _arg(mass, "mass", torch.float32), _arg(keep, "keep", i32, n), int(sink), int(recent),
+                              _arg(context_out, "context_out", i32, n),
+                              _arg(block_table_out, "block_table_out", i32, n * width),
+                              _arg(mass_out, "mass_out", torch.float32, n * heads * width),
+                              _arg(freed, "freed", i32, n * width), _arg(num_freed, "num_freed", i32, n),
+                              *_ws(workspace), _stream(stream)))

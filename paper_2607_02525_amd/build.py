@@ -20,8 +20,10 @@ FORCED_LIB = os.path.join(HERE, "libpeek_forced.so")
 FORCED = ["-DPEEK_SAMPLE_SEED=0", "-DPEEK_WAIT_SPINS=0"]
 BUILD_DIR = os.path.join(HERE, "_build")
 
+# Nothing of these depends on FORCED: compiled once, linked into both libraries
+UNFORCED = ["peek_kv.hip", "peek_attention.hip"]
 SOURCES = ["peek_host.hip", "peek_walk.hip", "peek_signals.hip", "peek_evict.hip", "peek_blocks.hip",
-           "peek_noalloc.hip"]
+           "peek_noalloc.hip", *UNFORCED]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -55,8 +57,12 @@ def build(verbose: bool = False) -> str:
     objs, forced, jobs = [], [], []
     for src in SOURCES:
         for made, prefix, defines in ((objs, "", []), (forced, "forced_", FORCED)):
+            if src in UNFORCED:
+                prefix = ""
             obj = os.path.join(BUILD_DIR, prefix + src.replace(".hip", ".o"))
             made.append(obj)
+            if made is forced and src in UNFORCED:
+                continue
             jobs.append([HIPCC, *FLAGS, *defines, "-c", os.path.join(CSRC, src), "-o", obj])
     with ThreadPoolExecutor(4) as pool:
         list(pool.map(lambda cmd: _run(cmd, verbose), jobs))

@@ -1,0 +1,108 @@
+// Types and device helpers shared by the calls on the cache's contents
+// (append, attention, eviction by attention weight).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/peek.h"
+
+namespace peek {
+namespace kv {
+
+// Scales stay within 2^-60 .. 2^60: their reciprocals and logarithms are then
+// ordinary floats, and a weight times a scale cannot leave float32's range.
+constexpr float kScaleMin = 0x1p-60f;
+constexpr float kScaleMax = 0x1p60f;
+
+// A pool as kernels see it.
+struct Pool {
+  uint8_t* pages;
+  float* scales;
+  uint32_t num_pages;
+  int32_t heads;
+  int32_t log_block;   // block_size = 1 << log_block
+};
+
+// Rows of heads in 16-bit elements; strides in elements.
+struct Rows {
+  const void* data;
+  int64_t token;
+  int64_t head;
+};
+
+struct Table {
+  const int32_t* ids;
+  int64_t stride;
+  int32_t width;       // max_blocks
+};
+
+// Page of block b of sequence r; a page outside the pool reads as page 0
+// (the header's promise: such an id never leads outside the pool's memory).
+__device__ __forceinline__ uint32_t page_of(const Table& t, const Pool& p, int32_t r, int32_t b) {
+  const uint32_t id = (uint32_t)t.ids[(int64_t)r * t.stride + b];
+  return id < p.num_pages ? id : 0u;
+}
+
+// Tokens of a sequence as the table can hold them.
+__device__ __forceinline__ int32_t clip_tokens(int32_t tokens, int32_t width, int32_t log_block) {
+  const int64_t most = (int64_t)width << log_block;
+  return tokens < 0 ? 0 : (int64_t)tokens > most ? (int32_t)most : tokens;
+}
+
+// A 16-bit element's value and its rounding to nearest, ties to even.
+template <int TYPE>
+__device__ __forceinline__ float to_float(uint16_t x) {
+  if constexpr (TYPE == PEEK_TYPE_BF16) {
+    return __builtin_bit_cast(float, (uint32_t)x << 16);
+  } else {
+    return (float)__builtin_bit_cast(_Float16, x);
+  }
+}
+template <int TYPE>
+__device__ __forceinline__ uint16_t from_float(float x) {
+  if constexpr (TYPE == PEEK_TYPE_BF16) {
+    return __builtin_bit_cast(uint16_t, (__bf16)x);
+  } else {
+    return __builtin_bit_cast(uint16_t, (_Float16)x);
+  }
+}
+
+// The value of an 8-bit code before its scale.
+template <int FMT>
+__device__ __forceinline__ float code_value(uint8_t c) {
+  if constexpr (FMT == PEEK_TYPE_F8E4M3) {
+    return __builtin_amdgcn_cvt_f32_fp8((int)c, 0);
+  } else {
+    return (float)(int8_t)c;
+  }
+}
+
+// Sequence that holds row `at` of packed rows: the last r with offsets[r] <= at
+// (offsets non-decreasing), in [0, n).
+__device__ __forceinline__ int32_t sequence_of(const int64_t* __restrict__ offsets, int32_t n, int64_t at) {
+  int32_t lo = 0, hi = n;   // offsets[lo] <= at < offsets[hi], as far as they are in order
+  while (hi - lo > 1) {
+    const int32_t mid = lo + (hi - lo) / 2;
+    if (offsets[mid] <= at) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+}  // namespace kv
+
+// Argument checks shared by the entry points (peek_kv.hip).
+peek_status check_pool(const peek_kv_pool* pool, kv::Pool* out);
+peek_status check_rows(const char* what, const void* data, int64_t token_stride, int64_t head_stride);
+peek_status check_table(const int32_t* table, int32_t max_blocks, int64_t stride, int32_t block_size);
+
+// With PEEK_VALIDATE: offsets (nullable) non-decreasing within num_tokens,
+// lengths within the table, the pages that they reach (with the new tokens,
+// where `appends`) inside the pool. Waits for `st`. PEEK_OK when off.
+peek_status validate_kv(int32_t n, const int64_t* d_offsets, int64_t num_tokens, const int32_t* d_len, bool appends,
+                        const int32_t* d_table, int32_t max_blocks, int64_t table_stride, int32_t block_size,
+                        int64_t num_pages, hipStream_t st);
+
+}  // namespace peek

@@ -1,0 +1,433 @@
+// The cache's contents on gfx950: quantising new tokens into 8-bit pages, and
+// evicting the blocks of a sequence that attention hardly reads.
+#include "peek_internal.h"
+#include "peek_kv.h"
+#include "peek_validate.h"
+
+namespace peek {
+
+using kv::Pool;
+using kv::Rows;
+using kv::Table;
+
+namespace {
+
+constexpr int kWave = 64;
+
+// ------------------------------------------------------------------ append
+//
+// A wavefront owns one (block, K or V, head): it alone writes that block's
+// codes and scale. Which block: sequence r's first is given the slot
+// offsets[r] / B + 2 r, which leaves every sequence room for the blocks it
+// can touch (new tokens / B + 2 at most), so slots need no counting; a slot past its
+// sequence's last block has nothing to do.
+
+__device__ __forceinline__ float wave_max(float x) {
+  for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+  return x;
+}
+
+// The scale of a block whose largest finite magnitude is `most`.
+template <int FMT>
+__device__ __forceinline__ float scale_of(float most) {
+  if constexpr (FMT == PEEK_TYPE_F8E4M3) {
+    // most = m * 2^e with m in [1, 2); 448 = 1.75 * 2^8
+    const uint32_t bits = __builtin_bit_cast(uint32_t, most);
+    int32_t e = (int32_t)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    e = max(-60, min(60, e));
+    return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
+  } else {
+    return fminf(fmaxf(most / 127.0f, kv::kScaleMin), kv::kScaleMax);
+  }
+}
+
+template <int FMT>
+__device__ __forceinline__ uint8_t code_of(float x, float scale) {
+  const float y = x / scale;
+  if constexpr (FMT == PEEK_TYPE_F8E4M3) {
+    const float z = y < -448.0f ? -448.0f : y > 448.0f ? 448.0f : y;   // NaN stays
+    return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(z, z, 0, false);
+  } else {
+    const float z = y != y ? 0.0f : y < -127.0f ? -127.0f : y > 127.0f ? 127.0f : y;
+    return (uint8_t)(int8_t)(int32_t)rintf(z);
+  }
+}
+
+template <int TYPE, int FMT>
+__global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, int32_t n, int64_t num_tokens,
+                                                   int32_t dim, const int64_t* __restrict__ offsets,
+                                                   const int32_t* __restrict__ context, Table table, int64_t slots) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t unit = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  const int32_t parts = 2 * pool.heads;
+  const int64_t slot = unit / parts;
+  if (slot >= slots) return;
+  const int32_t part = (int32_t)(unit % parts), is_v = part / pool.heads, head = part % pool.heads;
+  const int32_t lb = pool.log_block;
+  // the last r with offsets[r] / B + 2 r <= slot
+  int32_t lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int32_t mid = lo + (hi - lo) / 2;
+    if ((offsets[mid] >> lb) + 2 * (int64_t)mid <= slot) lo = mid;
+    else hi = mid;
+  }
+  const int32_t r = lo;
+  const int64_t first = max((int64_t)0, offsets[r]), end = min(num_tokens, offsets[r + 1]);
+  const int64_t ctx = max(0, context[r]);
+  const int64_t b = (ctx >> lb) + slot - ((offsets[r] >> lb) + 2 * (int64_t)r);
+  // positions of the block's new tokens
+  const int64_t from = max(ctx, b << lb), to = min(ctx + (end - first), (b + 1) << lb);
+  if (b < 0 || b >= table.width || from >= to) return;
+  const uint32_t page = (uint32_t)table.ids[(int64_t)r * table.stride + b];
+  if (page >= pool.num_pages) return;
+  const int32_t old = (int32_t)(from - (b << lb)), count = (int32_t)(to - from);
+
+  const Rows& src = is_v ? v : k;
+  const uint16_t* x = (const uint16_t*)src.data + (first + from - ctx) * src.token + head * src.head;
+  const int64_t at = ((int64_t)page * 2 + is_v) * pool.heads + head;
+  uint8_t* codes = pool.pages + ((at << lb) * dim);
+  float most = 0.0f;
+  for (int32_t i = lane; i < count * dim; i += kWave) {
+    const float a = fabsf(kv::to_float<TYPE>(x[(int64_t)(i / dim) * src.token + i % dim]));
+    if (a < __builtin_inff()) most = fmaxf(most, a);
+  }
+  float scale = scale_of<FMT>(wave_max(most));
+  if (old > 0) {
+    const float held = pool.scales[at];
+    if (scale > held) {
+      for (int32_t i = lane; i < old * dim; i += kWave) codes[i] = code_of<FMT>(kv::code_value<FMT>(codes[i]) * held, scale);
+    } else {
+      scale = held;
+    }
+  }
+  for (int32_t i = lane; i < count * dim; i += kWave)
+    codes[old * dim + i] = code_of<FMT>(kv::to_float<TYPE>(x[(int64_t)(i / dim) * src.token + i % dim]), scale);
+  if (lane == 0) pool.scales[at] = scale;
+}
+
+// ---------------------------------------------------------------- eviction
+//
+// One workgroup per sequence. Scores become keys whose unsigned order is
+// theirs; four counting passes of eight bits find the key of the last block to go,
+// and a pass over the blocks in order drops those below it and the first of those
+// equal to it.
+
+constexpr int kEvictThreads = 256;
+
+__device__ __forceinline__ uint32_t score_key(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);   // -0 counts as 0
+  return (u >> 31) ? ~u : u | 0x80000000u;
+}
+
+// Exclusive sum over the workgroup; *total gets the whole.
+__device__ __forceinline__ int32_t group_sum(int32_t x, int32_t* s_part, int32_t* total) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  int32_t inc = x;
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int32_t y = __shfl_up(inc, d);
+    if (lane >= d) inc += y;
+  }
+  if (lane == kWave - 1) s_part[wave] = inc;
+  __syncthreads();
+  int32_t before = 0, all = 0;
+  for (int w = 0; w < kEvictThreads / kWave; ++w) {
+    if (w < wave) before += s_part[w];
+    all += s_part[w];
+  }
+  __syncthreads();
+  *total = all;
+  return before + inc - x;
+}
+
+__global__ __launch_bounds__(kEvictThreads) void k_kv_evict(
+    int32_t heads, int32_t log_block, const int32_t* context, Table table, const float* __restrict__ mass,
+    const int32_t* __restrict__ keep, int32_t sink, int32_t recent, int32_t* context_out,
+    int32_t* __restrict__ table_out, float* __restrict__ mass_out, int32_t* __restrict__ freed,
+    int32_t* __restrict__ num_freed, uint32_t* __restrict__ keys) {
+  __shared__ int32_t s_part[kEvictThreads / kWave];
+  __shared__ int32_t s_count[256];
+  __shared__ uint32_t s_prefix;
+  __shared__ int32_t s_left;
+  const int32_t r = blockIdx.x, t = threadIdx.x, width = table.width;
+  const int32_t* ids = table.ids + (int64_t)r * table.stride;
+  const float* m = mass + (int64_t)r * heads * width;
+  uint32_t* key = keys + (int64_t)r * width;
+  const int32_t ctx = context[r];
+  const int32_t nb = (int32_t)(((int64_t)kv::clip_tokens(ctx, width, log_block) + (1 << log_block) - 1) >> log_block);
+  const int32_t lo = min(sink, nb), hi = (int32_t)max((int64_t)lo, (int64_t)nb - recent);
+  const int32_t drop = (int32_t)min((int64_t)(hi - lo), max((int64_t)0, (int64_t)nb - max(0, keep[r])));
+
+  uint32_t last = 0;       // key of the last block to go
+  int32_t equal = 0;       // how many of that key go
+  if (drop > 0) {
+    for (int32_t b = lo + t; b < hi; b += kEvictThreads) {
+      float s = m[b];
+      for (int32_t h = 1; h < heads; ++h) s += m[(int64_t)h * width + b];
+      key[b] = score_key(s);
+    }
+    if (t == 0) { s_prefix = 0; s_left = drop; }
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      s_count[t] = 0;
+      __syncthreads();
+      const uint32_t prefix = s_prefix;
+      const int32_t left = s_left;
+      const uint32_t above = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
+      for (int32_t b = lo + t; b < hi; b += kEvictThreads)
+        if ((key[b] & above) == prefix) atomicAdd(&s_count[(key[b] >> shift) & 255], 1);
+      __syncthreads();
+      const int32_t c = s_count[t];
+      int32_t all;
+      const int32_t before = group_sum(c, s_part, &all);
+      if (before < left && left <= before + c) {
+        s_prefix = prefix | ((uint32_t)t << shift);
+        s_left = left - before;
+      }
+      __syncthreads();
+    }
+    last = s_prefix;
+    equal = s_left;
+  }
+
+  int32_t gone = 0, ties = 0;
+  for (int32_t base = 0; base < width; base += kEvictThreads) {
+    const int32_t b = base + t;
+    const bool able = drop > 0 && b >= lo && b < hi;
+    const uint32_t k = able ? key[b] : 0;
+    int32_t all_ties, all_gone;
+    const int32_t tie = ties + group_sum(able && k == last, s_part, &all_ties);
+    const bool goes = able && (k < last || (k == last && tie < equal));
+    const int32_t before = gone + group_sum(goes, s_part, &all_gone);
+    if (b < width) {
+      const int32_t id = ids[b];
+      if (goes) {
+        freed[(int64_t)r * width + before] = id;
+      } else {
+        table_out[(int64_t)r * width + b - before] = id;
+        for (int32_t h = 0; h < heads; ++h)
+          mass_out[((int64_t)r * heads + h) * width + b - before] = m[(int64_t)h * width + b];
+      }
+    }
+    ties += all_ties;
+    gone += all_gone;
+  }
+  for (int32_t b = t; b < width; b += kEvictThreads) {
+    if (b >= drop) freed[(int64_t)r * width + b] = -1;
+    if (b >= width - drop) {
+      table_out[(int64_t)r * width + b] = -1;
+      for (int32_t h = 0; h < heads; ++h) mass_out[((int64_t)r * heads + h) * width + b] = 0.0f;
+    }
+  }
+  if (t == 0) {
+    num_freed[r] = drop;
+    context_out[r] = ctx - (drop << log_block);
+  }
+}
+
+// -------------------------------------------------------------- validation
+__global__ void k_validate_kv(int32_t n, const int64_t* __restrict__ offsets, int64_t num_tokens,
+                              const int32_t* __restrict__ len, bool appends, Table table, int32_t log_block,
+                              int64_t num_pages, int32_t* __restrict__ bad) {
+  const int32_t r = blockIdx.x;
+  int32_t f = 0;
+  int64_t fresh = 0;
+  if (offsets != nullptr) {
+    const int64_t a = offsets[r], b = offsets[r + 1];
+    if (a < 0 || b < a || b > num_tokens) f |= 1;
+    else fresh = b - a;
+  }
+  if (len != nullptr) {
+    const int64_t held = len[r], all = held + (appends ? fresh : 0);
+    if (held < 0 || all > ((int64_t)table.width << log_block)) {
+      f |= 2;
+    } else {
+      const int32_t from = appends ? (int32_t)(held >> log_block) : 0;
+      const int32_t to = (int32_t)((all + (1 << log_block) - 1) >> log_block);
+      for (int32_t b = from + (int32_t)threadIdx.x; b < to; b += (int32_t)blockDim.x) {
+        const int32_t id = table.ids[(int64_t)r * table.stride + b];
+        if (id < 0 || id >= num_pages) f |= 4;
+      }
+    }
+  }
+  if (f) atomicOr(bad, f);
+}
+
+__global__ void k_clear_flag(int32_t* flag) { *flag = 0; }
+
+}  // namespace
+
+peek_status validate_kv(int32_t n, const int64_t* d_offsets, int64_t num_tokens, const int32_t* d_len, bool appends,
+                        const int32_t* d_table, int32_t max_blocks, int64_t table_stride, int32_t block_size,
+                        int64_t num_pages, hipStream_t st) {
+  if (!validation_enabled() || n <= 0) return PEEK_OK;
+  int32_t* d_bad = nullptr;
+  PEEK_HIP_TRY(hipMalloc((void**)&d_bad, sizeof(int32_t)));
+  int32_t bad = 0;
+  hipLaunchKernelGGL(k_clear_flag, dim3(1), dim3(1), 0, st, d_bad);
+  hipLaunchKernelGGL(k_validate_kv, dim3((unsigned)n), dim3(64), 0, st, n, d_offsets, num_tokens, d_len, appends,
+                     Table{d_table, table_stride, max_blocks}, __builtin_ctz((unsigned)block_size), num_pages, d_bad);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess) e = hipMemcpyAsync(&bad, d_bad, sizeof(int32_t), hipMemcpyDeviceToHost, st);
+  if (e == hipSuccess) e = hipStreamSynchronize(st);
+  (void)hipFree(d_bad);
+  if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "input validation failed to run: %s", hipGetErrorString(e));
+  if (bad & 1)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "d_offsets must be non-decreasing from 0 or more and end within num_tokens");
+  if (bad & 2) return fail(PEEK_ERR_INVALID_ARGUMENT, "a sequence has fewer than 0 tokens or more than its table holds");
+  if (bad & 4) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_block_table names pages outside the pool");
+  return PEEK_OK;
+}
+
+peek_status check_pool(const peek_kv_pool* p, Pool* out) {
+  if (!p) return fail(PEEK_ERR_INVALID_ARGUMENT, "pool is NULL");
+  if (!p->d_pages || !p->d_scales) return fail(PEEK_ERR_INVALID_ARGUMENT, "the pool's d_pages and d_scales must not be NULL");
+  if ((reinterpret_cast<uintptr_t>(p->d_pages) & 15) != 0)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "the pool's d_pages must be 16-byte aligned");
+  if (p->num_pages < 1 || p->num_pages > INT32_MAX)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "num_pages must be in [1, 2^31) (got %lld)", (long long)p->num_pages);
+  if (p->kv_heads < 1 || p->kv_heads > 1024)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "kv_heads must be in [1, 1024] (got %d)", p->kv_heads);
+  if (p->block_size < 4 || p->block_size > 256 || (p->block_size & (p->block_size - 1)) != 0)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "block_size must be a power of two in [4, 256] (got %d)", p->block_size);
+  if (p->head_dim != 64 && p->head_dim != 128)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "head_dim must be 64 or 128 (got %d)", p->head_dim);
+  if (p->type != PEEK_TYPE_F8E4M3 && p->type != PEEK_TYPE_I8)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "the pool's type must be PEEK_TYPE_F8E4M3 or PEEK_TYPE_I8 (got %d)", p->type);
+  *out = Pool{(uint8_t*)p->d_pages, p->d_scales, (uint32_t)p->num_pages, p->kv_heads,
+              __builtin_ctz((unsigned)p->block_size)};
+  return PEEK_OK;
+}
+
+peek_status check_rows(const char* what, const void* data, int64_t token_stride, int64_t head_stride) {
+  if (!data) return fail(PEEK_ERR_INVALID_ARGUMENT, "%s must not be NULL", what);
+  if ((reinterpret_cast<uintptr_t>(data) & 15) != 0)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "%s must be 16-byte aligned", what);
+  if (token_stride < 0 || head_stride < 0 || ((token_stride | head_stride) & 7) != 0)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "%s: strides must be multiples of 8 from 0 on (got %lld, %lld)", what,
+                (long long)token_stride, (long long)head_stride);
+  return PEEK_OK;
+}
+
+peek_status check_table(const int32_t* table, int32_t max_blocks, int64_t stride, int32_t block_size) {
+  if (max_blocks < 0 || stride < max_blocks)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "max_blocks must be >= 0 and table_stride at least that (got %d, %lld)",
+                max_blocks, (long long)stride);
+  if ((int64_t)max_blocks * block_size > INT32_MAX)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "max_blocks * block_size must be below 2^31 (got %d * %d)", max_blocks,
+                block_size);
+  if (!table && max_blocks > 0) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_block_table must not be NULL");
+  return PEEK_OK;
+}
+
+namespace {
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+}  // namespace
+}  // namespace peek
+
+using namespace peek;
+
+extern "C" {
+
+peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_tokens, int32_t type, const void* d_k,
+                           int64_t k_token_stride, int64_t k_head_stride, const void* d_v, int64_t v_token_stride,
+                           int64_t v_head_stride, const int64_t* d_offsets, const int32_t* d_context,
+                           const int32_t* d_block_table, int32_t max_blocks, int64_t table_stride, void* stream) {
+  return guarded([&]() -> peek_status {
+    clear_error();
+    Pool p;
+    peek_status s = check_pool(pool, &p);
+    if (s != PEEK_OK) return s;
+    if (n < 0 || num_tokens < 0)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "n and num_tokens must be >= 0 (got %d, %lld)", n, (long long)num_tokens);
+    if (type != PEEK_TYPE_BF16 && type != PEEK_TYPE_F16)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "type must be PEEK_TYPE_BF16 or PEEK_TYPE_F16 (got %d)", type);
+    s = check_table(d_block_table, max_blocks, table_stride, pool->block_size);
+    if (s != PEEK_OK) return s;
+    if (n == 0 || num_tokens == 0) return PEEK_OK;
+    s = check_rows("d_k", d_k, k_token_stride, k_head_stride);
+    if (s != PEEK_OK) return s;
+    s = check_rows("d_v", d_v, v_token_stride, v_head_stride);
+    if (s != PEEK_OK) return s;
+    if (!d_offsets || !d_context)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "d_offsets and d_context must not be NULL");
+    const int64_t slots = (num_tokens >> p.log_block) + 2 * (int64_t)n;
+    const int64_t groups = (slots * 2 * p.heads + 3) / 4;
+    if (groups >= (1 << 24)) return fail(PEEK_ERR_INVALID_ARGUMENT, "too many tokens for one call (%lld)", (long long)num_tokens);
+    hipStream_t st = (hipStream_t)stream;
+    s = validate_kv(n, d_offsets, num_tokens, d_context, true, d_block_table, max_blocks, table_stride,
+                    pool->block_size, pool->num_pages, st);
+    if (s != PEEK_OK) return s;
+    const Rows k{d_k, k_token_stride, k_head_stride}, v{d_v, v_token_stride, v_head_stride};
+    const Table t{d_block_table, table_stride, max_blocks};
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, st, p, k, v, n, num_tokens, pool->head_dim,
+                         d_offsets, d_context, t, slots);
+    };
+    const bool bf = type == PEEK_TYPE_BF16, f8 = pool->type == PEEK_TYPE_F8E4M3;
+    if (bf && f8) go(k_kv_append<PEEK_TYPE_BF16, PEEK_TYPE_F8E4M3>);
+    else if (bf) go(k_kv_append<PEEK_TYPE_BF16, PEEK_TYPE_I8>);
+    else if (f8) go(k_kv_append<PEEK_TYPE_F16, PEEK_TYPE_F8E4M3>);
+    else go(k_kv_append<PEEK_TYPE_F16, PEEK_TYPE_I8>);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "append launch failed: %s", hipGetErrorString(e));
+    return PEEK_OK;
+  });
+}
+
+size_t peek_kv_evict_workspace(int32_t n, int32_t kv_heads, int32_t max_blocks) {
+  if (n < 0 || kv_heads < 1 || max_blocks < 0) return 0;
+  return ((size_t)n * max_blocks * sizeof(uint32_t) + 255) & ~(size_t)255;
+}
+
+peek_status peek_kv_evict(int32_t n, int32_t kv_heads, int32_t block_size, const int32_t* d_context,
+                          const int32_t* d_block_table, int32_t max_blocks, int64_t table_stride, const float* d_mass,
+                          const int32_t* d_keep, int32_t sink, int32_t recent, int32_t* d_context_out,
+                          int32_t* d_table_out, float* d_mass_out, int32_t* d_freed, int32_t* d_num_freed,
+                          void* d_workspace, size_t workspace_bytes, void* stream) {
+  return guarded([&]() -> peek_status {
+    clear_error();
+    if (n < 0 || n >= (1 << 22)) return fail(PEEK_ERR_INVALID_ARGUMENT, "n must be in [0, 2^22) (got %d)", n);
+    if (kv_heads < 1 || kv_heads > 1024)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "kv_heads must be in [1, 1024] (got %d)", kv_heads);
+    if (block_size < 4 || block_size > 256 || (block_size & (block_size - 1)) != 0)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "block_size must be a power of two in [4, 256] (got %d)", block_size);
+    if (sink < 0 || recent < 1)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "sink must be >= 0 and recent >= 1 (got %d, %d)", sink, recent);
+    peek_status s = check_table(d_block_table, max_blocks, table_stride, block_size);
+    if (s != PEEK_OK) return s;
+    if (n == 0) return PEEK_OK;
+    if (!d_context || !d_keep || !d_context_out || !d_num_freed)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "d_context, d_keep, d_context_out and d_num_freed must not be NULL");
+    if (max_blocks > 0 && (!d_mass || !d_table_out || !d_mass_out || !d_freed))
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "d_mass, d_table_out, d_mass_out and d_freed must not be NULL");
+    const size_t row = (size_t)n * max_blocks * 4, in_row = ((size_t)(n - 1) * table_stride + max_blocks) * 4;
+    if (overlap(d_table_out, row, d_block_table, in_row) || overlap(d_freed, row, d_block_table, in_row) ||
+        overlap(d_mass_out, row * kv_heads, d_mass, row * kv_heads))
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "the outputs must not overlap the table and the masses they are made from");
+    const size_t need = peek_kv_evict_workspace(n, kv_heads, max_blocks);
+    if (need > 0) {
+      if (!d_workspace) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_workspace is NULL");
+      if (workspace_bytes < need)
+        return fail(PEEK_ERR_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes, got %zu", need, workspace_bytes);
+      if ((reinterpret_cast<uintptr_t>(d_workspace) & 255) != 0)
+        return fail(PEEK_ERR_INVALID_ARGUMENT, "d_workspace must be 256-byte aligned");
+    }
+    hipStream_t st = (hipStream_t)stream;
+    s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, block_size, INT32_MAX, st);
+    if (s != PEEK_OK) return s;
+    hipLaunchKernelGGL(k_kv_evict, dim3((unsigned)n), dim3(kEvictThreads), 0, st, kv_heads,
+                       __builtin_ctz((unsigned)block_size), d_context, Table{d_block_table, table_stride, max_blocks},
+                       d_mass, d_keep, sink, recent, d_context_out, d_table_out, d_mass_out, d_freed, d_num_freed,
+                       (uint32_t*)d_workspace);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "eviction launch failed: %s", hipGetErrorString(e));
+    return PEEK_OK;
+  });
+}
+
+}  // extern "C"
