@@ -4,7 +4,9 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/peek.h"
 
@@ -97,6 +99,35 @@ __device__ __forceinline__ int32_t sequence_of(const int64_t* __restrict__ offse
 peek_status check_pool(const peek_kv_pool* pool, kv::Pool* out);
 peek_status check_rows(const char* what, const void* data, int64_t token_stride, int64_t head_stride);
 peek_status check_table(const int32_t* table, int32_t max_blocks, int64_t stride, int32_t block_size);
+
+peek_status check_heads(int32_t type, int32_t q_heads, int32_t kv_heads, float scale);
+peek_status check_workspace(const void* d_workspace, size_t bytes, size_t need);
+
+// A caller's scale as the kernels take it: a factor >= 0 of base-2 logits, and
+// what to do to q's bits so that it is one. With a factor of at least 2^-100,
+// a masked logit of -infinity stays one.
+inline void set_scale(float scale, float* factor, uint32_t* q_flip, uint32_t* q_mask) {
+  const float f = std::fabs(scale) * 1.44269504088896341f;
+  const bool none = f < 0x1p-100f;
+  *factor = none ? 1.0f : std::fmin(f, 3e38f);
+  *q_flip = !none && scale < 0 ? 0x80008000u : 0u;
+  *q_mask = none ? 0u : 0xffffffffu;
+}
+
+// Calls f with the element type, the cache format and the head's width as constants.
+template <typename F>
+void with_types(int32_t type, int32_t format, int32_t dim, F&& f) {
+  auto by_dim = [&](auto t, auto m) {
+    if (dim == 64) f(t, m, std::integral_constant<int, 64>{});
+    else f(t, m, std::integral_constant<int, 128>{});
+  };
+  auto by_format = [&](auto t) {
+    if (format == PEEK_TYPE_F8E4M3) by_dim(t, std::integral_constant<int, PEEK_TYPE_F8E4M3>{});
+    else by_dim(t, std::integral_constant<int, PEEK_TYPE_I8>{});
+  };
+  if (type == PEEK_TYPE_BF16) by_format(std::integral_constant<int, PEEK_TYPE_BF16>{});
+  else by_format(std::integral_constant<int, PEEK_TYPE_F16>{});
+}
 
 // With PEEK_VALIDATE: offsets (nullable) non-decreasing within num_tokens,
 // lengths within the table, the pages that they reach (with the new tokens,

@@ -319,6 +319,25 @@ peek_status check_table(const int32_t* table, int32_t max_blocks, int64_t stride
   return PEEK_OK;
 }
 
+peek_status check_heads(int32_t type, int32_t q_heads, int32_t kv_heads, float scale) {
+  if (type != PEEK_TYPE_BF16 && type != PEEK_TYPE_F16)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "type must be PEEK_TYPE_BF16 or PEEK_TYPE_F16 (got %d)", type);
+  if (q_heads < 1 || q_heads > 65536 || q_heads % kv_heads != 0)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "q_heads must be a multiple of kv_heads in [1, 65536] (got %d and %d)",
+                q_heads, kv_heads);
+  if (!std::isfinite(scale)) return fail(PEEK_ERR_INVALID_ARGUMENT, "scale must be finite");
+  return PEEK_OK;
+}
+
+peek_status check_workspace(const void* d_workspace, size_t bytes, size_t need) {
+  if (need == 0) return PEEK_OK;
+  if (!d_workspace) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_workspace is NULL");
+  if (bytes < need) return fail(PEEK_ERR_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes, got %zu", need, bytes);
+  if ((reinterpret_cast<uintptr_t>(d_workspace) & 255) != 0)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "d_workspace must be 256-byte aligned");
+  return PEEK_OK;
+}
+
 namespace {
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {

@@ -1,0 +1,431 @@
+// Attention of packed prompts after their cached prefixes, on gfx950.
+//
+// One workgroup of eight wavefronts takes 256 rows of one kv head of one
+// sequence, a row being a (token, query head of the group) pair in that
+// order, so that a few new tokens of a wide group still fill a tile and every
+// row of it shares the keys. It goes over the keys in tiles of 64, first the
+// cached prefix, then the sequence's own tokens up to its last row, and keeps
+// the running maximum and sum of every row's softmax (one pass over the keys).
+//
+// A wavefront has 32 rows. K times Q^T leaves lane l with keys of row l % 32
+// alone: its maximum and sum need one exchange with the lane 32 away,
+// and its weights are already the operand of V^T times weights (peek_mfma.h).
+// K and V tiles lie in LDS as 16-bit rows, two buffers of each; 16-byte
+// pieces of a row are permuted by the row's number so that reads down a
+// column of rows spread over the banks. V is read by transposing loads.
+//
+// Own tokens go from memory to LDS directly. Cached codes are widened to 16
+// bits on the way, which is exact, and their scales never touch them: K's
+// multiplies the logit, and V's goes into the weight as an exponent,
+//   w_j s_j = 2^(x_j + log2 s_j - m),   sum of weights = sum_j (w_j s_j) / s_j,
+// with m the running maximum of x_j + log2 s_j, so weights times scales stay
+// within [0, 2^8] in either 16-bit type.
+//
+// Rows and keys past the end: rows are clamped to the last one and not
+// stored; keys are clamped to the last one and masked, so nothing outside the
+// sequence is read.
+#include "peek_internal.h"
+#include "peek_kv.h"
+#include "peek_mfma.h"
+#include "peek_validate.h"
+
+namespace peek {
+
+using kv::Pool;
+using kv::Rows;
+using kv::Table;
+using namespace mm;
+
+namespace {
+
+constexpr int kWave = 64;
+constexpr int kWaves = 8;
+constexpr int kThreads = kWave * kWaves;
+constexpr int kRows = 32 * kWaves;    // rows of a tile
+constexpr int kKeys = 64;             // keys of a tile
+
+// How far (in powers of two) a row's maximum may rise before what it has
+// summed is scaled down: weights stay below 2^8, and most tiles scale nothing.
+constexpr float kSlack = 8.0f;
+constexpr float kNone = -1e30f;       // a maximum of nothing; finite, so that differences are numbers
+
+struct Prefill {
+  Pool pool;
+  Rows q, k, v;
+  const int64_t* offsets;
+  const int32_t* prefix;
+  Table table;
+  uint16_t* out;
+  int64_t out_token, out_head;
+  float* lse;
+  int64_t num_tokens;
+  int32_t n, group, kv_heads;
+  float scale;                        // of logits, in powers of two: >= 0
+  uint32_t q_flip;                    // sign bits to flip in q, where the caller's scale is negative
+  uint32_t q_mask;                    // 0 where the caller's scale is 0
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
+
+// Where the 16-byte piece c of row t lies in a tile of D / 8 pieces a row.
+template <int D>
+__device__ __forceinline__ uint32_t k_piece(uint32_t t, uint32_t c) {
+  return t * (D / 8) + (c ^ (t & (D / 8 - 1)));
+}
+// V is read by 16 lanes at a time from two adjacent pieces of four rows.
+template <int D>
+__device__ __forceinline__ uint32_t v_piece(uint32_t t, uint32_t c) {
+  return t * (D / 8) + (c ^ ((t << 1) & (D / 8 - 1)));
+}
+
+typedef __attribute__((address_space(3))) s4 lds_s4;
+
+template <int TYPE, int FMT, int D>
+struct Tile {
+  static constexpr int kPieces = D / 8;                      // of a row
+  static constexpr int kBytes = kKeys * D * 2;
+  static constexpr int kSteps = D / 16;                      // k steps of K Q^T
+  static constexpr int kParts = D / 32;                      // 32-wide parts of the output
+  static constexpr int kUnits = 2 * kKeys * (D / 16);        // 16-code units of a cached tile, K and V
+  static constexpr int kUnitsEach = kUnits / kThreads;       // 2 (D = 128) or 1
+
+  u4 q[kSteps];
+  f16 acc[kParts];
+  float top, sum;
+
+  // weights of 64 keys and what they add
+  template <bool CACHED>
+  __device__ __forceinline__ void step(const uint8_t* ks, const uint8_t* vs, const f4* scales, int lane, float scale,
+                                       bool masked, int32_t seen) {
+    const int col = lane & 31, half = lane >> 5;
+    f16 s[2] = {};
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const u4 a = *(const u4*)(ks + 16 * k_piece<D>(col + 32 * j, 2 * i + half));
+        s[j] = mul32<TYPE>(a, q[i], s[j]);
+      }
+    }
+    float inv[8];
+    if constexpr (CACHED) {      // logits with their scales; keys 4 g .. 4 g + 3 share one
+#pragma unroll
+      for (int g = 0; g < 8; ++g) {
+        const f4 c = scales[2 * g + half];
+        inv[g] = c[2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = (g & 3) * 4 + e;
+          s[g >> 2][at] = fmaf(s[g >> 2][at], c[0], c[1]);
+        }
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int key = 32 * j + 8 * (e >> 2) + 4 * half + (e & 3);
+          s[j][e] = key < seen ? s[j][e] : -__builtin_inff();
+        }
+    }
+    float most = s[0][0];
+#pragma unroll
+    for (int e = 1; e < 32; ++e) most = fmaxf(most, s[e >> 4][e & 15]);
+    most = max_halves(most);
+    if constexpr (!CACHED) most *= scale;
+    if (__any(most > top + kSlack)) {
+      const float next = most > top + kSlack ? most : top;
+      const float fall = exp2_fast(top - next);
+      top = next;
+      sum *= fall;
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) acc[p] *= fall;
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if constexpr (CACHED) {
+          s[j][e] = exp2_fast(s[j][e] - top);
+          sum = fmaf(s[j][e], inv[4 * j + (e >> 2)], sum);
+        } else {
+          s[j][e] = exp2_fast(fmaf(s[j][e], scale, -top));
+          sum += s[j][e];
+        }
+      }
+    // lane l reads, for the 16 lanes of its group, four tokens of 16 columns
+    const uint32_t i16 = lane & 15, wide = (lane >> 4) & 1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f16& w = s[i >> 1];
+      const int o = (i & 1) * 8;
+      u4 b;
+      b[0] = pack2<TYPE>(w[o + 0], w[o + 1]);
+      b[1] = pack2<TYPE>(w[o + 2], w[o + 3]);
+      b[2] = pack2<TYPE>(w[o + 4], w[o + 5]);
+      b[3] = pack2<TYPE>(w[o + 6], w[o + 7]);
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) {
+        u2 part[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t t = 16 * i + 8 * h + 4 * half + (i16 >> 2);
+          const uint32_t at = 16 * v_piece<D>(t, 4 * p + 2 * wide + ((i16 >> 1) & 1)) + 8 * (i16 & 1);
+          part[h] = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(vs + at)));
+        }
+        acc[p] = mul32<TYPE>((u4){part[0][0], part[0][1], part[1][0], part[1][1]}, b, acc[p]);
+      }
+    }
+  }
+};
+
+template <int TYPE, int FMT, int D>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_prefill(Prefill a) {
+  using T = Tile<TYPE, FMT, D>;
+  __shared__ __attribute__((aligned(1024))) uint8_t s_k[2][T::kBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t s_v[2][T::kBytes];
+  __shared__ f4 s_scale[2][kKeys / 4];
+
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  // kv heads side by side (each on XCDs of its own where there are eight), the
+  // last rows of the last sequences first: they have the most keys
+  const int32_t head = blockIdx.x % a.kv_heads;
+  const int64_t slot = (gridDim.x - 1 - blockIdx.x) / a.kv_heads;
+  // the last sequence r with offsets[r] * group / kRows + r <= slot: every
+  // sequence has a slot for each of its tiles, some one more
+  int32_t lo = 0, hi = a.n;
+  while (hi - lo > 1) {
+    const int32_t mid = lo + (hi - lo) / 2;
+    if (a.offsets[mid] * a.group / kRows + mid <= slot) lo = mid;
+    else hi = mid;
+  }
+  const int32_t r = lo;
+  const int64_t first = a.offsets[r], end = min(a.num_tokens, a.offsets[r + 1]);
+  const int64_t row0 = (slot - (first * a.group / kRows + r)) * kRows;
+  if (first < 0 || end <= first || row0 < 0 || row0 >= (end - first) * a.group) return;
+  const int64_t rows = (end - first) * a.group;
+  const int32_t held = a.prefix ? kv::clip_tokens(a.prefix[r], a.table.width, a.pool.log_block) : 0;
+  const int32_t cached = (held + kKeys - 1) / kKeys;
+  const int32_t last_row_token = (int32_t)((min(row0 + kRows, rows) - 1) / a.group);
+  const int32_t tiles = cached + last_row_token / kKeys + 1;
+
+  // this lane's row
+  const int col = lane & 31, half = lane >> 5;
+  const int64_t wave_row = row0 + wave * 32;
+  const bool active = wave_row < rows;
+  const int64_t row = min(wave_row + col, rows - 1);
+  const int32_t token = (int32_t)(row / a.group);
+  const int32_t q_head = head * a.group + (int32_t)(row - (int64_t)token * a.group);
+  // own tokens that all, and that any, of the wavefront's rows see
+  const int32_t least = (int32_t)(min(wave_row, rows - 1) / a.group) + 1;
+  const int32_t most = (int32_t)(min(wave_row + 31, rows - 1) / a.group) + 1;
+
+  T tile;
+  {
+    const uint16_t* q = (const uint16_t*)a.q.data + (first + token) * a.q.token + q_head * a.q.head + half * 8;
+#pragma unroll
+    for (int i = 0; i < T::kSteps; ++i) {
+      tile.q[i] = *(const u4*)(q + 16 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) tile.q[i][e] = (tile.q[i][e] ^ a.q_flip) & a.q_mask;
+    }
+#pragma unroll
+    for (int p = 0; p < T::kParts; ++p) tile.acc[p] = (f16){};
+    tile.top = kNone;
+    tile.sum = 0.0f;
+  }
+
+  // ---- bringing tiles in
+  const uint16_t* own_k = (const uint16_t*)a.k.data + first * a.k.token + head * a.k.head;
+  const uint16_t* own_v = (const uint16_t*)a.v.data + first * a.v.token + head * a.v.head;
+  const int32_t own = (int32_t)(end - first);
+  auto load_own = [&](int32_t t0, int buf) {
+#pragma unroll
+    for (int i = 0; i < T::kBytes / 1024 / kWaves; ++i) {
+      const uint32_t base = (i * kWaves + wave) * kWave, piece = base + lane;
+      const uint32_t t = piece / T::kPieces, at = piece % T::kPieces;
+      const int64_t key = min(t0 + (int32_t)t, own - 1);
+      const uint32_t ck = at ^ (t & (T::kPieces - 1)), cv = at ^ ((t << 1) & (T::kPieces - 1));
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(own_k + key * a.k.token + ck * 8),
+          (__attribute__((address_space(3))) void*)(s_k[buf] + base * 16), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(own_v + key * a.v.token + cv * 8),
+          (__attribute__((address_space(3))) void*)(s_v[buf] + base * 16), 16, 0, 0);
+    }
+  };
+  // a cached tile's 16-code units of this thread: unit u of K (then of V) is codes 16 (u % (D / 16)) of key u / (D / 16)
+  u4 codes[T::kUnitsEach];
+  float scale_k = 1.0f, scale_v = 1.0f;
+  uint32_t page = 0;
+  const int32_t unit_key = (tid % (kKeys * (D / 16))) / (D / 16), unit_at = tid % (D / 16);
+  const bool leads = tid < kKeys * (D / 16) && unit_at == 0 && (unit_key & 3) == 0;     // of four keys: fetches their scales
+  auto key_of = [&](int32_t j) { return min(j * kKeys + unit_key, held - 1); };
+  auto find_page = [&](int32_t j) { page = kv::page_of(a.table, a.pool, r, key_of(j) >> a.pool.log_block); };
+  auto fetch = [&](int32_t j) {
+    const int32_t in_block = key_of(j) & ((1 << a.pool.log_block) - 1);
+#pragma unroll
+    for (int i = 0; i < T::kUnitsEach; ++i) {
+      const int is_v = T::kUnitsEach == 2 ? i : tid >= kThreads / 2;
+      const int64_t at = ((int64_t)page * 2 + is_v) * a.pool.heads + head;
+      codes[i] = *(const u4*)(a.pool.pages + ((at << a.pool.log_block) + in_block) * D + unit_at * 16);
+    }
+    if (leads) {
+      const int64_t at = (int64_t)page * 2 * a.pool.heads + head;
+      scale_k = a.pool.scales[at];
+      scale_v = a.pool.scales[at + a.pool.heads];
+    }
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < T::kUnitsEach; ++i) {
+      const bool is_v = T::kUnitsEach == 2 ? i == 1 : tid >= kThreads / 2;
+      const u2 x0 = widen4<TYPE, FMT>(codes[i][0]), x1 = widen4<TYPE, FMT>(codes[i][1]);
+      const u2 x2 = widen4<TYPE, FMT>(codes[i][2]), x3 = widen4<TYPE, FMT>(codes[i][3]);
+      uint8_t* to = is_v ? s_v[buf] : s_k[buf];
+      const uint32_t c = 2 * unit_at;
+      const uint32_t p0 = is_v ? v_piece<D>(unit_key, c) : k_piece<D>(unit_key, c);
+      const uint32_t p1 = is_v ? v_piece<D>(unit_key, c + 1) : k_piece<D>(unit_key, c + 1);
+      *(u4*)(to + 16 * p0) = (u4){x0[0], x0[1], x1[0], x1[1]};
+      *(u4*)(to + 16 * p1) = (u4){x2[0], x2[1], x3[0], x3[1]};
+    }
+    if (leads) s_scale[buf][unit_key / 4] = (f4){scale_k * a.scale, log2_fast(scale_v), 1.0f / scale_v, 0.0f};
+  };
+
+  if (cached > 0) {
+    find_page(0);
+    fetch(0);
+    if (cached > 1) find_page(1);
+    store(0);
+  } else {
+    load_own(0, 0);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+
+  for (int32_t j = 0; j < tiles; ++j) {
+    const int buf = j & 1;
+    const bool more_cached = j + 1 < cached;
+    if (more_cached) {
+      fetch(j + 1);
+      if (j + 2 < cached) find_page(j + 2);
+    } else if (j + 1 < tiles) {
+      load_own((j + 1 - cached) * kKeys, buf ^ 1);
+    }
+    if (j < cached) {
+      const int32_t left = held - j * kKeys;
+      if (active) tile.template step<true>(s_k[buf], s_v[buf], s_scale[buf], lane, a.scale, left < kKeys, left);
+    } else {
+      const int32_t t0 = (j - cached) * kKeys;
+      if (active && t0 < most)
+        tile.template step<false>(s_k[buf], s_v[buf], nullptr, lane, a.scale, t0 + kKeys > least, token + 1 - t0);
+    }
+    if (more_cached) store(buf ^ 1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+
+  if (!active || wave_row + col >= rows) return;
+  const float sum = sum_halves(tile.sum);
+  const float part = 1.0f / sum;
+  uint16_t* out = a.out + (first + token) * a.out_token + q_head * a.out_head + half * 4;
+#pragma unroll
+  for (int p = 0; p < T::kParts; ++p)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f16& x = tile.acc[p];
+      *(u2*)(out + 32 * p + 8 * e) = (u2){pack2<TYPE>(x[4 * e] * part, x[4 * e + 1] * part),
+                                          pack2<TYPE>(x[4 * e + 2] * part, x[4 * e + 3] * part)};
+    }
+  if (a.lse && half == 0)
+    a.lse[(first + token) * a.kv_heads * a.group + q_head] = (tile.top + log2_fast(sum)) * 0.69314718055994531f;
+}
+
+}  // namespace
+}  // namespace peek
+
+using namespace peek;
+
+extern "C" {
+
+size_t peek_prefill_attention_workspace(int32_t n, int64_t num_tokens, int32_t q_heads, int32_t kv_heads,
+                                        int32_t head_dim, int64_t max_context) {
+  return 0;
+}
+
+peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t num_tokens, int32_t type,
+                                   int32_t q_heads, int32_t kv_heads, int32_t head_dim, const void* d_q,
+                                   int64_t q_token_stride, int64_t q_head_stride, const void* d_k,
+                                   int64_t k_token_stride, int64_t k_head_stride, const void* d_v,
+                                   int64_t v_token_stride, int64_t v_head_stride, const int64_t* d_offsets,
+                                   const int32_t* d_prefix, const int32_t* d_block_table, int32_t max_blocks,
+                                   int64_t table_stride, float scale, void* d_out, int64_t out_token_stride,
+                                   int64_t out_head_stride, float* d_lse, void* d_workspace, size_t workspace_bytes,
+                                   void* stream) {
+  return guarded([&]() -> peek_status {
+    clear_error();
+    if (n < 0 || num_tokens < 0)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "n and num_tokens must be >= 0 (got %d, %lld)", n, (long long)num_tokens);
+    if (kv_heads < 1 || kv_heads > 1024)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "kv_heads must be in [1, 1024] (got %d)", kv_heads);
+    if (head_dim != 64 && head_dim != 128)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "head_dim must be 64 or 128 (got %d)", head_dim);
+    peek_status s = check_heads(type, q_heads, kv_heads, scale);
+    if (s != PEEK_OK) return s;
+    Prefill a{};
+    if ((pool != nullptr) != (d_prefix != nullptr))
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "pool and d_prefix must be given together");
+    if (pool) {
+      s = check_pool(pool, &a.pool);
+      if (s != PEEK_OK) return s;
+      if (pool->kv_heads != kv_heads || pool->head_dim != head_dim)
+        return fail(PEEK_ERR_INVALID_ARGUMENT, "the pool has %d heads of %d, the rows %d of %d", pool->kv_heads,
+                    pool->head_dim, kv_heads, head_dim);
+      s = check_table(d_block_table, max_blocks, table_stride, pool->block_size);
+      if (s != PEEK_OK) return s;
+    }
+    if (n == 0 || num_tokens == 0) return PEEK_OK;
+    if ((s = check_rows("d_q", d_q, q_token_stride, q_head_stride)) != PEEK_OK) return s;
+    if ((s = check_rows("d_k", d_k, k_token_stride, k_head_stride)) != PEEK_OK) return s;
+    if ((s = check_rows("d_v", d_v, v_token_stride, v_head_stride)) != PEEK_OK) return s;
+    if ((s = check_rows("d_out", d_out, out_token_stride, out_head_stride)) != PEEK_OK) return s;
+    if (!d_offsets) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_offsets must not be NULL");
+    const int64_t context = pool ? (int64_t)max_blocks * pool->block_size : 0;
+    s = check_workspace(d_workspace, workspace_bytes,
+                        peek_prefill_attention_workspace(n, num_tokens, q_heads, kv_heads, head_dim, context));
+    if (s != PEEK_OK) return s;
+    const int32_t group = q_heads / kv_heads;
+    if (num_tokens >= ((int64_t)1 << 40) || (num_tokens * group / kRows + n) * kv_heads >= (1 << 22))
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "too many rows for one call (%lld)", (long long)num_tokens);
+    hipStream_t st = (hipStream_t)stream;
+    s = validate_kv(n, d_offsets, num_tokens, d_prefix, false, d_block_table, max_blocks, table_stride,
+                    pool ? pool->block_size : 4, pool ? pool->num_pages : 0, st);
+    if (s != PEEK_OK) return s;
+    a.q = Rows{d_q, q_token_stride, q_head_stride};
+    a.k = Rows{d_k, k_token_stride, k_head_stride};
+    a.v = Rows{d_v, v_token_stride, v_head_stride};
+    a.offsets = d_offsets;
+    a.prefix = d_prefix;
+    a.table = Table{d_block_table, table_stride, max_blocks};
+    a.out = (uint16_t*)d_out;
+    a.out_token = out_token_stride;
+    a.out_head = out_head_stride;
+    a.lse = d_lse;
+    a.num_tokens = num_tokens;
+    a.n = n;
+    a.group = group;
+    a.kv_heads = kv_heads;
+    set_scale(scale, &a.scale, &a.q_flip, &a.q_mask);
+    const unsigned groups = (unsigned)((num_tokens * group / kRows + n) * kv_heads);
+    with_types(type, pool ? pool->type : PEEK_TYPE_F8E4M3, head_dim, [&](auto t, auto m, auto d) {
+      hipLaunchKernelGGL((k_prefill<t(), m(), d()>), dim3(groups), dim3(kThreads), 0, st, a);
+    });
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return fail(PEEK_ERR_DEVICE, "prefill launch failed: %s", hipGetErrorString(err));
+    return PEEK_OK;
+  });
+}
+
+}  // extern "C"
