@@ -81,16 +81,21 @@ __device__ __forceinline__ float code_value(uint8_t c) {
   }
 }
 
-// Sequence that holds row `at` of packed rows: the last r with offsets[r] <= at
-// (offsets non-decreasing), in [0, n).
-__device__ __forceinline__ int32_t sequence_of(const int64_t* __restrict__ offsets, int32_t n, int64_t at) {
-  int32_t lo = 0, hi = n;   // offsets[lo] <= at < offsets[hi], as far as they are in order
+// The last r in [0, n) with at(r) <= x, for at() that does not decrease (0 if
+// there is none). A wavefront looks at 64 places at a time: one load's
+// wait up to 64 sequences, two up to 4096.
+template <typename F>
+__device__ __forceinline__ int32_t last_at_most(int32_t n, int64_t x, int lane, F&& at) {
+  int32_t lo = 0, hi = n;
   while (hi - lo > 1) {
-    const int32_t mid = lo + (hi - lo) / 2;
-    if (offsets[mid] <= at) lo = mid;
-    else hi = mid;
+    const int32_t step = (hi - lo + 63) / 64;
+    const int64_t place = lo + (int64_t)lane * step;
+    const uint64_t below = __ballot(place < hi && at((int32_t)(place < hi ? place : lo)) <= x);
+    const int32_t count = __popcll(below);      // the places are in order, so these are the first
+    lo += (count > 0 ? count - 1 : 0) * step;
+    hi = count > 0 ? min(hi, lo + step) : lo + 1;
   }
-  return lo;
+  return __builtin_amdgcn_readfirstlane(lo);
 }
 
 }  // namespace kv

@@ -21,6 +21,12 @@ constexpr int kWave = 64;
 // offsets[r] / B + 2 r, which leaves every sequence room for the blocks it
 // can touch (new tokens / B + 2 at most), so slots need no counting; a slot past its
 // sequence's last block has nothing to do.
+//
+// Bound by memory: 16-byte loads of eight elements, which stay in registers
+// from the maximum to the rounding up to kHeld of them a lane (blocks of 16
+// tokens of 128); larger blocks are read again, from L2.
+
+constexpr int kHeld = 4;
 
 __device__ __forceinline__ float wave_max(float x) {
   for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
@@ -41,78 +47,152 @@ __device__ __forceinline__ float scale_of(float most) {
   }
 }
 
+// x / scale, correctly rounded where it is below 512 (beyond, any value there
+// is as good): the product with the rounded reciprocal is at most two units off,
+// its remainder is exact, and the quotient corrected by that is the nearest.
+__device__ __forceinline__ float quotient(float x, float scale, float inv) {
+  const float y = x * inv;
+  return fabsf(y) < 512.0f ? fmaf(fmaf(-y, scale, x), inv, y) : y;
+}
+
+// Four values' codes. `plain`: none is NaN or above the largest code.
 template <int FMT>
-__device__ __forceinline__ uint8_t code_of(float x, float scale) {
-  const float y = x / scale;
+__device__ __forceinline__ uint32_t codes_of(const float* x, float scale, float inv, bool plain) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = quotient(x[i], scale, inv);
+    if (!plain) {
+      if constexpr (FMT == PEEK_TYPE_F8E4M3) y[i] = y[i] < -448.0f ? -448.0f : y[i] > 448.0f ? 448.0f : y[i];
+      else y[i] = y[i] != y[i] ? 0.0f : y[i] < -127.0f ? -127.0f : y[i] > 127.0f ? 127.0f : y[i];
+    }
+  }
   if constexpr (FMT == PEEK_TYPE_F8E4M3) {
-    const float z = y < -448.0f ? -448.0f : y > 448.0f ? 448.0f : y;   // NaN stays
-    return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(z, z, 0, false);
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
   } else {
-    const float z = y != y ? 0.0f : y < -127.0f ? -127.0f : y > 127.0f ? 127.0f : y;
-    return (uint8_t)(int8_t)(int32_t)rintf(z);
+    // 1.5 * 2^23 + y has y, rounded to nearest even, in its low byte
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = __builtin_bit_cast(uint32_t, y[i] + 12582912.0f);
+    const uint32_t ab = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400), cd = __builtin_amdgcn_perm(u[3], u[2], 0x04000c0c);
+    return ab | cd;
   }
 }
 
-template <int TYPE, int FMT>
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+
+template <int TYPE>
+__device__ __forceinline__ void spread8(const u4 w, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u = w[i];
+    x[2 * i] = kv::to_float<TYPE>((uint16_t)u);
+    x[2 * i + 1] = kv::to_float<TYPE>((uint16_t)(u >> 16));
+  }
+}
+
+template <int TYPE, int FMT, int D>
 __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, int32_t n, int64_t num_tokens,
-                                                   int32_t dim, const int64_t* __restrict__ offsets,
+                                                   const int64_t* __restrict__ offsets,
                                                    const int32_t* __restrict__ context, Table table, int64_t slots) {
+  constexpr int kPieces = D / 8;       // of a token
   const int lane = threadIdx.x & (kWave - 1);
-  const int64_t unit = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int32_t parts = 2 * pool.heads;
   const int64_t slot = unit / parts;
   if (slot >= slots) return;
   const int32_t part = (int32_t)(unit % parts), is_v = part / pool.heads, head = part % pool.heads;
   const int32_t lb = pool.log_block;
-  // the last r with offsets[r] / B + 2 r <= slot
-  int32_t lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int32_t mid = lo + (hi - lo) / 2;
-    if ((offsets[mid] >> lb) + 2 * (int64_t)mid <= slot) lo = mid;
-    else hi = mid;
-  }
-  const int32_t r = lo;
-  const int64_t first = max((int64_t)0, offsets[r]), end = min(num_tokens, offsets[r + 1]);
+  const int32_t r =
+      kv::last_at_most(n, slot, lane, [&](int32_t i) { return (offsets[i] >> lb) + 2 * (int64_t)i; });
+  const int64_t start = offsets[r], first = max((int64_t)0, start), end = min(num_tokens, offsets[r + 1]);
   const int64_t ctx = max(0, context[r]);
-  const int64_t b = (ctx >> lb) + slot - ((offsets[r] >> lb) + 2 * (int64_t)r);
+  const int64_t b = (ctx >> lb) + slot - ((start >> lb) + 2 * (int64_t)r);
   // positions of the block's new tokens
   const int64_t from = max(ctx, b << lb), to = min(ctx + (end - first), (b + 1) << lb);
   if (b < 0 || b >= table.width || from >= to) return;
   const uint32_t page = (uint32_t)table.ids[(int64_t)r * table.stride + b];
   if (page >= pool.num_pages) return;
-  const int32_t old = (int32_t)(from - (b << lb)), count = (int32_t)(to - from);
+  const int32_t old = (int32_t)(from - (b << lb)), pieces = (int32_t)(to - from) * kPieces;
 
-  const Rows& src = is_v ? v : k;
+  const Rows src = is_v ? v : k;
   const uint16_t* x = (const uint16_t*)src.data + (first + from - ctx) * src.token + head * src.head;
   const int64_t at = ((int64_t)page * 2 + is_v) * pool.heads + head;
-  uint8_t* codes = pool.pages + ((at << lb) * dim);
+  uint8_t* codes = pool.pages + (at << lb) * D;
+  const float held = old > 0 ? pool.scales[at] : 0.0f;
+
+  u4 w[kHeld];
+  auto load = [&](int32_t p0) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int32_t p = p0 + i * kWave + lane;
+      w[i] = p < pieces ? *(const u4*)(x + (int64_t)(p / kPieces) * src.token + p % kPieces * 8) : (u4){};
+    }
+  };
   float most = 0.0f;
-  for (int32_t i = lane; i < count * dim; i += kWave) {
-    const float a = fabsf(kv::to_float<TYPE>(x[(int64_t)(i / dim) * src.token + i % dim]));
-    if (a < __builtin_inff()) most = fmaxf(most, a);
-  }
-  float scale = scale_of<FMT>(wave_max(most));
-  if (old > 0) {
-    const float held = pool.scales[at];
-    if (scale > held) {
-      for (int32_t i = lane; i < old * dim; i += kWave) codes[i] = code_of<FMT>(kv::code_value<FMT>(codes[i]) * held, scale);
-    } else {
-      scale = held;
+  bool plain = true;
+  for (int32_t p0 = 0; p0 < pieces; p0 += kHeld * kWave) {
+    load(p0);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      float y[8];
+      spread8<TYPE>(w[i], y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float m = fabsf(y[e]);
+        plain = plain && m < __builtin_inff();
+        most = fmaxf(most, m < __builtin_inff() ? m : 0.0f);
+      }
     }
   }
-  for (int32_t i = lane; i < count * dim; i += kWave)
-    codes[old * dim + i] = code_of<FMT>(kv::to_float<TYPE>(x[(int64_t)(i / dim) * src.token + i % dim]), scale);
+  float scale = scale_of<FMT>(wave_max(most));
+  plain = __all(plain) && scale < kv::kScaleMax;
+  if (old > 0 && !(scale > held)) scale = held;
+  const float inv = 1.0f / scale;
+  if (old > 0 && scale > held) {
+    // older values are at most the largest code times a smaller scale; NaN codes stay NaN
+    for (int32_t p = lane; p < old * kPieces; p += kWave) {
+      u2 c = *(const u2*)(codes + p * 8);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float y[4];
+        const uint32_t word = c[h];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = kv::code_value<FMT>((uint8_t)(word >> (8 * e))) * held;
+        c[h] = codes_of<FMT>(y, scale, inv, false);
+      }
+      *(u2*)(codes + p * 8) = c;
+    }
+  }
+  for (int32_t p0 = 0; p0 < pieces; p0 += kHeld * kWave) {
+    if (pieces > kHeld * kWave) load(p0);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int32_t p = p0 + i * kWave + lane;
+      if (p < pieces) {
+        float y[8];
+        spread8<TYPE>(w[i], y);
+        *(u2*)(codes + old * D + p * 8) = (u2){codes_of<FMT>(y, scale, inv, plain), codes_of<FMT>(y + 4, scale, inv, plain)};
+      }
+    }
+  }
   if (lane == 0) pool.scales[at] = scale;
 }
 
 // ---------------------------------------------------------------- eviction
 //
 // One workgroup per sequence. Scores become keys whose unsigned order is
-// theirs; four counting passes of eight bits find the key of the last block to go,
-// and a pass over the blocks in order drops those below it and the first of those
-// equal to it.
+// theirs, kept in LDS (in the workspace, where a table is too wide for that);
+// three counting passes of 11, 11 and 10 bits find the key of the last block to
+// go. The blocks below it go, and the first `equal` of those that equal
+// it, so the number gone before a block is (lower keys before it) +
+// min(equal keys before it, equal): one sum over 64-block segments places
+// every block.
 
-constexpr int kEvictThreads = 256;
+constexpr int kEvictBins = 2048;
+constexpr int kEvictLdsKeys = 32768;      // 128 KB
 
 __device__ __forceinline__ uint32_t score_key(float x) {
   if (x != x) return 0xffffffffu;
@@ -120,39 +200,47 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// Exclusive sum over the workgroup; *total gets the whole.
-__device__ __forceinline__ int32_t group_sum(int32_t x, int32_t* s_part, int32_t* total) {
+// Exclusive sum over the workgroup of two counts at once; *total gets the wholes.
+template <int THREADS>
+__device__ __forceinline__ int2 group_sum(int2 x, int2* s_part, int2* total) {
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  int32_t inc = x;
+  int2 inc = x;
   for (int d = 1; d < kWave; d <<= 1) {
-    const int32_t y = __shfl_up(inc, d);
-    if (lane >= d) inc += y;
+    const int a = __shfl_up(inc.x, d), b = __shfl_up(inc.y, d);
+    if (lane >= d) { inc.x += a; inc.y += b; }
   }
   if (lane == kWave - 1) s_part[wave] = inc;
   __syncthreads();
-  int32_t before = 0, all = 0;
-  for (int w = 0; w < kEvictThreads / kWave; ++w) {
-    if (w < wave) before += s_part[w];
-    all += s_part[w];
+  int2 before{0, 0}, all{0, 0};
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave; ++w) {
+    const int2 p = s_part[w];
+    if (w < wave) { before.x += p.x; before.y += p.y; }
+    all.x += p.x;
+    all.y += p.y;
   }
   __syncthreads();
   *total = all;
-  return before + inc - x;
+  return int2{before.x + inc.x - x.x, before.y + inc.y - x.y};
 }
 
-__global__ __launch_bounds__(kEvictThreads) void k_kv_evict(
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_kv_evict(
     int32_t heads, int32_t log_block, const int32_t* context, Table table, const float* __restrict__ mass,
     const int32_t* __restrict__ keep, int32_t sink, int32_t recent, int32_t* context_out,
     int32_t* __restrict__ table_out, float* __restrict__ mass_out, int32_t* __restrict__ freed,
-    int32_t* __restrict__ num_freed, uint32_t* __restrict__ keys) {
-  __shared__ int32_t s_part[kEvictThreads / kWave];
-  __shared__ int32_t s_count[256];
+    int32_t* __restrict__ num_freed, uint32_t* __restrict__ workspace, int32_t keys_in_lds) {
+  extern __shared__ uint32_t s_keys[];
+  __shared__ int32_t s_count[kEvictBins];
+  __shared__ int2 s_part[THREADS / kWave];
+  __shared__ int2 s_wave[THREADS / kWave];
   __shared__ uint32_t s_prefix;
   __shared__ int32_t s_left;
   const int32_t r = blockIdx.x, t = threadIdx.x, width = table.width;
+  const int lane = t & (kWave - 1), wave = t / kWave;
   const int32_t* ids = table.ids + (int64_t)r * table.stride;
   const float* m = mass + (int64_t)r * heads * width;
-  uint32_t* key = keys + (int64_t)r * width;
+  uint32_t* key = keys_in_lds ? s_keys : workspace + (int64_t)r * width;
   const int32_t ctx = context[r];
   const int32_t nb = (int32_t)(((int64_t)kv::clip_tokens(ctx, width, log_block) + (1 << log_block) - 1) >> log_block);
   const int32_t lo = min(sink, nb), hi = (int32_t)max((int64_t)lo, (int64_t)nb - recent);
@@ -161,27 +249,38 @@ __global__ __launch_bounds__(kEvictThreads) void k_kv_evict(
   uint32_t last = 0;       // key of the last block to go
   int32_t equal = 0;       // how many of that key go
   if (drop > 0) {
-    for (int32_t b = lo + t; b < hi; b += kEvictThreads) {
+    for (int32_t b = lo + t; b < hi; b += THREADS) {
       float s = m[b];
+#pragma unroll 8
       for (int32_t h = 1; h < heads; ++h) s += m[(int64_t)h * width + b];
       key[b] = score_key(s);
     }
     if (t == 0) { s_prefix = 0; s_left = drop; }
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      s_count[t] = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+      for (int32_t i = t; i < kEvictBins; i += THREADS) s_count[i] = 0;
       __syncthreads();
-      const uint32_t prefix = s_prefix;
+      const uint32_t prefix = s_prefix, above = pass == 0 ? 0u : 0xffffffffu << (shift + bits);
       const int32_t left = s_left;
-      const uint32_t above = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-      for (int32_t b = lo + t; b < hi; b += kEvictThreads)
-        if ((key[b] & above) == prefix) atomicAdd(&s_count[(key[b] >> shift) & 255], 1);
+      for (int32_t b = lo + t; b < hi; b += THREADS) {
+        const uint32_t k = key[b];
+        if ((k & above) == prefix) atomicAdd(&s_count[(k >> shift) & ((1 << bits) - 1)], 1);
+      }
       __syncthreads();
-      const int32_t c = s_count[t];
-      int32_t all;
-      const int32_t before = group_sum(c, s_part, &all);
-      if (before < left && left <= before + c) {
-        s_prefix = prefix | ((uint32_t)t << shift);
-        s_left = left - before;
+      constexpr int kEach = kEvictBins / THREADS;
+      int32_t c[kEach], sum = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) sum += c[i] = s_count[t * kEach + i];
+      int2 all;
+      int32_t before = group_sum<THREADS>(int2{sum, 0}, s_part, &all).x;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        if (before < left && left <= before + c[i]) {
+          s_prefix = prefix | ((uint32_t)(t * kEach + i) << shift);
+          s_left = left - before;
+        }
+        before += c[i];
       }
       __syncthreads();
     }
@@ -189,34 +288,58 @@ __global__ __launch_bounds__(kEvictThreads) void k_kv_evict(
     equal = s_left;
   }
 
-  int32_t gone = 0, ties = 0;
-  for (int32_t base = 0; base < width; base += kEvictThreads) {
-    const int32_t b = base + t;
+  // A wavefront places a run of 64-block segments; what lies before the run first
+  const int32_t segments = (width + kWave - 1) / kWave, each = (segments + THREADS / kWave - 1) / (THREADS / kWave);
+  const int32_t seg0 = min(segments, wave * each), seg1 = min(segments, seg0 + each);
+  auto votes = [&](int32_t seg, uint64_t* lower, uint64_t* same) {
+    const int32_t b = seg * kWave + lane;
     const bool able = drop > 0 && b >= lo && b < hi;
-    const uint32_t k = able ? key[b] : 0;
-    int32_t all_ties, all_gone;
-    const int32_t tie = ties + group_sum(able && k == last, s_part, &all_ties);
-    const bool goes = able && (k < last || (k == last && tie < equal));
-    const int32_t before = gone + group_sum(goes, s_part, &all_gone);
+    const uint32_t k = able ? key[b] : 0xffffffffu;
+    *lower = __ballot(able && k < last);
+    *same = __ballot(able && k == last);
+  };
+  int2 mine{0, 0};
+  if (drop > 0) {
+    for (int32_t seg = seg0; seg < seg1; ++seg) {
+      uint64_t lower, same;
+      votes(seg, &lower, &same);
+      mine.x += __popcll(lower);
+      mine.y += __popcll(same);
+    }
+    if (lane == 0) s_wave[wave] = mine;
+    __syncthreads();
+    mine = int2{0, 0};
+    for (int w = 0; w < wave; ++w) {
+      mine.x += s_wave[w].x;
+      mine.y += s_wave[w].y;
+    }
+  }
+  int32_t* out_ids = table_out + (int64_t)r * width;
+  float* out_mass = mass_out + (int64_t)r * heads * width;
+  for (int32_t seg = seg0; seg < seg1; ++seg) {
+    uint64_t lower = 0, same = 0;
+    if (drop > 0) votes(seg, &lower, &same);
+    const uint64_t under = ((uint64_t)1 << lane) - 1;
+    const int32_t b = seg * kWave + lane, ties = mine.y + __popcll(same & under);
+    const int32_t gone = mine.x + __popcll(lower & under) + min(ties, equal);
+    const bool goes = ((lower >> lane) & 1) || (((same >> lane) & 1) && ties < equal);
     if (b < width) {
       const int32_t id = ids[b];
       if (goes) {
-        freed[(int64_t)r * width + before] = id;
+        freed[(int64_t)r * width + gone] = id;
       } else {
-        table_out[(int64_t)r * width + b - before] = id;
-        for (int32_t h = 0; h < heads; ++h)
-          mass_out[((int64_t)r * heads + h) * width + b - before] = m[(int64_t)h * width + b];
+        out_ids[b - gone] = id;
+#pragma unroll 8
+        for (int32_t h = 0; h < heads; ++h) out_mass[(int64_t)h * width + b - gone] = m[(int64_t)h * width + b];
       }
     }
-    ties += all_ties;
-    gone += all_gone;
+    mine.x += __popcll(lower);
+    mine.y += __popcll(same);
   }
-  for (int32_t b = t; b < width; b += kEvictThreads) {
-    if (b >= drop) freed[(int64_t)r * width + b] = -1;
-    if (b >= width - drop) {
-      table_out[(int64_t)r * width + b] = -1;
-      for (int32_t h = 0; h < heads; ++h) mass_out[((int64_t)r * heads + h) * width + b] = 0.0f;
-    }
+  for (int32_t b = drop + t; b < width; b += THREADS) freed[(int64_t)r * width + b] = -1;
+  for (int32_t b = width - drop + t; b < width; b += THREADS) {
+    out_ids[b] = -1;
+    for (int32_t h = 0; h < heads; ++h) out_mass[(int64_t)h * width + b] = 0.0f;
   }
   if (t == 0) {
     num_freed[r] = drop;
@@ -384,14 +507,10 @@ peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_toke
     const Rows k{d_k, k_token_stride, k_head_stride}, v{d_v, v_token_stride, v_head_stride};
     const Table t{d_block_table, table_stride, max_blocks};
     auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, st, p, k, v, n, num_tokens, pool->head_dim,
-                         d_offsets, d_context, t, slots);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, st, p, k, v, n, num_tokens, d_offsets, d_context,
+                         t, slots);
     };
-    const bool bf = type == PEEK_TYPE_BF16, f8 = pool->type == PEEK_TYPE_F8E4M3;
-    if (bf && f8) go(k_kv_append<PEEK_TYPE_BF16, PEEK_TYPE_F8E4M3>);
-    else if (bf) go(k_kv_append<PEEK_TYPE_BF16, PEEK_TYPE_I8>);
-    else if (f8) go(k_kv_append<PEEK_TYPE_F16, PEEK_TYPE_F8E4M3>);
-    else go(k_kv_append<PEEK_TYPE_F16, PEEK_TYPE_I8>);
+    with_types(type, pool->type, pool->head_dim, [&](auto e, auto f, auto d) { go(k_kv_append<e(), f(), d()>); });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "append launch failed: %s", hipGetErrorString(e));
     return PEEK_OK;
@@ -399,7 +518,7 @@ peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_toke
 }
 
 size_t peek_kv_evict_workspace(int32_t n, int32_t kv_heads, int32_t max_blocks) {
-  if (n < 0 || kv_heads < 1 || max_blocks < 0) return 0;
+  if (n < 0 || kv_heads < 1 || max_blocks <= kEvictLdsKeys) return 0;
   return ((size_t)n * max_blocks * sizeof(uint32_t) + 255) & ~(size_t)255;
 }
 
@@ -439,10 +558,15 @@ peek_status peek_kv_evict(int32_t n, int32_t kv_heads, int32_t block_size, const
     hipStream_t st = (hipStream_t)stream;
     s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, block_size, INT32_MAX, st);
     if (s != PEEK_OK) return s;
-    hipLaunchKernelGGL(k_kv_evict, dim3((unsigned)n), dim3(kEvictThreads), 0, st, kv_heads,
-                       __builtin_ctz((unsigned)block_size), d_context, Table{d_block_table, table_stride, max_blocks},
-                       d_mass, d_keep, sink, recent, d_context_out, d_table_out, d_mass_out, d_freed, d_num_freed,
-                       (uint32_t*)d_workspace);
+    const bool in_lds = max_blocks <= kEvictLdsKeys;
+    auto go = [&](auto kernel, int threads) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(threads), in_lds ? max_blocks * sizeof(uint32_t) : 0, st, kv_heads,
+                         __builtin_ctz((unsigned)block_size), d_context, Table{d_block_table, table_stride, max_blocks},
+                         d_mass, d_keep, sink, recent, d_context_out, d_table_out, d_mass_out, d_freed, d_num_freed,
+                         (uint32_t*)d_workspace, in_lds ? 1 : 0);
+    };
+    if (max_blocks > 1024) go(k_kv_evict<1024>, 1024);
+    else go(k_kv_evict<256>, 256);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "eviction launch failed: %s", hipGetErrorString(e));
     return PEEK_OK;

@@ -195,13 +195,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int64_t slot = (gridDim.x - 1 - blockIdx.x) / a.kv_heads;
   // the last sequence r with offsets[r] * group / kRows + r <= slot: every
   // sequence has a slot for each of its tiles, some one more
-  int32_t lo = 0, hi = a.n;
-  while (hi - lo > 1) {
-    const int32_t mid = lo + (hi - lo) / 2;
-    if (a.offsets[mid] * a.group / kRows + mid <= slot) lo = mid;
-    else hi = mid;
-  }
-  const int32_t r = lo;
+  const int32_t r = kv::last_at_most(a.n, slot, lane, [&](int32_t i) { return a.offsets[i] * a.group / kRows + i; });
   const int64_t first = a.offsets[r], end = min(a.num_tokens, a.offsets[r + 1]);
   const int64_t row0 = (slot - (first * a.group / kRows + r)) * kRows;
   if (first < 0 || end <= first || row0 < 0 || row0 >= (end - first) * a.group) return;
