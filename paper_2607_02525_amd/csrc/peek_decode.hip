@@ -23,6 +23,7 @@
 // With weights wanted, every row's weight of every 16 tokens (of a block, where
 // that is smaller) is kept as a logarithm, which needs no maximum to go with
 // it; the second kernel sums them over the rows once the rows' sums are known.
+// They take 4 bytes a row and 16 tokens, of the 4 KB that the tokens take.
 #include <algorithm>
 
 #include "peek_internal.h"
@@ -58,9 +59,9 @@ struct Decode {
   float* lse;
   const float* mass_in;
   float* mass;
-  float* part_out;       // [n][splits][q_heads][D]: a chunk's sum of weight * value / its sum of weights
-  float* part_lse;       // [n][splits][q_heads]: base-2 logarithm of its sum of weights
-  float* weights;        // [n][q_heads][grains]: base-2 logarithm of the weight on every grain of tokens
+  float* part_out;       // [n][q_heads][splits][D]: a chunk's sum of weight * value / its sum of weights
+  float* part_lse;       // [n][q_heads][splits]: base-2 logarithm of its sum of weights
+  float* weights;        // [n][kv_heads][row_tiles][grains][16]: base-2 logarithm of the weight on every grain of tokens
   int64_t grains;
   int32_t log_grain;
   int32_t n, group, row_tiles, chunk, splits;
@@ -101,12 +102,16 @@ __device__ __forceinline__ void turn4(const uint32_t a, const uint32_t b, const 
   r[3] = __builtin_amdgcn_perm(cd1, ab1, 0x07060302);
 }
 
-template <int TYPE, int FMT, int D, bool MASS>
-__global__ __launch_bounds__(kThreads) void k_decode(Decode a) {
+// WIDE: blocks of 16 tokens or more. Sixteen tokens that start at a multiple
+// of 16 then lie in one block, whose page and scales are the same for the whole
+// wavefront and come by scalar loads; smaller blocks are looked up by every
+// lane in LDS.
+template <int TYPE, int FMT, int D, bool MASS, bool WIDE>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ? 4 : 3))) void k_decode(Decode a) {
   constexpr int kSteps = D / 32;        // products of keys and queries a 16-token half
   constexpr int kParts = D / 16;        // 16-wide parts of the output; also bytes of a token's values in a lane
   constexpr int kKeyWords = D / 16;     // words of a token's key in a lane
-  __shared__ Block s_block[kMaxChunk / 4 + 1];           // of the chunk's blocks
+  __shared__ Block s_block[WIDE ? 1 : kMaxChunk / 4 + 1];           // of the chunk's blocks
   __shared__ float s_out[kWaves][kRows][D + 4];
   __shared__ float s_top[kWaves][kRows], s_sum[kWaves][kRows];
 
@@ -131,12 +136,15 @@ __global__ __launch_bounds__(kThreads) void k_decode(Decode a) {
     return;
   }
 
-  const int32_t block0 = from >> lb, blocks = ((to - 1) >> lb) - block0 + 1;
-  for (int32_t i = tid; i < blocks; i += kThreads) {
-    const uint32_t page = kv::page_of(a.table, a.pool, r, block0 + i);
-    const int64_t at = (int64_t)page * 2 * a.pool.heads + head;
-    const float k = a.pool.scales[at], v = a.pool.scales[at + a.pool.heads];
-    s_block[i] = Block{k * a.scale, log2_fast(v), 1.0f / v, page};
+  const int32_t block0 = from >> lb;
+  if constexpr (!WIDE) {
+    const int32_t blocks = ((to - 1) >> lb) - block0 + 1;
+    for (int32_t i = tid; i < blocks; i += kThreads) {
+      const uint32_t page = kv::page_of(a.table, a.pool, r, block0 + i);
+      const int64_t at = (int64_t)page * 2 * a.pool.heads + head;
+      const float k = a.pool.scales[at], v = a.pool.scales[at + a.pool.heads];
+      s_block[i] = Block{k * a.scale, log2_fast(v), __builtin_amdgcn_rcpf(v), page};
+    }
   }
 
   const int32_t grp = lane >> 4, col = lane & 15;
@@ -151,70 +159,115 @@ __global__ __launch_bounds__(kThreads) void k_decode(Decode a) {
       for (int e = 0; e < 4; ++e) q[i][e] = (q[i][e] ^ a.q_flip) & a.q_mask;
     }
   }
-  __syncthreads();
+  if constexpr (!WIDE) __syncthreads();
 
   f4 acc[kParts] = {};
   float top = kNone, sum = 0.0f;
+  uint32_t kw[2][kKeyWords];        // keys, and values, of the tile at hand, then of the next
+  uint32_t vw[8][kParts / 4];
+  float scale[2], log_v[2], inv_v[2];
+  const int64_t half_page = ((int64_t)a.pool.heads << lb) * D;      // bytes from a page's keys to its values
 
-  struct Raw {
-    uint32_t k[2][kKeyWords];
-    uint32_t v[8][kParts / 4];
+  // Where the 16 tokens from t on (WIDE), or this lane's token t, begin.
+  typedef const __attribute__((address_space(4))) int32_t* const_ints;
+  typedef const __attribute__((address_space(4))) float* const_floats;
+  const const_ints ids = (const_ints)(a.table.ids + (int64_t)r * a.table.stride);
+  const const_floats scales = (const_floats)a.pool.scales;
+  const uint8_t* base[2];           // WIDE: of the next tile's halves
+  int32_t limit[2];                 // and the last of their 16 tokens that there is
+  auto place = [&](int32_t t0) {    // pages and scales of the tile at t0 (its halves past the end: of the last tokens)
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int32_t t = min(t0 + 16 * h, (to - 1) & ~15);
+        const uint32_t id = (uint32_t)ids[t >> lb], page = id < a.pool.num_pages ? id : 0u;
+        const int64_t at = (int64_t)page * 2 * a.pool.heads + head;
+        base[h] = a.pool.pages + ((at << lb) + (t & ((1 << lb) - 1))) * D;
+        limit[h] = to - 1 - t;
+        const float v = scales[at + a.pool.heads];
+        scale[h] = scales[at] * a.scale;
+        log_v[h] = log2_fast(v);
+        inv_v[h] = __builtin_amdgcn_rcpf(v);
+      }
+    }
   };
-  const int64_t half_page = (int64_t)a.pool.heads << lb;      // tokens from a page's keys to its values
-  auto token_at = [&](int32_t t) {                            // of the pool's rows of D bytes
+  auto row_at = [&](int32_t t) {    // !WIDE: this lane's token
     const uint32_t page = s_block[(t >> lb) - block0].page;
-    return (((int64_t)page * 2 * a.pool.heads + head) << lb) + (t & ((1 << lb) - 1));
+    return a.pool.pages + ((((int64_t)page * 2 * a.pool.heads + head) << lb) + (t & ((1 << lb) - 1))) * D;
   };
-  auto load = [&](int32_t t0, Raw& x) {
+  auto load_keys = [&](int32_t t0) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint8_t* p = a.pool.pages + token_at(min(t0 + 16 * h + col, to - 1)) * D + grp * (D / 4);
+      const uint8_t* p;
+      if constexpr (WIDE) p = base[h] + (uint32_t)(min(col, limit[h]) * D + grp * (D / 4));
+      else p = row_at(min(t0 + 16 * h + col, to - 1)) + grp * (D / 4);
 #pragma unroll
       for (int i = 0; i < kKeyWords / 4; ++i) {
         const u4 w = *(const u4*)(p + 16 * i);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x.k[h][4 * i + e] = w[e];
+        for (int e = 0; e < 4; ++e) kw[h][4 * i + e] = w[e];
       }
+    }
+  };
+  auto load_values = [&](int32_t t0) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t t = min(t0 + 16 * h + 4 * grp, (to - 1) & ~3);      // !WIDE: four tokens of one block
+      const uint8_t* p = WIDE ? base[h] : row_at(t);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint8_t* pv = a.pool.pages + (token_at(min(t0 + 16 * h + 4 * grp + e, to - 1)) + half_page) * D + col * kParts;
+        const int32_t at = WIDE ? min(4 * grp + e, limit[h]) : min(e, to - 1 - t);
+        const uint8_t* pv = p + half_page + (uint32_t)(at * D + col * kParts);
         if constexpr (kParts == 8) {
           const u2 w = *(const u2*)pv;
-          x.v[4 * h + e][0] = w[0];
-          x.v[4 * h + e][1] = w[1];
+          vw[4 * h + e][0] = w[0];
+          vw[4 * h + e][1] = w[1];
         } else {
-          x.v[4 * h + e][0] = *(const uint32_t*)pv;
+          vw[4 * h + e][0] = *(const uint32_t*)pv;
         }
       }
     }
   };
-  auto step = [&](int32_t t0, const Raw& x) {
+  // One tile; the next one's keys are fetched as soon as this one's are used, then its values.
+  auto step = [&](int32_t t0, int32_t next) {
     f4 s[2];
-    float inv[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       s[h] = (f4){};
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
-        const u2 lo = widen4<TYPE, FMT>(x.k[h][2 * i]), hi = widen4<TYPE, FMT>(x.k[h][2 * i + 1]);
+        const u2 lo = widen4<TYPE, FMT>(kw[h][2 * i]), hi = widen4<TYPE, FMT>(kw[h][2 * i + 1]);
         s[h] = mul16<TYPE>((u4){lo[0], lo[1], hi[0], hi[1]}, q[i], s[h]);
       }
-      const int32_t t = t0 + 16 * h + 4 * grp;
-      const Block c = s_block[(min(t, to - 1) >> lb) - block0];
-      inv[h] = c.inv_v;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float y = fmaf(s[h][e], c.scale, c.log_v);
-        s[h][e] = t + e < to ? y : -__builtin_inff();
+      if constexpr (!WIDE) {
+        const Block c = s_block[(min(t0 + 16 * h + 4 * grp, to - 1) >> lb) - block0];
+        scale[h] = c.scale;
+        log_v[h] = c.log_v;
+        inv_v[h] = c.inv_v;
       }
+    }
+    const float inv[2] = {inv_v[0], inv_v[1]};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[h][e] = fmaf(s[h][e], scale[h], log_v[h]);
+    if (next < to) {
+      place(next);
+      load_keys(next);
+    }
+    if (t0 + kTile > to) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[h][e] = t0 + 16 * h + 4 * grp + e < to ? s[h][e] : -__builtin_inff();
     }
     float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                        fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     most = max_halves(swap16_max(most));
     if (__any(most > top + kSlack)) {
-      const float next = most > top + kSlack ? most : top;
-      const float fall = exp2_fast(top - next);
-      top = next;
+      const float higher = most > top + kSlack ? most : top;
+      const float fall = exp2_fast(top - higher);
+      top = higher;
       sum *= fall;
 #pragma unroll
       for (int p = 0; p < kParts; ++p) acc[p] *= fall;
@@ -229,36 +282,38 @@ __global__ __launch_bounds__(kThreads) void k_decode(Decode a) {
       w[2 * h] = pack2<TYPE>(s[h][0], s[h][1]);
       w[2 * h + 1] = pack2<TYPE>(s[h][2], s[h][3]);
       if constexpr (MASS) {
-        if (a.log_grain >= 3) add = swap16_sum(add);
-        if (a.log_grain >= 4) add = sum_halves(add);
+        if (WIDE || a.log_grain >= 3) add = swap16_sum(add);
+        if (WIDE || a.log_grain >= 4) add = sum_halves(add);
         const int32_t t = t0 + 16 * h + 4 * grp;
-        if (t < to && (t & ((1 << a.log_grain) - 1)) == 0 && row < a.group)
-          a.weights[((int64_t)r * q_heads + head * a.group + row) * a.grains + (t >> a.log_grain)] = log2_fast(add) + top;
+        if (t < to && (t & ((1 << a.log_grain) - 1)) == 0)
+          a.weights[((((int64_t)r * a.pool.heads + head) * a.row_tiles + row_tile) * a.grains + (t >> a.log_grain)) * kRows +
+                    col] = log2_fast(add) + top;
       }
     }
 #pragma unroll
     for (int p = 0; p < kParts / 4; ++p) {
       uint32_t lo[4], hi[4];
-      turn4(x.v[0][p], x.v[1][p], x.v[2][p], x.v[3][p], lo);
-      turn4(x.v[4][p], x.v[5][p], x.v[6][p], x.v[7][p], hi);
+      turn4(vw[0][p], vw[1][p], vw[2][p], vw[3][p], lo);
+      turn4(vw[4][p], vw[5][p], vw[6][p], vw[7][p], hi);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const u2 y = widen4<TYPE, FMT>(lo[e]), z = widen4<TYPE, FMT>(hi[e]);
         acc[4 * p + e] = mul16<TYPE>((u4){y[0], y[1], z[0], z[1]}, w, acc[4 * p + e]);
       }
     }
+    if (next < to) load_values(next);
   };
 
   {
-    Raw x, y;
     int32_t t = from + wave * kTile;
-    if (t < to) load(t, x);
+    if (t < to) {
+      place(t);
+      load_keys(t);
+      load_values(t);
+    }
     while (t < to) {
-      const int32_t next = t + kWaves * kTile;
-      if (next < to) load(next, y);
-      step(t, x);
-      x = y;
-      t = next;
+      step(t, t + kWaves * kTile);
+      t += kWaves * kTile;
     }
   }
 
@@ -295,83 +350,96 @@ __global__ __launch_bounds__(kThreads) void k_decode(Decode a) {
           (u4){pack2<TYPE>(o[0], o[1]), pack2<TYPE>(o[2], o[3]), pack2<TYPE>(o[4], o[5]), pack2<TYPE>(o[6], o[7])};
       if (a.lse && d == 0) a.lse[(int64_t)r * q_heads + q_head] = l2 * 0.69314718055994531f;
     } else {
-      f4* p = (f4*)(a.part_out + (((int64_t)r * a.splits + split) * q_heads + q_head) * D + d);
+      f4* p = (f4*)(a.part_out + (((int64_t)r * q_heads + q_head) * a.splits + split) * D + d);
       p[0] = (f4){o[0], o[1], o[2], o[3]};
       p[1] = (f4){o[4], o[5], o[6], o[7]};
     }
-    if (d == 0 && (MASS || !whole)) a.part_lse[((int64_t)r * a.splits + split) * q_heads + q_head] = l2;
+    if (d == 0 && (MASS || !whole)) a.part_lse[((int64_t)r * q_heads + q_head) * a.splits + split] = l2;
   }
 }
 
 // ------------------------------------------------------------------- join
-// Workgroups below `outs` join the chunks of 256 / (D / 8) rows each; the
-// others turn kept logarithms into the weights of 1024 blocks of a (sequence, kv head).
-constexpr int kMassBlocks = 1024;
+// Workgroups below `outs` join the chunks of four rows, a wavefront to a row
+// and a lane to a chunk for its weight; the others turn kept logarithms into
+// the weights of kThreads blocks of a (sequence, kv head).
 
-__device__ __forceinline__ float row_log_sum(const Decode& a, int32_t r, int32_t q_head, int32_t parts, int32_t q_heads) {
-  const float* p = a.part_lse + (int64_t)r * a.splits * q_heads + q_head;
-  float highest = p[0];
-  for (int32_t s = 1; s < parts; ++s) highest = fmaxf(highest, p[(int64_t)s * q_heads]);
-  float total = 0.0f;
-  for (int32_t s = 0; s < parts; ++s) total += exp2_fast(p[(int64_t)s * q_heads] - highest);
-  return highest + log2_fast(total);
+// Base-2 logarithm of a row's sum of weights over `parts` chunks, by a whole wavefront.
+__device__ __forceinline__ float row_log_sum(const float* __restrict__ p, int32_t parts, int lane) {
+  float top = kNone, sum = 0.0f;
+  for (int32_t s = lane; s < parts; s += kWave) {
+    const float x = p[s], next = fmaxf(top, x);
+    sum = sum * exp2_fast(top - next) + exp2_fast(x - next);
+    top = next;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const float x = __shfl_xor(top, d), y = __shfl_xor(sum, d), next = fmaxf(top, x);
+    sum = sum * exp2_fast(top - next) + y * exp2_fast(x - next);
+    top = next;
+  }
+  return top + log2_fast(sum);
 }
 
 template <int TYPE, int D>
 __global__ __launch_bounds__(kThreads) void k_decode_join(Decode a, uint32_t outs) {
   const int32_t tid = threadIdx.x, q_heads = a.group * a.pool.heads, lb = a.pool.log_block;
+  const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   if (blockIdx.x < outs) {
-    constexpr int kPerGroup = kThreads / (D / 8);
-    const int64_t at = (int64_t)blockIdx.x * kPerGroup + tid / (D / 8);
-    const int32_t d = tid % (D / 8) * 8;
+    const int64_t at = (int64_t)blockIdx.x * kWaves + wave;
     if (at >= (int64_t)a.n * q_heads) return;
     const int32_t r = (int32_t)(at / q_heads), q_head = (int32_t)(at % q_heads);
     const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb), parts = (held + a.chunk - 1) / a.chunk;
     if (parts < 2) return;
-    const float l2 = row_log_sum(a, r, q_head, parts, q_heads);
-    float o[8] = {};
-    for (int32_t s = 0; s < parts; ++s) {
-      const int64_t from = ((int64_t)r * a.splits + s) * q_heads + q_head;
-      const float part = exp2_fast(a.part_lse[from] - l2);
-      const f4 x = *(const f4*)(a.part_out + from * D + d), y = *(const f4*)(a.part_out + from * D + d + 4);
+    const float* lse = a.part_lse + at * a.splits;
+    const float l2 = row_log_sum(lse, parts, lane);
+    constexpr int kEach = D / kWave;       // elements of a lane
+    float o[kEach] = {};
+    const float* from = a.part_out + at * a.splits * D + lane * kEach;
+    for (int32_t s0 = 0; s0 < parts; s0 += kWave) {
+      const int32_t count = min(kWave, parts - s0);
+      const float mine = lane < count ? exp2_fast(lse[s0 + lane] - l2) : 0.0f;
+      for (int32_t s1 = 0; s1 < count; s1 += 8) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        o[e] = fmaf(part, x[e], o[e]);
-        o[4 + e] = fmaf(part, y[e], o[4 + e]);
+        for (int i = 0; i < 8; ++i) {      // those past the last have weight 0, and read the last again
+          const int32_t s = s1 + i;
+          const float part = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), s));
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) o[e] = fmaf(part, from[(int64_t)(s0 + min(s, count - 1)) * D + e], o[e]);
+        }
       }
     }
-    *(u4*)(a.out + (int64_t)r * a.out_token + q_head * a.out_head + d) =
-        (u4){pack2<TYPE>(o[0], o[1]), pack2<TYPE>(o[2], o[3]), pack2<TYPE>(o[4], o[5]), pack2<TYPE>(o[6], o[7])};
-    if (a.lse && d == 0) a.lse[at] = l2 * 0.69314718055994531f;
+    uint16_t* out = a.out + (int64_t)r * a.out_token + q_head * a.out_head + lane * kEach;
+    if constexpr (kEach == 2) *(uint32_t*)out = pack2<TYPE>(o[0], o[1]);
+    else *out = kv::from_float<TYPE>(o[0]);
+    if (a.lse && lane == 0) a.lse[at] = l2 * 0.69314718055994531f;
     return;
   }
-  __shared__ float s_lse[kThreads];
-  const int32_t width = a.table.width, spans = (width + kMassBlocks - 1) / kMassBlocks;
+  __shared__ float s_lse[kRows];
+  const int32_t width = a.table.width, spans = (width + kThreads - 1) / kThreads;
   const uint32_t unit = blockIdx.x - outs;
   const int32_t span = unit % spans, head = unit / spans % a.pool.heads, r = unit / spans / a.pool.heads;
   const int32_t held = kv::clip_tokens(a.context[r], width, lb), parts = (held + a.chunk - 1) / a.chunk;
-  const int32_t live = (held + (1 << lb) - 1) >> lb, sub = 1 << (lb - a.log_grain);
-  const int64_t mass_at = ((int64_t)r * a.pool.heads + head) * width;
-  constexpr int kEach = kMassBlocks / kThreads;
-  float w[kEach] = {};
-  for (int32_t g0 = 0; g0 < a.group; g0 += kThreads) {
-    __syncthreads();
-    if (parts > 0 && g0 + tid < a.group) s_lse[tid] = row_log_sum(a, r, head * a.group + g0 + tid, parts, q_heads);
-    __syncthreads();
-    for (int i = 0; i < kEach; ++i) {
-      const int32_t b = span * kMassBlocks + i * kThreads + tid;
-      if (b >= live) continue;
-      const int32_t grains = min(sub, (int32_t)(((int64_t)held + (1 << a.log_grain) - 1) >> a.log_grain) - b * sub);
-      for (int32_t g = 0; g < min(kThreads, a.group - g0); ++g) {
-        const float* p = a.weights + ((int64_t)r * q_heads + head * a.group + g0 + g) * a.grains + (int64_t)b * sub;
-        for (int32_t e = 0; e < grains; ++e) w[i] += exp2_fast(p[e] - s_lse[g]);
+  const int32_t sub = 1 << (lb - a.log_grain), b = span * kThreads + tid;
+  const int64_t mass_at = ((int64_t)r * a.pool.heads + head) * width + b;
+  const int32_t grains = min(sub, (int32_t)(((int64_t)held + (1 << a.log_grain) - 1) >> a.log_grain) - b * sub);
+  float w = 0.0f;
+  if (span * kThreads * (int64_t)sub << a.log_grain < held) {
+    for (int32_t tile = 0; tile < a.row_tiles; ++tile) {
+      const int32_t rows = min(kRows, a.group - tile * kRows);
+      __syncthreads();
+      for (int32_t g = wave; g < rows; g += kWaves) {
+        const float l2 =
+            row_log_sum(a.part_lse + ((int64_t)r * q_heads + head * a.group + tile * kRows + g) * a.splits, parts, lane);
+        if (lane == 0) s_lse[g] = l2;
       }
+      __syncthreads();
+      const float* p = a.weights +
+          ((((int64_t)r * a.pool.heads + head) * a.row_tiles + tile) * a.grains + (int64_t)b * sub) * kRows;
+      for (int32_t e = 0; e < grains; ++e)
+        for (int32_t g = 0; g < rows; ++g) w += exp2_fast(p[e * kRows + g] - s_lse[g]);
     }
   }
-  for (int i = 0; i < kEach; ++i) {
-    const int32_t b = span * kMassBlocks + i * kThreads + tid;
-    if (b < width) a.mass[mass_at + b] = (a.mass_in ? a.mass_in[mass_at + b] : 0.0f) + w[i];
-  }
+  if (b < width) a.mass[mass_at] = (a.mass_in ? a.mass_in[mass_at] : 0.0f) + w;
 }
 
 // -------------------------------------------------------------------- plan
@@ -404,7 +472,7 @@ Plan plan_for(const peek_kv_pool& pool, int32_t n, int32_t q_heads, int32_t max_
   p.part_lse = at;
   if (p.splits > 1 || with_mass) at = up(at + rows * p.splits * sizeof(float));
   p.weights = at;
-  if (with_mass) at = up(at + rows * (size_t)p.grains * sizeof(float));
+  if (with_mass) at = up(at + (size_t)n * pool.kv_heads * row_tiles * (size_t)p.grains * kRows * sizeof(float));
   p.bytes = at;
   return p;
 }
@@ -451,9 +519,8 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
     a.group = q_heads / a.pool.heads;
     a.row_tiles = (a.group + kRows - 1) / kRows;
     const int64_t groups = (int64_t)n * a.pool.heads * a.row_tiles * p.splits;
-    const int32_t per_group = kThreads / (pool->head_dim / 8);
-    const int64_t outs = p.splits > 1 ? ((int64_t)n * q_heads + per_group - 1) / per_group : 0;
-    const int64_t masses = d_mass ? (int64_t)n * a.pool.heads * ((max_blocks + kMassBlocks - 1) / kMassBlocks) : 0;
+    const int64_t outs = p.splits > 1 ? ((int64_t)n * q_heads + kWaves - 1) / kWaves : 0;
+    const int64_t masses = d_mass ? (int64_t)n * a.pool.heads * ((max_blocks + kThreads - 1) / kThreads) : 0;
     if (groups >= (1 << 24) || outs + masses >= (1 << 24))
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
     hipStream_t st = (hipStream_t)stream;
@@ -479,11 +546,9 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
     a.splits = p.splits;
     set_scale(scale, &a.scale, &a.q_flip, &a.q_mask);
     with_types(type, pool->type, pool->head_dim, [&](auto t, auto m, auto d) {
-      if (d_mass) {
-        hipLaunchKernelGGL((k_decode<t(), m(), d(), true>), dim3((unsigned)groups), dim3(kThreads), 0, st, a);
-      } else {
-        hipLaunchKernelGGL((k_decode<t(), m(), d(), false>), dim3((unsigned)groups), dim3(kThreads), 0, st, a);
-      }
+      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kThreads), 0, st, a); };
+      if (a.pool.log_block >= 4) d_mass ? go(k_decode<t(), m(), d(), true, true>) : go(k_decode<t(), m(), d(), false, true>);
+      else d_mass ? go(k_decode<t(), m(), d(), true, false>) : go(k_decode<t(), m(), d(), false, false>);
     });
     hipError_t err = hipGetLastError();
     if (err == hipSuccess && outs + masses > 0) {
