@@ -45,7 +45,7 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWave * kWaves;
 constexpr int kRows = 16;
 constexpr int kTile = 32;                        // tokens of a wavefront's step
-constexpr int kMaxChunk = 2048;                  // tokens of a workgroup, at most
+constexpr int kMaxChunk = 4096;                  // tokens of a workgroup, at most
 constexpr float kSlack = 8.0f;                   // see peek_prefill.hip
 constexpr float kNone = -1e30f;
 
@@ -450,7 +450,7 @@ struct Plan {
 };
 
 // Tokens of a chunk: as many as leave about kGroups workgroups, from 256 on.
-constexpr int64_t kGroups = 2048;
+constexpr int64_t kGroups = 8192;
 
 Plan plan_for(const peek_kv_pool& pool, int32_t n, int32_t q_heads, int32_t max_blocks, bool with_mass) {
   Plan p{};
