@@ -80,6 +80,22 @@ __device__ __forceinline__ uint32_t v_piece(uint32_t t, uint32_t c) {
 }
 
 typedef __attribute__((address_space(3))) s4 lds_s4;
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+
+// Each lane's 16 bytes at `from` to LDS at `to` + 16 * lane, `to` the same for
+// the wavefront. Written out because the builtin makes every later LDS read
+// wait for the load, the reads of the other buffer included. Done when vmcnt
+// says so; no vector register is written. (m0 is reserved: the compiler keeps
+// nothing there.)
+__device__ __forceinline__ void to_lds(const uint16_t* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+               : "memory");
+}
+
+// What sched_group_barrier calls them.
+constexpr int kProducts = 0x8, kLdsReads = 0x100;
 
 template <int TYPE, int FMT, int D>
 struct Tile {
@@ -107,6 +123,13 @@ struct Tile {
         const u4 a = *(const u4*)(ks + 16 * k_piece<D>(col + 32 * j, 2 * i + half));
         s[j] = mul32<TYPE>(a, q[i], s[j]);
       }
+    }
+    // LDS reads three products ahead
+    __builtin_amdgcn_sched_group_barrier(kLdsReads, 6, 0);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kProducts, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
     }
     float inv[8];
     if constexpr (CACHED) {      // logits with their scales; keys 4 g .. 4 g + 3 share one
@@ -235,19 +258,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const uint16_t* own_k = (const uint16_t*)a.k.data + first * a.k.token + head * a.k.head;
   const uint16_t* own_v = (const uint16_t*)a.v.data + first * a.v.token + head * a.v.head;
   const int32_t own = (int32_t)(end - first);
-  auto load_own = [&](int32_t t0, int buf) {
+  const uint32_t lds_k = (uint32_t)(uintptr_t)(lds_byte*)s_k, lds_v = (uint32_t)(uintptr_t)(lds_byte*)s_v;
+  constexpr int kLoads = T::kBytes / 1024 / kWaves;      // of each of K and V, a wavefront and tile
+  int64_t lane_k[kLoads], lane_v[kLoads];                // from a tile's first token to what this lane loads
 #pragma unroll
-    for (int i = 0; i < T::kBytes / 1024 / kWaves; ++i) {
-      const uint32_t base = (i * kWaves + wave) * kWave, piece = base + lane;
-      const uint32_t t = piece / T::kPieces, at = piece % T::kPieces;
-      const int64_t key = min(t0 + (int32_t)t, own - 1);
-      const uint32_t ck = at ^ (t & (T::kPieces - 1)), cv = at ^ ((t << 1) & (T::kPieces - 1));
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(own_k + key * a.k.token + ck * 8),
-          (__attribute__((address_space(3))) void*)(s_k[buf] + base * 16), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(own_v + key * a.v.token + cv * 8),
-          (__attribute__((address_space(3))) void*)(s_v[buf] + base * 16), 16, 0, 0);
+  for (int i = 0; i < kLoads; ++i) {
+    const uint32_t piece = (i * kWaves + wave) * kWave + lane, t = piece / T::kPieces, at = piece % T::kPieces;
+    lane_k[i] = t * a.k.token + (at ^ (t & (T::kPieces - 1))) * 8;
+    lane_v[i] = t * a.v.token + (at ^ ((t << 1) & (T::kPieces - 1))) * 8;
+  }
+  auto load_own = [&](int32_t t0, int buf) {
+    const uint16_t* k0 = own_k + t0 * a.k.token;
+    const uint16_t* v0 = own_v + t0 * a.v.token;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t base = (i * kWaves + wave) * kWave;
+      int64_t from_k = lane_k[i], from_v = lane_v[i];
+      if (t0 + kKeys > own) {                            // past the end: the last token again
+        const int32_t t = (base + lane) / T::kPieces, back = max(0, t0 + t - (own - 1));
+        from_k -= back * a.k.token;
+        from_v -= back * a.v.token;
+      }
+      to_lds(k0 + from_k, lds_k + buf * T::kBytes + base * 16);
+      to_lds(v0 + from_v, lds_v + buf * T::kBytes + base * 16);
     }
   };
   // a cached tile's 16-code units of this thread: unit u of K (then of V) is codes 16 (u % (D / 16)) of key u / (D / 16)
@@ -285,7 +318,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       *(u4*)(to + 16 * p0) = (u4){x0[0], x0[1], x1[0], x1[1]};
       *(u4*)(to + 16 * p1) = (u4){x2[0], x2[1], x3[0], x3[1]};
     }
-    if (leads) s_scale[buf][unit_key / 4] = (f4){scale_k * a.scale, log2_fast(scale_v), 1.0f / scale_v, 0.0f};
+    if (leads) s_scale[buf][unit_key / 4] = (f4){scale_k * a.scale, log2_fast(scale_v), __builtin_amdgcn_rcpf(scale_v), 0.0f};
   };
 
   if (cached > 0) {
@@ -299,24 +332,28 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
 
-  for (int32_t j = 0; j < tiles; ++j) {
+  // a loop for the cached tiles and one for the sequence's own, so that each
+  // keeps the accumulators where they are
+  for (int32_t j = 0; j < cached; ++j) {
     const int buf = j & 1;
-    const bool more_cached = j + 1 < cached;
-    if (more_cached) {
+    if (j + 1 < cached) {
       fetch(j + 1);
       if (j + 2 < cached) find_page(j + 2);
-    } else if (j + 1 < tiles) {
-      load_own((j + 1 - cached) * kKeys, buf ^ 1);
-    }
-    if (j < cached) {
-      const int32_t left = held - j * kKeys;
-      if (active) tile.template step<true>(s_k[buf], s_v[buf], s_scale[buf], lane, a.scale, left < kKeys, left);
     } else {
-      const int32_t t0 = (j - cached) * kKeys;
-      if (active && t0 < most)
-        tile.template step<false>(s_k[buf], s_v[buf], nullptr, lane, a.scale, t0 + kKeys > least, token + 1 - t0);
+      load_own(0, buf ^ 1);
     }
-    if (more_cached) store(buf ^ 1);
+    const int32_t left = held - j * kKeys;
+    if (active) tile.template step<true>(s_k[buf], s_v[buf], s_scale[buf], lane, a.scale, left < kKeys, left);
+    if (j + 1 < cached) store(buf ^ 1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+  for (int32_t j = cached; j < tiles; ++j) {
+    const int buf = j & 1;
+    const int32_t t0 = (j - cached) * kKeys;
+    if (j + 1 < tiles) load_own(t0 + kKeys, buf ^ 1);
+    if (active && t0 < most)
+      tile.template step<false>(s_k[buf], s_v[buf], nullptr, lane, a.scale, t0 + kKeys > least, token + 1 - t0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
