@@ -131,6 +131,7 @@ struct Tile {
       __builtin_amdgcn_sched_group_barrier(kProducts, 2, 0);
       __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
     }
+    if constexpr (CACHED) __builtin_amdgcn_sched_barrier(0);      // the scales are read after them
     float inv[8];
     if constexpr (CACHED) {      // logits with their scales; keys 4 g .. 4 g + 3 share one
 #pragma unroll
@@ -145,13 +146,11 @@ struct Tile {
       }
     }
     if (masked) {
+      const int32_t left = seen - 4 * half;
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = 32 * j + 8 * (e >> 2) + 4 * half + (e & 3);
-          s[j][e] = key < seen ? s[j][e] : -__builtin_inff();
-        }
+        for (int e = 0; e < 16; ++e) s[j][e] = 32 * j + 8 * (e >> 2) + (e & 3) < left ? s[j][e] : -__builtin_inff();
     }
     float most = s[0][0];
 #pragma unroll
@@ -260,20 +259,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int32_t own = (int32_t)(end - first);
   const uint32_t lds_k = (uint32_t)(uintptr_t)(lds_byte*)s_k, lds_v = (uint32_t)(uintptr_t)(lds_byte*)s_v;
   constexpr int kLoads = T::kBytes / 1024 / kWaves;      // of each of K and V, a wavefront and tile
-  int64_t lane_k[kLoads], lane_v[kLoads];                // from a tile's first token to what this lane loads
+  struct From {
+    int64_t k[kLoads], v[kLoads];                        // from a tile's first token to what this lane loads
+  };
+  auto find_lane = [&](From& f, int32_t l) {
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const uint32_t piece = (i * kWaves + wave) * kWave + lane, t = piece / T::kPieces, at = piece % T::kPieces;
-    lane_k[i] = t * a.k.token + (at ^ (t & (T::kPieces - 1))) * 8;
-    lane_v[i] = t * a.v.token + (at ^ ((t << 1) & (T::kPieces - 1))) * 8;
-  }
-  auto load_own = [&](int32_t t0, int buf) {
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t piece = (i * kWaves + wave) * kWave + l, t = piece / T::kPieces, at = piece % T::kPieces;
+      f.k[i] = t * a.k.token + (at ^ (t & (T::kPieces - 1))) * 8;
+      f.v[i] = t * a.v.token + (at ^ ((t << 1) & (T::kPieces - 1))) * 8;
+    }
+  };
+  auto load_own = [&](const From& f, int32_t t0, int buf) {
     const uint16_t* k0 = own_k + t0 * a.k.token;
     const uint16_t* v0 = own_v + t0 * a.v.token;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const uint32_t base = (i * kWaves + wave) * kWave;
-      int64_t from_k = lane_k[i], from_v = lane_v[i];
+      int64_t from_k = f.k[i], from_v = f.v[i];
       if (t0 + kKeys > own) {                            // past the end: the last token again
         const int32_t t = (base + lane) / T::kPieces, back = max(0, t0 + t - (own - 1));
         from_k -= back * a.k.token;
@@ -286,23 +289,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   // a cached tile's 16-code units of this thread: unit u of K (then of V) is codes 16 (u % (D / 16)) of key u / (D / 16)
   u4 codes[T::kUnitsEach];
   float scale_k = 1.0f, scale_v = 1.0f;
-  uint32_t page = 0;
+  int32_t page = 0;      // as the table has it: looked at only when it is used, a tile later
   const int32_t unit_key = (tid % (kKeys * (D / 16))) / (D / 16), unit_at = tid % (D / 16);
   const bool leads = tid < kKeys * (D / 16) && unit_at == 0 && (unit_key & 3) == 0;     // of four keys: fetches their scales
+  const uint32_t half_bytes = ((uint32_t)a.pool.heads << a.pool.log_block) * D;         // of a page's keys, or values: <= 32 MB
+  const uint8_t* head_pages = a.pool.pages + ((int64_t)head << a.pool.log_block) * D;
+  const int32_t* ids = a.table.ids + (int64_t)r * a.table.stride;
   auto key_of = [&](int32_t j) { return min(j * kKeys + unit_key, held - 1); };
-  auto find_page = [&](int32_t j) { page = kv::page_of(a.table, a.pool, r, key_of(j) >> a.pool.log_block); };
+  auto find_page = [&](int32_t j) { page = ids[key_of(j) >> a.pool.log_block]; };
   auto fetch = [&](int32_t j) {
-    const int32_t in_block = key_of(j) & ((1 << a.pool.log_block) - 1);
+    const uint32_t id = (uint32_t)page < a.pool.num_pages ? (uint32_t)page : 0u;
+    const uint32_t in_block = key_of(j) & ((1 << a.pool.log_block) - 1);
+    const uint8_t* p = head_pages + (uint64_t)id * (2 * half_bytes) + in_block * D + unit_at * 16;
 #pragma unroll
     for (int i = 0; i < T::kUnitsEach; ++i) {
       const int is_v = T::kUnitsEach == 2 ? i : tid >= kThreads / 2;
-      const int64_t at = ((int64_t)page * 2 + is_v) * a.pool.heads + head;
-      codes[i] = *(const u4*)(a.pool.pages + ((at << a.pool.log_block) + in_block) * D + unit_at * 16);
+      codes[i] = *(const u4*)(p + (is_v ? half_bytes : 0u));
     }
     if (leads) {
-      const int64_t at = (int64_t)page * 2 * a.pool.heads + head;
-      scale_k = a.pool.scales[at];
-      scale_v = a.pool.scales[at + a.pool.heads];
+      const float* x = a.pool.scales + head + (uint64_t)id * (uint32_t)(2 * a.pool.heads);
+      scale_k = x[0];
+      scale_v = x[a.pool.heads];
     }
   };
   auto store = [&](int buf) {
@@ -327,7 +334,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (cached > 1) find_page(1);
     store(0);
   } else {
-    load_own(0, 0);
+    From f;
+    find_lane(f, lane);
+    load_own(f, 0, 0);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -340,7 +349,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       fetch(j + 1);
       if (j + 2 < cached) find_page(j + 2);
     } else {
-      load_own(0, buf ^ 1);
+      From f;
+      int32_t l = lane;
+      asm volatile("" : "+v"(l));         // the addresses are not to be kept over the loop
+      find_lane(f, l);
+      load_own(f, 0, buf ^ 1);
     }
     const int32_t left = held - j * kKeys;
     if (active) tile.template step<true>(s_k[buf], s_v[buf], s_scale[buf], lane, a.scale, left < kKeys, left);
@@ -348,10 +361,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
+  From from;
+  {
+    int32_t l = lane;
+    asm volatile("" : "+v"(l));
+    find_lane(from, l);
+  }
   for (int32_t j = cached; j < tiles; ++j) {
     const int buf = j & 1;
     const int32_t t0 = (j - cached) * kKeys;
-    if (j + 1 < tiles) load_own(t0 + kKeys, buf ^ 1);
+    if (j + 1 < tiles) load_own(from, t0 + kKeys, buf ^ 1);
     if (active && t0 < most)
       tile.template step<false>(s_k[buf], s_v[buf], nullptr, lane, a.scale, t0 + kKeys > least, token + 1 - t0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
