@@ -46,8 +46,6 @@ constexpr int kThreads = kWave * kWaves;
 constexpr int kRows = 16;
 constexpr int kTile = 32;                        // tokens of a wavefront's step
 constexpr int kMaxChunk = 4096;                  // tokens of a workgroup, at most
-constexpr float kSlack = 8.0f;                   // see peek_prefill.hip
-constexpr float kNone = -1e30f;
 
 struct Decode {
   Pool pool;
@@ -75,9 +73,6 @@ struct alignas(16) Block {
   float scale, log_v, inv_v;
   uint32_t page;
 };
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
 // Over the lanes that hold the same row: l, l ^ 16, l ^ 32, l ^ 48.
 __device__ __forceinline__ float swap16_max(float x) {
@@ -363,23 +358,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
 // and a lane to a chunk for its weight; the others turn kept logarithms into
 // the weights of kThreads blocks of a (sequence, kv head).
 
-// Base-2 logarithm of a row's sum of weights over `parts` chunks, by a whole wavefront.
-__device__ __forceinline__ float row_log_sum(const float* __restrict__ p, int32_t parts, int lane) {
-  float top = kNone, sum = 0.0f;
-  for (int32_t s = lane; s < parts; s += kWave) {
-    const float x = p[s], next = fmaxf(top, x);
-    sum = sum * exp2_fast(top - next) + exp2_fast(x - next);
-    top = next;
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    const float x = __shfl_xor(top, d), y = __shfl_xor(sum, d), next = fmaxf(top, x);
-    sum = sum * exp2_fast(top - next) + y * exp2_fast(x - next);
-    top = next;
-  }
-  return top + log2_fast(sum);
-}
-
 template <int TYPE, int D>
 __global__ __launch_bounds__(kThreads) void k_decode_join(Decode a, uint32_t outs) {
   const int32_t tid = threadIdx.x, q_heads = a.group * a.pool.heads, lb = a.pool.log_block;
@@ -390,27 +368,9 @@ __global__ __launch_bounds__(kThreads) void k_decode_join(Decode a, uint32_t out
     const int32_t r = (int32_t)(at / q_heads), q_head = (int32_t)(at % q_heads);
     const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb), parts = (held + a.chunk - 1) / a.chunk;
     if (parts < 2) return;
-    const float* lse = a.part_lse + at * a.splits;
-    const float l2 = row_log_sum(lse, parts, lane);
-    constexpr int kEach = D / kWave;       // elements of a lane
-    float o[kEach] = {};
-    const float* from = a.part_out + at * a.splits * D + lane * kEach;
-    for (int32_t s0 = 0; s0 < parts; s0 += kWave) {
-      const int32_t count = min(kWave, parts - s0);
-      const float mine = lane < count ? exp2_fast(lse[s0 + lane] - l2) : 0.0f;
-      for (int32_t s1 = 0; s1 < count; s1 += 8) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {      // those past the last have weight 0, and read the last again
-          const int32_t s = s1 + i;
-          const float part = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), s));
-#pragma unroll
-          for (int e = 0; e < kEach; ++e) o[e] = fmaf(part, from[(int64_t)(s0 + min(s, count - 1)) * D + e], o[e]);
-        }
-      }
-    }
-    uint16_t* out = a.out + (int64_t)r * a.out_token + q_head * a.out_head + lane * kEach;
-    if constexpr (kEach == 2) *(uint32_t*)out = pack2<TYPE>(o[0], o[1]);
-    else *out = kv::from_float<TYPE>(o[0]);
+    float l2;
+    uint16_t* out = a.out + (int64_t)r * a.out_token + q_head * a.out_head + lane * (D / kWave);
+    join_parts<TYPE, D>(a.part_out + at * a.splits * D, a.part_lse + at * a.splits, parts, lane, out, &l2);
     if (a.lse && lane == 0) a.lse[at] = l2 * 0.69314718055994531f;
     return;
   }

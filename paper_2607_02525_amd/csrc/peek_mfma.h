@@ -85,5 +85,58 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
 
+// ------------------------------------------- running softmax, parts of a row
+// How far (in powers of two) a row's maximum may rise before what it has
+// summed is scaled down: weights stay below 2^8, and most tiles scale nothing.
+constexpr float kSlack = 8.0f;
+constexpr float kNone = -1e30f;       // a maximum of nothing; finite, so that differences are numbers
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
+
+// Base-2 logarithm of a row's sum of weights from its parts' (-infinity: none), by a whole wavefront.
+__device__ __forceinline__ float row_log_sum(const float* __restrict__ p, int32_t parts, int lane) {
+  float top = kNone, sum = 0.0f;
+  for (int32_t s = lane; s < parts; s += 64) {
+    const float x = p[s], next = fmaxf(top, x);
+    sum = sum * exp2_fast(top - next) + exp2_fast(x - next);
+    top = next;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const float x = __shfl_xor(top, d), y = __shfl_xor(sum, d), next = fmaxf(top, x);
+    sum = sum * exp2_fast(top - next) + y * exp2_fast(x - next);
+    top = next;
+  }
+  return top + log2_fast(sum);
+}
+
+// A row's parts [parts][D] joined by a wavefront, a lane to each part for its
+// weight and to D / 64 elements (at `out`) for the sum.
+template <int TYPE, int D>
+__device__ __forceinline__ void join_parts(const float* __restrict__ part_out, const float* __restrict__ lse, int32_t parts,
+                                           int lane, uint16_t* out, float* log_sum) {
+  constexpr int kEach = D / 64;
+  const float l2 = row_log_sum(lse, parts, lane);
+  float o[kEach] = {};
+  const float* from = part_out + lane * kEach;
+  for (int32_t s0 = 0; s0 < parts; s0 += 64) {
+    const int32_t count = min(64, parts - s0);
+    const float mine = lane < count ? exp2_fast(lse[s0 + lane] - l2) : 0.0f;
+    for (int32_t s1 = 0; s1 < count; s1 += 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {      // those past the last have weight 0, and read the last again
+        const int32_t s = s1 + i;
+        const float part = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), s));
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) o[e] = fmaf(part, from[(int64_t)(s0 + min(s, count - 1)) * D + e], o[e]);
+      }
+    }
+  }
+  if constexpr (kEach == 2) *(uint32_t*)out = pack2<TYPE>(o[0], o[1]);
+  else *out = kv::from_float<TYPE>(o[0]);
+  *log_sum = l2;
+}
+
 }  // namespace mm
 }  // namespace peek

@@ -24,6 +24,8 @@
 // Rows and keys past the end: rows are clamped to the last one and not
 // stored; keys are clamped to the last one and masked, so nothing outside the
 // sequence is read.
+#include <algorithm>
+
 #include "peek_internal.h"
 #include "peek_kv.h"
 #include "peek_mfma.h"
@@ -43,11 +45,7 @@ constexpr int kWaves = 8;
 constexpr int kThreads = kWave * kWaves;
 constexpr int kRows = 32 * kWaves;    // rows of a tile
 constexpr int kKeys = 64;             // keys of a tile
-
-// How far (in powers of two) a row's maximum may rise before what it has
-// summed is scaled down: weights stay below 2^8, and most tiles scale nothing.
-constexpr float kSlack = 8.0f;
-constexpr float kNone = -1e30f;       // a maximum of nothing; finite, so that differences are numbers
+constexpr int64_t kTargetGroups = 256;
 
 struct Prefill {
   Pool pool;
@@ -58,15 +56,14 @@ struct Prefill {
   uint16_t* out;
   int64_t out_token, out_head;
   float* lse;
+  float* part_out;                    // [rows][splits][D]: a part's sum of weight * value / its sum of weights
+  float* part_lse;                    // [rows][splits]: base-2 logarithm of its sum of weights, -infinity for none
   int64_t num_tokens;
-  int32_t n, group, kv_heads;
+  int32_t n, group, kv_heads, splits;
   float scale;                        // of logits, in powers of two: >= 0
   uint32_t q_flip;                    // sign bits to flip in q, where the caller's scale is negative
   uint32_t q_mask;                    // 0 where the caller's scale is 0
 };
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
 // Where the 16-byte piece c of row t lies in a tile of D / 8 pieces a row.
 template <int D>
@@ -214,7 +211,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   // kv heads side by side (each on XCDs of its own where there are eight), the
   // last rows of the last sequences first: they have the most keys
   const int32_t head = blockIdx.x % a.kv_heads;
-  const int64_t slot = (gridDim.x - 1 - blockIdx.x) / a.kv_heads;
+  const uint32_t unit = (gridDim.x - 1 - blockIdx.x) / a.kv_heads;
+  const int32_t split = unit % a.splits;
+  const int64_t slot = unit / a.splits;
   // the last sequence r with offsets[r] * group / kRows + r <= slot: every
   // sequence has a slot for each of its tiles, some one more
   const int32_t r = kv::last_at_most(a.n, slot, lane, [&](int32_t i) { return a.offsets[i] * a.group / kRows + i; });
@@ -225,7 +224,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int32_t held = a.prefix ? kv::clip_tokens(a.prefix[r], a.table.width, a.pool.log_block) : 0;
   const int32_t cached = (held + kKeys - 1) / kKeys;
   const int32_t last_row_token = (int32_t)((min(row0 + kRows, rows) - 1) / a.group);
-  const int32_t tiles = cached + last_row_token / kKeys + 1;
+  // this part's tiles of all (the cached ones, then the sequence's own)
+  const int32_t all_tiles = cached + last_row_token / kKeys + 1, each = (all_tiles + a.splits - 1) / a.splits;
+  const int32_t tile0 = min(split * each, all_tiles), tiles = min(tile0 + each, all_tiles);
 
   // this lane's row
   const int col = lane & 31, half = lane >> 5;
@@ -328,27 +329,28 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (leads) s_scale[buf][unit_key / 4] = (f4){scale_k * a.scale, log2_fast(scale_v), __builtin_amdgcn_rcpf(scale_v), 0.0f};
   };
 
-  if (cached > 0) {
-    find_page(0);
-    fetch(0);
-    if (cached > 1) find_page(1);
-    store(0);
-  } else {
+  const int32_t cached_end = min(cached, tiles);
+  if (tile0 < cached_end) {
+    find_page(tile0);
+    fetch(tile0);
+    if (tile0 + 1 < cached_end) find_page(tile0 + 1);
+    store(tile0 & 1);
+  } else if (tile0 < tiles) {
     From f;
     find_lane(f, lane);
-    load_own(f, 0, 0);
+    load_own(f, (tile0 - cached) * kKeys, tile0 & 1);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
 
   // a loop for the cached tiles and one for the sequence's own, so that each
   // keeps the accumulators where they are
-  for (int32_t j = 0; j < cached; ++j) {
+  for (int32_t j = tile0; j < cached_end; ++j) {
     const int buf = j & 1;
-    if (j + 1 < cached) {
+    if (j + 1 < cached_end) {
       fetch(j + 1);
-      if (j + 2 < cached) find_page(j + 2);
-    } else {
+      if (j + 2 < cached_end) find_page(j + 2);
+    } else if (j + 1 < tiles) {
       From f;
       int32_t l = lane;
       asm volatile("" : "+v"(l));         // the addresses are not to be kept over the loop
@@ -357,7 +359,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
     const int32_t left = held - j * kKeys;
     if (active) tile.template step<true>(s_k[buf], s_v[buf], s_scale[buf], lane, a.scale, left < kKeys, left);
-    if (j + 1 < cached) store(buf ^ 1);
+    if (j + 1 < cached_end) store(buf ^ 1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
@@ -367,7 +369,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     asm volatile("" : "+v"(l));
     find_lane(from, l);
   }
-  for (int32_t j = cached; j < tiles; ++j) {
+  for (int32_t j = max(cached, tile0); j < tiles; ++j) {
     const int buf = j & 1;
     const int32_t t0 = (j - cached) * kKeys;
     if (j + 1 < tiles) load_own(from, t0 + kKeys, buf ^ 1);
@@ -379,18 +381,60 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
   if (!active || wave_row + col >= rows) return;
   const float sum = sum_halves(tile.sum);
-  const float part = 1.0f / sum;
+  const int64_t out_row = (first + token) * a.kv_heads * a.group + q_head;
+  if (a.splits > 1) {
+    const bool none = sum == 0.0f;      // this part has no key that the row sees
+    const float over = none ? 0.0f : 1.0f / sum;
+    float* out = a.part_out + (out_row * a.splits + split) * D + half * 4;
+#pragma unroll
+    for (int p = 0; p < T::kParts; ++p)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f16& x = tile.acc[p];
+        *(f4*)(out + 32 * p + 8 * e) = (f4){x[4 * e] * over, x[4 * e + 1] * over, x[4 * e + 2] * over, x[4 * e + 3] * over};
+      }
+    if (half == 0) a.part_lse[out_row * a.splits + split] = none ? -__builtin_inff() : tile.top + log2_fast(sum);
+    return;
+  }
+  const float over = 1.0f / sum;
   uint16_t* out = a.out + (first + token) * a.out_token + q_head * a.out_head + half * 4;
 #pragma unroll
   for (int p = 0; p < T::kParts; ++p)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const f16& x = tile.acc[p];
-      *(u2*)(out + 32 * p + 8 * e) = (u2){pack2<TYPE>(x[4 * e] * part, x[4 * e + 1] * part),
-                                          pack2<TYPE>(x[4 * e + 2] * part, x[4 * e + 3] * part)};
+      *(u2*)(out + 32 * p + 8 * e) = (u2){pack2<TYPE>(x[4 * e] * over, x[4 * e + 1] * over),
+                                          pack2<TYPE>(x[4 * e + 2] * over, x[4 * e + 3] * over)};
     }
-  if (a.lse && half == 0)
-    a.lse[(first + token) * a.kv_heads * a.group + q_head] = (tile.top + log2_fast(sum)) * 0.69314718055994531f;
+  if (a.lse && half == 0) a.lse[out_row] = (tile.top + log2_fast(sum)) * 0.69314718055994531f;
+}
+
+// Joins the parts of four rows, a wavefront to a row. Rows of no sequence are left alone.
+template <int TYPE, int D>
+__global__ __launch_bounds__(256) void k_prefill_join(Prefill a) {
+  const int lane = threadIdx.x & (kWave - 1), q_heads = a.kv_heads * a.group;
+  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t token = row / q_heads;
+  if (token >= a.num_tokens) return;
+  const int32_t q_head = (int32_t)(row - token * q_heads);
+  const int32_t r = kv::last_at_most(a.n, token, lane, [&](int32_t i) { return a.offsets[i]; });
+  if (a.offsets[r] > token || token >= a.offsets[r + 1]) return;
+  float l2;
+  uint16_t* out = a.out + token * a.out_token + q_head * a.out_head + lane * (D / kWave);
+  join_parts<TYPE, D>(a.part_out + row * a.splits * D, a.part_lse + row * a.splits, a.splits, lane, out, &l2);
+  if (a.lse && lane == 0) a.lse[row] = l2 * 0.69314718055994531f;
+}
+
+// Parts of a tile's keys, where there are too few tiles for the device's 256
+// compute units: about one workgroup each, and eight tiles of keys at least, as a
+// part costs each row 2 KB of traffic.
+int32_t splits_for(int64_t groups, int64_t num_tokens, int64_t max_context) {
+  const int64_t tiles = (max_context + num_tokens + kKeys - 1) / kKeys;
+  return (int32_t)std::max<int64_t>(1, std::min(kTargetGroups / std::max<int64_t>(1, groups), tiles / 8));
+}
+
+int64_t groups_for(int32_t n, int64_t num_tokens, int32_t q_heads, int32_t kv_heads) {
+  return (num_tokens * (q_heads / kv_heads) / kRows + n) * kv_heads;
 }
 
 }  // namespace
@@ -402,7 +446,12 @@ extern "C" {
 
 size_t peek_prefill_attention_workspace(int32_t n, int64_t num_tokens, int32_t q_heads, int32_t kv_heads,
                                         int32_t head_dim, int64_t max_context) {
-  return 0;
+  if (n < 1 || num_tokens < 1 || kv_heads < 1 || q_heads < kv_heads || (head_dim != 64 && head_dim != 128) ||
+      max_context < 0 || num_tokens >= ((int64_t)1 << 40))
+    return 0;
+  const int32_t splits = splits_for(groups_for(n, num_tokens, q_heads, kv_heads), num_tokens, max_context);
+  if (splits < 2) return 0;
+  return ((size_t)num_tokens * q_heads * splits * (head_dim + 1) * sizeof(float) + 255) & ~(size_t)255;
 }
 
 peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t num_tokens, int32_t type,
@@ -447,8 +496,10 @@ peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t 
                         peek_prefill_attention_workspace(n, num_tokens, q_heads, kv_heads, head_dim, context));
     if (s != PEEK_OK) return s;
     const int32_t group = q_heads / kv_heads;
-    if (num_tokens >= ((int64_t)1 << 40) || (num_tokens * group / kRows + n) * kv_heads >= (1 << 22))
+    const int64_t tiles = num_tokens < ((int64_t)1 << 40) ? groups_for(n, num_tokens, q_heads, kv_heads) : INT64_MAX;
+    if (tiles >= (1 << 22))
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many rows for one call (%lld)", (long long)num_tokens);
+    a.splits = splits_for(tiles, num_tokens, context);
     hipStream_t st = (hipStream_t)stream;
     s = validate_kv(n, d_offsets, num_tokens, d_prefix, false, d_block_table, max_blocks, table_stride,
                     pool ? pool->block_size : 4, pool ? pool->num_pages : 0, st);
@@ -468,9 +519,12 @@ peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t 
     a.group = group;
     a.kv_heads = kv_heads;
     set_scale(scale, &a.scale, &a.q_flip, &a.q_mask);
-    const unsigned groups = (unsigned)((num_tokens * group / kRows + n) * kv_heads);
+    a.part_out = (float*)d_workspace;
+    a.part_lse = a.part_out + num_tokens * q_heads * a.splits * head_dim;
     with_types(type, pool ? pool->type : PEEK_TYPE_F8E4M3, head_dim, [&](auto t, auto m, auto d) {
-      hipLaunchKernelGGL((k_prefill<t(), m(), d()>), dim3(groups), dim3(kThreads), 0, st, a);
+      hipLaunchKernelGGL((k_prefill<t(), m(), d()>), dim3((unsigned)(tiles * a.splits)), dim3(kThreads), 0, st, a);
+      if (a.splits > 1)
+        hipLaunchKernelGGL((k_prefill_join<t(), d()>), dim3((unsigned)((num_tokens * q_heads + 3) / 4)), dim3(256), 0, st, a);
     });
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return fail(PEEK_ERR_DEVICE, "prefill launch failed: %s", hipGetErrorString(err));
