@@ -139,7 +139,7 @@ def _arg(t, name: str, dtype=None, count: int | None = None):
         raise ValueError(f"{name} needs at least {count} elements, has {t.numel()}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _queue_n(offsets) -> int:
@@ -157,13 +157,16 @@ def _num_nodes(cache) -> int:
     return cache._num_nodes
 
 
+# The current stream's handle without a Stream object around it, where this torch has that (3 us less a call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
-    if isinstance(stream, int):
-        return ctypes.c_void_p(stream)
-    return ctypes.c_void_p(stream.cuda_stream)
+        if _raw_stream is not None and torch.cuda.is_initialized():
+            return _raw_stream(torch.cuda.current_device())
+        return torch.cuda.current_stream().cuda_stream
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def peek_tree_canonical_ids(parent, edge_offsets, edge_tokens) -> np.ndarray:

@@ -200,6 +200,17 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
+
+__device__ __forceinline__ f4 load4(const float* __restrict__ p, int32_t at, int32_t end) {
+  if (at + 4 <= end) return *(const f4_unaligned*)(p + at);
+  f4 x = {};
+  for (int i = 0; i < 3; ++i)
+    if (at + i < end) x[i] = p[at + i];
+  return x;
+}
+
 // Exclusive sum over the workgroup of two counts at once; *total gets the wholes.
 template <int THREADS>
 __device__ __forceinline__ int2 group_sum(int2 x, int2* s_part, int2* total) {
@@ -249,11 +260,22 @@ __global__ __launch_bounds__(THREADS) void k_kv_evict(
   uint32_t last = 0;       // key of the last block to go
   int32_t equal = 0;       // how many of that key go
   if (drop > 0) {
-    for (int32_t b = lo + t; b < hi; b += THREADS) {
-      float s = m[b];
-#pragma unroll 8
-      for (int32_t h = 1; h < heads; ++h) s += m[(int64_t)h * width + b];
-      key[b] = score_key(s);
+    // four blocks a thread: a row of masses begins at any multiple of 4 bytes
+    for (int32_t b = (lo & ~3) + 4 * t; b < hi; b += 4 * THREADS) {
+      f4 s = load4(m, b, width);
+      int32_t h = 1;
+      for (; h + 8 <= heads; h += 8) {
+        f4 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = load4(m + (int64_t)(h + i) * width, b, width);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += x[i];
+      }
+#pragma unroll 7
+      for (; h < heads; ++h) s += load4(m + (int64_t)h * width, b, width);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (b + i >= lo && b + i < hi) key[b + i] = score_key(s[i]);
     }
     if (t == 0) { s_prefix = 0; s_left = drop; }
 #pragma unroll
@@ -316,25 +338,36 @@ __global__ __launch_bounds__(THREADS) void k_kv_evict(
   }
   int32_t* out_ids = table_out + (int64_t)r * width;
   float* out_mass = mass_out + (int64_t)r * heads * width;
-  for (int32_t seg = seg0; seg < seg1; ++seg) {
-    uint64_t lower = 0, same = 0;
-    if (drop > 0) votes(seg, &lower, &same);
-    const uint64_t under = ((uint64_t)1 << lane) - 1;
-    const int32_t b = seg * kWave + lane, ties = mine.y + __popcll(same & under);
-    const int32_t gone = mine.x + __popcll(lower & under) + min(ties, equal);
-    const bool goes = ((lower >> lane) & 1) || (((same >> lane) & 1) && ties < equal);
-    if (b < width) {
-      const int32_t id = ids[b];
-      if (goes) {
-        freed[(int64_t)r * width + gone] = id;
-      } else {
-        out_ids[b - gone] = id;
-#pragma unroll 8
-        for (int32_t h = 0; h < heads; ++h) out_mass[(int64_t)h * width + b - gone] = m[(int64_t)h * width + b];
+  if (drop > 0) {      // a block's key becomes its place, or -1
+    for (int32_t seg = seg0; seg < seg1; ++seg) {
+      uint64_t lower, same;
+      votes(seg, &lower, &same);
+      const uint64_t under = ((uint64_t)1 << lane) - 1;
+      const int32_t b = seg * kWave + lane, ties = mine.y + __popcll(same & under);
+      const int32_t gone = mine.x + __popcll(lower & under) + min(ties, equal);
+      const bool goes = ((lower >> lane) & 1) || (((same >> lane) & 1) && ties < equal);
+      if (b < width) {
+        if (goes) freed[(int64_t)r * width + gone] = ids[b];
+        key[b] = goes ? 0xffffffffu : (uint32_t)(b - gone);
       }
+      mine.x += __popcll(lower);
+      mine.y += __popcll(same);
     }
-    mine.x += __popcll(lower);
-    mine.y += __popcll(same);
+    __syncthreads();
+  }
+  for (int32_t b = t; b < width; b += THREADS) {
+    const int32_t to = drop > 0 ? (int32_t)key[b] : b;
+    if (to < 0) continue;
+    out_ids[to] = ids[b];
+    int32_t h = 0;
+    for (; h + 8 <= heads; h += 8) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = m[(int64_t)(h + i) * width + b];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) out_mass[(int64_t)(h + i) * width + to] = x[i];
+    }
+    for (; h < heads; ++h) out_mass[(int64_t)h * width + to] = m[(int64_t)h * width + b];
   }
   for (int32_t b = drop + t; b < width; b += THREADS) freed[(int64_t)r * width + b] = -1;
   for (int32_t b = width - drop + t; b < width; b += THREADS) {
