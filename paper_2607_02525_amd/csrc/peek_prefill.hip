@@ -129,51 +129,60 @@ struct Tile {
       __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
     }
     if constexpr (CACHED) __builtin_amdgcn_sched_barrier(0);      // the scales are read after them
-    float inv[8];
-    if constexpr (CACHED) {      // logits with their scales; keys 4 g .. 4 g + 3 share one
-#pragma unroll
-      for (int g = 0; g < 8; ++g) {
-        const f4 c = scales[2 * g + half];
-        inv[g] = c[2];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int at = (g & 3) * 4 + e;
-          s[g >> 2][at] = fmaf(s[g >> 2][at], c[0], c[1]);
-        }
-      }
-    }
-    if (masked) {
+    if (masked) {                // (a logit's scale is at least 2^-100: -infinity stays)
       const int32_t left = seen - 4 * half;
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[j][e] = 32 * j + 8 * (e >> 2) + (e & 3) < left ? s[j][e] : -__builtin_inff();
     }
-    float most = s[0][0];
+    auto largest = [&]() {
+      float most = s[0][0];
 #pragma unroll
-    for (int e = 1; e < 32; ++e) most = fmaxf(most, s[e >> 4][e & 15]);
-    most = max_halves(most);
-    if constexpr (!CACHED) most *= scale;
-    if (__any(most > top + kSlack)) {
-      const float next = most > top + kSlack ? most : top;
-      const float fall = exp2_fast(top - next);
+      for (int e = 1; e < 32; ++e) most = fmaxf(most, s[e >> 4][e & 15]);
+      return max_halves(most);
+    };
+    auto raise = [&](float most) {
+      const float next = most > top + kSlack ? most : top, fall = exp2_fast(top - next);
       top = next;
       sum *= fall;
 #pragma unroll
       for (int p = 0; p < kParts; ++p) acc[p] *= fall;
-    }
+    };
+    if constexpr (CACHED) {      // keys 4 g .. 4 g + 3 share a scale of logits, and its values' logarithm and reciprocal
+      f4 by[8];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+      for (int g = 0; g < 8; ++g) by[g] = scales[2 * g + half];
+      auto scaled = [&](const f16* from, f16* to, float less) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        if constexpr (CACHED) {
-          s[j][e] = exp2_fast(s[j][e] - top);
-          sum = fmaf(s[j][e], inv[4 * j + (e >> 2)], sum);
-        } else {
-          s[j][e] = exp2_fast(fmaf(s[j][e], scale, -top));
-          sum += s[j][e];
+        for (int g = 0; g < 8; ++g) {
+          const float add = by[g][1] - less;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            to[g >> 2][(g & 3) * 4 + e] = fmaf(from[g >> 2][(g & 3) * 4 + e], by[g][0], add);
         }
+      };
+      const f16 raw[2] = {s[0], s[1]};
+      scaled(raw, s, top);       // less the maximum so far: most often that is all
+      if (__any(largest() > kSlack)) {
+        scaled(raw, s, 0.0f);    // (beside kNone nothing is left of a logit)
+        raise(largest());
+        scaled(raw, s, top);
       }
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        s[e >> 4][e & 15] = exp2_fast(s[e >> 4][e & 15]);
+        sum = fmaf(s[e >> 4][e & 15], by[e >> 2][2], sum);
+      }
+    } else {
+      const float most = largest() * scale;
+      if (__any(most > top + kSlack)) raise(most);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        s[e >> 4][e & 15] = exp2_fast(fmaf(s[e >> 4][e & 15], scale, -top));
+        sum += s[e >> 4][e & 15];
+      }
+    }
     // lane l reads, for the 16 lanes of its group, four tokens of 16 columns
     const uint32_t i16 = lane & 15, wide = (lane >> 4) & 1;
 #pragma unroll
