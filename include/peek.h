@@ -407,7 +407,7 @@ typedef struct peek_kv_pool {
  * that gets new tokens, for K and for V and for every head:
  *   a  = the largest finite magnitude among the block's new values
  *   s' = F8E4M3: the smallest power of two with a <= 448 * s'
- *        I8:     a / 127
+ *        I8:     a * (1 / 127), both in 32 bits
  *        (both kept within 2^-60 .. 2^60)
  *   s  = s' if the block's first token is new, else max(s', old scale)
  *   code = x / s (in 32 bits) to the nearest the format holds, ties to even,
@@ -437,7 +437,7 @@ peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_toke
  * d_lse (nullable) is float32[num_tokens][q_heads]. Rows in no sequence are
  * left as they are. A prompt's own later tokens reach none of its rows'
  * weights, but a NaN or infinity among their values may reach rows of the
- * same sequence up to 255 tokens before them.
+ * same sequence up to 63 tokens before them.
  * Scratch comes only from d_workspace (device, 256-byte aligned, at least
  * peek_prefill_attention_workspace bytes for these sizes; max_context =
  * max_blocks * block_size, 0 without a cache). Asynchronous on `stream`.

@@ -43,7 +43,7 @@ __device__ __forceinline__ float scale_of(float most) {
     e = max(-60, min(60, e));
     return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
   } else {
-    return fminf(fmaxf(most / 127.0f, kv::kScaleMin), kv::kScaleMax);
+    return fminf(fmaxf(most * (1.0f / 127.0f), kv::kScaleMin), kv::kScaleMax);
   }
 }
 

@@ -60,8 +60,8 @@ def logit_error(reach, dim):
 
 def out_bound(out, spread, reach, dtype, tokens=0, most=0.0):
     """|computed - exact| of an output element: the output's own rounding, the rounding of each weight to the type, the
-    weights' error through their logits (twice: above and below the fraction), and 2^-18 for sums, exponentials and scales in
-    32 bits. A weight below the type's normal range is off by up to SMALLEST of the largest: `tokens` of them, times the
+    weights' error through their logits (twice: above and below the fraction), and 2^-18 for sums, exponentials and scales
+    in 32 bits. A weight below the type's normal range is off by up to SMALLEST of the largest: `tokens` of them, times the
     largest value that any scale lets a code stand for (`most`)."""
     u = ROUNDOFF[dtype]
     delta = logit_error(reach, out.shape[-1])[..., None]
@@ -69,7 +69,7 @@ def out_bound(out, spread, reach, dtype, tokens=0, most=0.0):
 
 
 def most_of(scales, fmt):
-    """The largest value that a code of this pool can stand for (pages in no use have NaN for a scale), or 8 of fresh rows."""
+    """The largest value that a code of this pool can stand for (unused pages have NaN for a scale), or 8 of fresh rows."""
     live = scales[~scales.isnan()]
     return max(8.0, float(live.max()) * (448 if fmt == torch.float8_e4m3fn else 127) if live.numel() else 0.0)
 
@@ -101,7 +101,8 @@ def round_e4m3(y):
 
 def block_scale(most, fmt):
     if fmt == torch.int8:
-        return float(np.clip(np.float32(most) / np.float32(127), np.float32(2.0 ** -60), np.float32(2.0 ** 60)))
+        s = np.float32(most) * (np.float32(1) / np.float32(127))     # 32 bits, as defined
+        return float(np.clip(s, np.float32(2.0 ** -60), np.float32(2.0 ** 60)))
     e = -60 if most == 0 else math.ceil(math.log2(most / 448.0))
     while most > 448.0 * 2.0 ** e:
         e += 1
@@ -111,7 +112,7 @@ def block_scale(most, fmt):
 
 
 def quantised(x, scale, fmt):
-    """Values (not codes' bits) that x's codes stand for, before the scale; the quotient is one of 32 bits, as defined."""
+    """Values (not bits) that x's codes stand for, before the scale; the quotient is one of 32 bits, as defined."""
     with np.errstate(invalid="ignore", over="ignore"):
         y = (x.astype(np.float32) / np.float32(scale)).astype(np.float64)
     if fmt == torch.int8:

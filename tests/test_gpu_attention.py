@@ -186,8 +186,6 @@ def test_pages_past_32_bit_offsets():
     table = torch.tensor([[N - 1, 5, N - 2]], dtype=torch.int32)
     zero = torch.zeros(1, dtype=torch.int32).cuda()
     P.peek_kv_append(pool, dk, dv, torch.tensor([0, T]).cuda(), zero, table.cuda())
-    codes = torch.zeros(N, 1, dtype=torch.uint8)    # only the three pages are looked at
-    del codes
     ids = table[0].long().cuda()
     pages = pool.pages.view(torch.uint8)[ids].view(F8).cpu()
     scales = pool.scales[ids].cpu()
@@ -217,6 +215,8 @@ PREFILL = [
     ([(0, 700)], 1, 7, 16, 128, BF, F8),
     ([(100, 1), (3, 1), (0, 1)], 1, 33, 16, 128, BF, F8),
     ([(0, 0), (16, 0)], 1, 4, 16, 128, BF, F8),
+    ([(0, 2100)], 1, 1, 16, 64, BF, F8),                                # few tiles: keys in parts, of which early rows see one
+    ([(1500, 600), (0, 40)], 1, 2, 16, 128, HF, F8),
 ]
 
 
@@ -256,7 +256,8 @@ def run_prefill(gen, seqs, H, G, B, D, dtype, fmt, layout="plain", scale=None, c
         pk, pv = R.cached(codes, scales, table[r], held[r])
         want, wl, _, spread_, reach = R.attend(q[a:b], torch.cat([pk, k[a:b].double()]),
                                                torch.cat([pv, v[a:b].double()]), s, held[r] + 1)
-        near(out[a:b], want, R.out_bound(want, spread_, reach, dtype, held[r] + new[r], most), f"out of sequence {r} {seqs[r]}")
+        near(out[a:b], want, R.out_bound(want, spread_, reach, dtype, held[r] + new[r], most),
+             f"out of sequence {r} {seqs[r]}")
         near(lse[a:b], wl, R.lse_bound(wl, reach, D), f"lse of sequence {r} {seqs[r]}")
     assert (out[sum(new):] == -7).all() and (lse[sum(new):] == -7).all(), "rows of no sequence were written"
     return (dq, dk, dv, doff, out, ws), dict(scale=scale, lse=lse, **more)
@@ -328,6 +329,18 @@ def test_decode_equals_a_prefill_of_one_token():
         near(out, want, R.out_bound(want, spread, reach, BF), "out")
 
 
+def test_many_short_sequences():
+    """More sequences than one look of 64 places, or two, can tell apart."""
+    gen = torch.Generator().manual_seed(14)
+    for n in (65, 4097, 6000):
+        lens = torch.randint(0, 4, (n,), generator=gen).tolist()
+        held = (torch.randint(0, 3, (n,), generator=gen) * 4).tolist()
+        seqs = list(zip(held, lens))
+        run_prefill(gen, seqs, 1, 1, 4, 64, BF, I8)
+        run_append(gen, seqs, 1, 4, 64, BF, F8)
+        run_decode(gen, held, 1, 2, 4, 64, HF, F8)
+
+
 # ------------------------------------------------------------------ append
 APPEND = [
     # (cached before, new), kv heads, block, dim, dtype, format
@@ -397,7 +410,7 @@ def test_append_zeros_tiny_huge_and_nonfinite_values(fmt):
 
 
 def test_append_one_token_at_a_time_fills_a_block():
-    """Sixteen appends of one token: the scale never falls, and every older code is the one that the definition gives."""
+    """Sixteen appends of one token: the scale never falls, and older codes are those that the definition gives."""
     import paper_2607_02525_amd as P
     gen = torch.Generator().manual_seed(13)
     H, B, D = 2, 16, 128
@@ -458,8 +471,8 @@ def run_evict(contexts, H, B, keep, sink, recent, kind, seed=0, spare_columns=3)
     out = [torch.full((n, W), -5, dtype=torch.int32).cuda(), torch.full((n, H, W), -5.0).cuda(),
            torch.full((n, W), -5, dtype=torch.int32).cuda(), torch.full((n,), -5, dtype=torch.int32).cuda()]
     ws = torch.full((max(256, P.peek_kv_evict_workspace(n, H, W)),), 0xFF, dtype=torch.uint8).cuda()
-    P.peek_kv_evict(ctx, wide.cuda()[:, :W], torch.from_numpy(mass).cuda(), torch.tensor(keep, dtype=torch.int32).cuda(),
-                    B, sink, recent, ctx, *out, ws)       # the context is updated in place
+    P.peek_kv_evict(ctx, wide.cuda()[:, :W], torch.from_numpy(mass).cuda(),
+                    torch.tensor(keep, dtype=torch.int32).cuda(), B, sink, recent, ctx, *out, ws)  # context in place
     torch.cuda.synchronize()
     c, t, m, f, k = R.evict(contexts, table, mass, keep, B, sink, recent)
     np.testing.assert_array_equal(out[3].cpu().numpy(), k)
@@ -568,7 +581,8 @@ def test_validation_reports_broken_preconditions(monkeypatch):
         return e.value.status, str(e.value)
 
     P.peek_decode_attention(pool, q, torch.tensor([32], **i32), good, out, ws)
-    for ctx, table in ((33, good), (-1, good), (32, torch.tensor([[0, 4]], **i32)), (32, torch.tensor([[-1, 0]], **i32))):
+    outside, none = torch.tensor([[0, 4]], **i32), torch.tensor([[-1, 0]], **i32)
+    for ctx, table in ((33, good), (-1, good), (32, outside), (32, none)):
         held = torch.tensor([ctx], **i32)
         calls = [lambda: P.peek_decode_attention(pool, q, held, table, out, ws),
                  lambda: P.peek_prefill_attention(q, k, k, one, out, ws, pool=pool, prefix=held, block_table=table)]
