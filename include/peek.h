@@ -435,9 +435,8 @@ peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_toke
  *   x_j = scale * q . k_j
  *   out = sum_j exp(x_j) v_j / sum_j exp(x_j),   lse = log sum_j exp(x_j)
  * d_lse (nullable) is float32[num_tokens][q_heads]. Rows in no sequence are
- * left as they are. A prompt's own later tokens reach none of its rows'
- * weights, but a NaN or infinity among their values may reach rows of the
- * same sequence up to 63 tokens before them.
+ * left as they are. A prompt's later tokens do not reach its earlier rows,
+ * whatever they hold.
  * Scratch comes only from d_workspace (device, 256-byte aligned, at least
  * peek_prefill_attention_workspace bytes for these sizes; max_context =
  * max_blocks * block_size, 0 without a cache). Asynchronous on `stream`.

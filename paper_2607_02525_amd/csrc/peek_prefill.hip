@@ -183,28 +183,87 @@ struct Tile {
         sum += s[e >> 4][e & 15];
       }
     }
-    // lane l reads, for the 16 lanes of its group, four tokens of 16 columns
-    const uint32_t i16 = lane & 15, wide = (lane >> 4) & 1;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    auto weights = [&](int i) {
       const f16& w = s[i >> 1];
       const int o = (i & 1) * 8;
-      u4 b;
-      b[0] = pack2<TYPE>(w[o + 0], w[o + 1]);
-      b[1] = pack2<TYPE>(w[o + 2], w[o + 3]);
-      b[2] = pack2<TYPE>(w[o + 4], w[o + 5]);
-      b[3] = pack2<TYPE>(w[o + 6], w[o + 7]);
+      return (u4){pack2<TYPE>(w[o], w[o + 1]), pack2<TYPE>(w[o + 2], w[o + 3]), pack2<TYPE>(w[o + 4], w[o + 5]),
+                  pack2<TYPE>(w[o + 6], w[o + 7])};
+    };
+    // lane l reads, for the 16 lanes of its group, four tokens of 16 columns
+    const uint32_t i16 = lane & 15, wide = (lane >> 4) & 1;
+    auto values = [&](int i, int p) {
+      u2 part[2];
 #pragma unroll
-      for (int p = 0; p < kParts; ++p) {
-        u2 part[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t t = 16 * i + 8 * h + 4 * half + (i16 >> 2);
-          const uint32_t at = 16 * v_piece<D>(t, 4 * p + 2 * wide + ((i16 >> 1) & 1)) + 8 * (i16 & 1);
-          part[h] = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(vs + at)));
-        }
-        acc[p] = mul32<TYPE>((u4){part[0][0], part[0][1], part[1][0], part[1][1]}, b, acc[p]);
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t t = 16 * i + 8 * h + 4 * half + (i16 >> 2);
+        const uint32_t at = 16 * v_piece<D>(t, 4 * p + 2 * wide + ((i16 >> 1) & 1)) + 8 * (i16 & 1);
+        part[h] = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(vs + at)));
       }
+      return (u4){part[0][0], part[0][1], part[1][0], part[1][1]};
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u4 w = weights(i);
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) acc[p] = mul32<TYPE>(values(i, p), w, acc[p]);
+    }
+  }
+
+  // An element that is infinite or NaN, and eight of them with only those or without.
+  static __device__ __forceinline__ bool odd(uint32_t x) {
+    return (x & 0x7fffu) >= (TYPE == PEEK_TYPE_BF16 ? 0x7f80u : 0x7c00u);
+  }
+  static __device__ __forceinline__ uint32_t only(uint32_t w, bool odds) {
+    return (odd(w) == odds ? w & 0xffffu : 0u) | (odd(w >> 16) == odds ? w & 0xffff0000u : 0u);
+  }
+
+  // Puts zeros for what is infinite or NaN in this wavefront's share of a tile; whether there was any.
+  static __device__ __forceinline__ bool clean(uint8_t* tile, int wave, int lane) {
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < kBytes / 1024 / kWaves; ++i) {
+      u4* at = (u4*)(tile + ((i * kWaves + wave) * kWave + lane) * 16);
+      const u4 x = *at;
+      u4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = only(x[e], false);
+      const bool differs = x[0] != y[0] || x[1] != y[1] || x[2] != y[2] || x[3] != y[3];
+      if (differs) *at = y;
+      found = found || differs;
+    }
+    return __any(found);
+  }
+
+  // Adds the infinite and NaN values of own keys [t0, end) to the rows, of which
+  // each sees the first `seen`: one key at a time, so that a row takes only what
+  // it sees. With the final maximum; the sum has their weights already.
+  __device__ __forceinline__ void add_seen(const uint16_t* k, int64_t k_token, const uint16_t* v, int64_t v_token, int32_t t0,
+                                           int32_t end, int half, float scale, int32_t seen) {
+    for (int32_t t = t0; t < end; ++t) {
+      float dot = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const u4 x = *(const u4*)(k + t * k_token + 16 * i + 8 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t a = x[e], b = q[i][e];
+          dot = fmaf(kv::to_float<TYPE>((uint16_t)a), kv::to_float<TYPE>((uint16_t)b), dot);
+          dot = fmaf(kv::to_float<TYPE>((uint16_t)(a >> 16)), kv::to_float<TYPE>((uint16_t)(b >> 16)), dot);
+        }
+      }
+      const float w = exp2_fast(fmaf(sum_halves(dot), scale, -top));
+      if (t >= seen) continue;
+#pragma unroll
+      for (int p = 0; p < kParts; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const u2 x = *(const u2*)(v + t * v_token + 32 * p + 8 * e + 4 * half);
+          const uint32_t a = only(x[0], true), b = only(x[1], true);
+          acc[p][4 * e] = fmaf(w, kv::to_float<TYPE>((uint16_t)a), acc[p][4 * e]);
+          acc[p][4 * e + 1] = fmaf(w, kv::to_float<TYPE>((uint16_t)(a >> 16)), acc[p][4 * e + 1]);
+          acc[p][4 * e + 2] = fmaf(w, kv::to_float<TYPE>((uint16_t)b), acc[p][4 * e + 2]);
+          acc[p][4 * e + 3] = fmaf(w, kv::to_float<TYPE>((uint16_t)(b >> 16)), acc[p][4 * e + 3]);
+        }
     }
   }
 };
@@ -215,6 +274,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   __shared__ __attribute__((aligned(1024))) uint8_t s_k[2][T::kBytes];
   __shared__ __attribute__((aligned(1024))) uint8_t s_v[2][T::kBytes];
   __shared__ f4 s_scale[2][kKeys / 4];
+  __shared__ uint32_t s_odd;
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   // kv heads side by side (each on XCDs of its own where there are eight), the
@@ -338,6 +398,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (leads) s_scale[buf][unit_key / 4] = (f4){scale_k * a.scale, log2_fast(scale_v), __builtin_amdgcn_rcpf(scale_v), 0.0f};
   };
 
+  if (tid == 0) s_odd = 0;
   const int32_t cached_end = min(cached, tiles);
   if (tile0 < cached_end) {
     find_page(tile0);
@@ -378,16 +439,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     asm volatile("" : "+v"(l));
     find_lane(from, l);
   }
+  // from here on, some row must not see all of a tile, and 0 times a NaN or an
+  // infinity is no 0: such values are taken out of it, and given to the rows that see them at the end
+  const int32_t whole = cached + (int32_t)(row0 / a.group + 1) / kKeys;
   for (int32_t j = max(cached, tile0); j < tiles; ++j) {
     const int buf = j & 1;
     const int32_t t0 = (j - cached) * kKeys;
     if (j + 1 < tiles) load_own(from, t0 + kKeys, buf ^ 1);
+    if (j >= whole) {
+      if (T::clean(s_v[buf], wave, lane) && lane == 0) atomicOr(&s_odd, 1u << (j - whole));
+      __syncthreads();
+    }
     if (active && t0 < most)
       tile.template step<false>(s_k[buf], s_v[buf], nullptr, lane, a.scale, t0 + kKeys > least, token + 1 - t0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
-
+  // (a tile of rows spans 256 tokens at most: five tiles of keys)
+  for (uint32_t odd = active ? s_odd : 0; odd != 0; odd &= odd - 1) {
+    const int32_t t0 = (whole - cached + (int32_t)__builtin_ctz(odd)) * kKeys;
+    tile.add_seen(own_k, a.k.token, own_v, a.v.token, t0, min(t0 + kKeys, most), half, a.scale, token + 1);
+  }
   if (!active || wave_row + col >= rows) return;
   const float sum = sum_halves(tile.sum);
   const int64_t out_row = (first + token) * a.kv_heads * a.group + q_head;

@@ -329,6 +329,30 @@ def test_decode_equals_a_prefill_of_one_token():
         near(out, want, R.out_bound(want, spread, reach, BF), "out")
 
 
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 64)])
+def test_prefill_does_not_see_later_tokens_whatever_they_hold(dtype, D):
+    """NaN and infinities in K and V of some tokens: rows before them are as if they were not there; rows from
+    them on have what the sums give (an infinity of one sign, or NaN), element by element."""
+    import paper_2607_02525_amd as P
+    gen = torch.Generator().manual_seed(15)
+    H, G, new = 2, 4, [150, 70]
+    T = sum(new)
+    q, k, v = ((torch.randn(T, h, D, generator=gen)).to(dtype) for h in (H * G, H, H))
+    v[20, 0, 3], v[21, 0, 4], v[40, 0, 4], v[100, 0, 5] = math.nan, math.inf, -math.inf, -math.inf
+    v[63, 0, 7], v[149, 0], k[130, 0, 1], v[160, 1, 9] = math.inf, math.nan, math.nan, math.nan
+    doff = torch.tensor([0, 150, 220]).cuda()
+    dq = q.cuda()
+    out, lse = torch.empty_like(dq), torch.empty(T, H * G).cuda()
+    ws = torch.empty(P.peek_prefill_attention_workspace(2, T, H * G, H, D, 0) + 256, dtype=torch.uint8).cuda()
+    P.peek_prefill_attention(dq, k.cuda(), v.cuda(), doff, out, ws, lse=lse)
+    for a, b in ((0, 150), (150, 220)):
+        for i in range(a, b):
+            want, wl, _, spread, reach = R.attend(q[i:i + 1], k[a:i + 1], v[a:i + 1], D ** -0.5, i - a + 1)
+            bound = R.out_bound(want, spread, reach, dtype, i - a + 1, 8.0).nan_to_num(0, 0)
+            near(out[i:i + 1], want, bound, f"out of row {i - a}")
+            near(lse[i:i + 1], wl, R.lse_bound(wl, reach, D).nan_to_num(0, 0), f"lse of row {i - a}")
+
+
 def test_many_short_sequences():
     """More sequences than one look of 64 places, or two, can tell apart."""
     gen = torch.Generator().manual_seed(14)
