@@ -77,17 +77,18 @@ __device__ __forceinline__ uint32_t v_piece(uint32_t t, uint32_t c) {
 }
 
 typedef __attribute__((address_space(3))) s4 lds_s4;
+typedef __attribute__((address_space(3))) u4 lds_u4;
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 
-// Each lane's 16 bytes at `from` to LDS at `to` + 16 * lane, `to` the same for
-// the wavefront. Written out because the builtin makes every later LDS read
-// wait for the load, the reads of the other buffer included. Done when vmcnt
-// says so; no vector register is written. (m0 is reserved: the compiler keeps
-// nothing there.)
-__device__ __forceinline__ void to_lds(const uint16_t* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+// Each lane's 16 bytes at `base` + its offset to LDS at `to` + 16 * lane, base
+// and `to` the same for the wavefront. Written out because the builtin makes
+// every later LDS read wait for the load, the reads of the other buffer
+// included. Done when vmcnt says so; no vector register is written. (m0 is
+// reserved: the compiler keeps nothing there.)
+__device__ __forceinline__ void to_lds(const uint16_t* base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
-               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+               : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(base)
                : "memory");
 }
 
@@ -107,17 +108,34 @@ struct Tile {
   f16 acc[kParts];
   float top, sum;
 
-  // weights of 64 keys and what they add
+  // Where lane l begins to read a tile of K, and of V, at `tile` of LDS. From
+  // there, k step i is at ^ 32 i and part p of the output at ^ 64 p: addresses
+  // that are made anew for every tile take fewer registers than those kept.
+  static __device__ __forceinline__ uint32_t k_lane(uint32_t tile, int lane) {
+    uint32_t at = tile + 16 * k_piece<D>(lane & 31, lane >> 5);
+    asm volatile("" : "+v"(at));
+    return at;
+  }
+  static __device__ __forceinline__ uint32_t v_lane(uint32_t tile, int lane) {
+    // lane l reads, for the 16 lanes of its group, four tokens of 16 columns
+    const uint32_t i16 = lane & 15, t = 4 * (lane >> 5) + (i16 >> 2), piece = 2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1);
+    uint32_t at = tile + 16 * v_piece<D>(t, piece) + 8 * (i16 & 1);
+    asm volatile("" : "+v"(at));
+    return at;
+  }
+
+  // weights of 64 keys and what they add; K and V at these places of LDS
   template <bool CACHED>
-  __device__ __forceinline__ void step(const uint8_t* ks, const uint8_t* vs, const f4* scales, int lane, float scale,
-                                       bool masked, int32_t seen) {
-    const int col = lane & 31, half = lane >> 5;
+  __device__ __forceinline__ void step(uint32_t ks, uint32_t vs, const f4* scales, int lane, float scale, bool masked,
+                                       int32_t seen) {
+    const int half = lane >> 5;
+    const uint32_t at_k = k_lane(ks, lane);
     f16 s[2] = {};
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const u4 a = *(const u4*)(ks + 16 * k_piece<D>(col + 32 * j, 2 * i + half));
+        const u4 a = *(const lds_u4*)(uintptr_t)((at_k ^ (32 * i)) + 32 * j * D * 2);
         s[j] = mul32<TYPE>(a, q[i], s[j]);
       }
     }
@@ -189,16 +207,13 @@ struct Tile {
       return (u4){pack2<TYPE>(w[o], w[o + 1]), pack2<TYPE>(w[o + 2], w[o + 3]), pack2<TYPE>(w[o + 4], w[o + 5]),
                   pack2<TYPE>(w[o + 6], w[o + 7])};
     };
-    // lane l reads, for the 16 lanes of its group, four tokens of 16 columns
-    const uint32_t i16 = lane & 15, wide = (lane >> 4) & 1;
+    const uint32_t at_v = v_lane(vs, lane);
     auto values = [&](int i, int p) {
       u2 part[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t t = 16 * i + 8 * h + 4 * half + (i16 >> 2);
-        const uint32_t at = 16 * v_piece<D>(t, 4 * p + 2 * wide + ((i16 >> 1) & 1)) + 8 * (i16 & 1);
-        part[h] = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(vs + at)));
-      }
+      for (int h = 0; h < 2; ++h)
+        part[h] = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                             (lds_s4*)(uintptr_t)((at_v ^ (64 * p)) + (16 * i + 8 * h) * D * 2)));
       return (u4){part[0][0], part[0][1], part[1][0], part[1][1]};
     };
 #pragma unroll
@@ -329,31 +344,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int32_t own = (int32_t)(end - first);
   const uint32_t lds_k = (uint32_t)(uintptr_t)(lds_byte*)s_k, lds_v = (uint32_t)(uintptr_t)(lds_byte*)s_v;
   constexpr int kLoads = T::kBytes / 1024 / kWaves;      // of each of K and V, a wavefront and tile
-  struct From {
-    int64_t k[kLoads], v[kLoads];                        // from a tile's first token to what this lane loads
-  };
-  auto find_lane = [&](From& f, int32_t l) {
+  uint32_t from_k[kLoads], from_v[kLoads];               // bytes from a tile's first token to what this lane loads
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const uint32_t piece = (i * kWaves + wave) * kWave + l, t = piece / T::kPieces, at = piece % T::kPieces;
-      f.k[i] = t * a.k.token + (at ^ (t & (T::kPieces - 1))) * 8;
-      f.v[i] = t * a.v.token + (at ^ ((t << 1) & (T::kPieces - 1))) * 8;
-    }
-  };
-  auto load_own = [&](const From& f, int32_t t0, int buf) {
+  for (int i = 0; i < kLoads; ++i) {
+    const uint32_t piece = (i * kWaves + wave) * kWave + lane, t = piece / T::kPieces, at = piece % T::kPieces;
+    from_k[i] = t * (uint32_t)a.k.token * 2 + (at ^ (t & (T::kPieces - 1))) * 16;
+    from_v[i] = t * (uint32_t)a.v.token * 2 + (at ^ ((t << 1) & (T::kPieces - 1))) * 16;
+  }
+  auto load_own = [&](int32_t t0, int buf) {
     const uint16_t* k0 = own_k + t0 * a.k.token;
     const uint16_t* v0 = own_v + t0 * a.v.token;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const uint32_t base = (i * kWaves + wave) * kWave;
-      int64_t from_k = f.k[i], from_v = f.v[i];
-      if (t0 + kKeys > own) {                            // past the end: the last token again
-        const int32_t t = (base + lane) / T::kPieces, back = max(0, t0 + t - (own - 1));
-        from_k -= back * a.k.token;
-        from_v -= back * a.v.token;
-      }
-      to_lds(k0 + from_k, lds_k + buf * T::kBytes + base * 16);
-      to_lds(v0 + from_v, lds_v + buf * T::kBytes + base * 16);
+      uint32_t back = 0;
+      if (t0 + kKeys > own) back = max(0, t0 + (int32_t)((base + lane) / T::kPieces) - (own - 1));   // the last token again
+      to_lds(k0, from_k[i] - back * (uint32_t)a.k.token * 2, lds_k + buf * T::kBytes + base * 16);
+      to_lds(v0, from_v[i] - back * (uint32_t)a.v.token * 2, lds_v + buf * T::kBytes + base * 16);
     }
   };
   // a cached tile's 16-code units of this thread: unit u of K (then of V) is codes 16 (u % (D / 16)) of key u / (D / 16)
@@ -406,9 +413,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (tile0 + 1 < cached_end) find_page(tile0 + 1);
     store(tile0 & 1);
   } else if (tile0 < tiles) {
-    From f;
-    find_lane(f, lane);
-    load_own(f, (tile0 - cached) * kKeys, tile0 & 1);
+    load_own((tile0 - cached) * kKeys, tile0 & 1);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -421,23 +426,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       fetch(j + 1);
       if (j + 2 < cached_end) find_page(j + 2);
     } else if (j + 1 < tiles) {
-      From f;
-      int32_t l = lane;
-      asm volatile("" : "+v"(l));         // the addresses are not to be kept over the loop
-      find_lane(f, l);
-      load_own(f, 0, buf ^ 1);
+      load_own(0, buf ^ 1);
     }
     const int32_t left = held - j * kKeys;
-    if (active) tile.template step<true>(s_k[buf], s_v[buf], s_scale[buf], lane, a.scale, left < kKeys, left);
+    if (active) tile.template step<true>(lds_k + buf * T::kBytes, lds_v + buf * T::kBytes, s_scale[buf], lane, a.scale, left < kKeys, left);
     if (j + 1 < cached_end) store(buf ^ 1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-  }
-  From from;
-  {
-    int32_t l = lane;
-    asm volatile("" : "+v"(l));
-    find_lane(from, l);
   }
   // from here on, some row must not see all of a tile, and 0 times a NaN or an
   // infinity is no 0: such values are taken out of it, and given to the rows that see them at the end
@@ -445,13 +440,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   for (int32_t j = max(cached, tile0); j < tiles; ++j) {
     const int buf = j & 1;
     const int32_t t0 = (j - cached) * kKeys;
-    if (j + 1 < tiles) load_own(from, t0 + kKeys, buf ^ 1);
+    if (j + 1 < tiles) load_own(t0 + kKeys, buf ^ 1);
     if (j >= whole) {
       if (T::clean(s_v[buf], wave, lane) && lane == 0) atomicOr(&s_odd, 1u << (j - whole));
       __syncthreads();
     }
     if (active && t0 < most)
-      tile.template step<false>(s_k[buf], s_v[buf], nullptr, lane, a.scale, t0 + kKeys > least, token + 1 - t0);
+      tile.template step<false>(lds_k + buf * T::kBytes, lds_v + buf * T::kBytes, nullptr, lane, a.scale, t0 + kKeys > least, token + 1 - t0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
@@ -571,6 +566,9 @@ peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t 
     if ((s = check_rows("d_k", d_k, k_token_stride, k_head_stride)) != PEEK_OK) return s;
     if ((s = check_rows("d_v", d_v, v_token_stride, v_head_stride)) != PEEK_OK) return s;
     if ((s = check_rows("d_out", d_out, out_token_stride, out_head_stride)) != PEEK_OK) return s;
+    if (k_token_stride >= (1 << 23) || v_token_stride >= (1 << 23))
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "the token strides of d_k and d_v must be below 2^23 (got %lld, %lld)",
+                  (long long)k_token_stride, (long long)v_token_stride);
     if (!d_offsets) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_offsets must not be NULL");
     const int64_t context = pool ? (int64_t)max_blocks * pool->block_size : 0;
     s = check_workspace(d_workspace, workspace_bytes,
