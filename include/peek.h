@@ -440,6 +440,7 @@ peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_toke
  * Scratch comes only from d_workspace (device, 256-byte aligned, at least
  * peek_prefill_attention_workspace bytes for these sizes; max_context =
  * max_blocks * block_size, 0 without a cache). Asynchronous on `stream`.
+ * The token strides of k and v are below 2^23.
  * Errors: INVALID_ARGUMENT, WORKSPACE_TOO_SMALL, DEVICE.
  * ---------------------------------------------------------------------- */
 size_t peek_prefill_attention_workspace(int32_t n, int64_t num_tokens, int32_t q_heads, int32_t kv_heads,

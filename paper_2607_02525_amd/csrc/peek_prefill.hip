@@ -70,10 +70,12 @@ template <int D>
 __device__ __forceinline__ uint32_t k_piece(uint32_t t, uint32_t c) {
   return t * (D / 8) + (c ^ (t & (D / 8 - 1)));
 }
-// V is read by 16 lanes at a time from two adjacent pieces of four rows.
+// V is read by 32 lanes at a time, from four adjacent pieces of four rows: all
+// of the 64 banks, once these lie in different quarters (halves, where two rows fill the banks).
+__device__ __forceinline__ uint32_t v_turn(uint32_t t, int dim) { return dim == 128 ? (t << 2) & 12 : (t << 1) & 4; }
 template <int D>
 __device__ __forceinline__ uint32_t v_piece(uint32_t t, uint32_t c) {
-  return t * (D / 8) + (c ^ ((t << 1) & (D / 8 - 1)));
+  return t * (D / 8) + (c ^ v_turn(t, D));
 }
 
 typedef __attribute__((address_space(3))) s4 lds_s4;
@@ -349,7 +351,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   for (int i = 0; i < kLoads; ++i) {
     const uint32_t piece = (i * kWaves + wave) * kWave + lane, t = piece / T::kPieces, at = piece % T::kPieces;
     from_k[i] = t * (uint32_t)a.k.token * 2 + (at ^ (t & (T::kPieces - 1))) * 16;
-    from_v[i] = t * (uint32_t)a.v.token * 2 + (at ^ ((t << 1) & (T::kPieces - 1))) * 16;
+    from_v[i] = t * (uint32_t)a.v.token * 2 + (at ^ v_turn(t, D)) * 16;
   }
   auto load_own = [&](int32_t t0, int buf) {
     const uint16_t* k0 = own_k + t0 * a.k.token;

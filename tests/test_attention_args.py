@@ -92,7 +92,7 @@ def test_attention_refusals():
                    dict(out=None), dict(out=ODD), dict(os=(512, 100))):
             assert call(p, **kw) == BAD, kw
     for kw in (dict(h=4), dict(d=64), dict(d=96), dict(h=0), dict(k=None), dict(v=ODD), dict(off=None),
-               dict(tokens=-1)):
+               dict(tokens=-1), dict(ks=(1 << 23, 128)), dict(vs=(1 << 23, 128))):
         assert prefill(p, **kw) == BAD, kw
     assert decode(p, ctx=None) == BAD
     assert decode(p, mass_in=FAKE) == BAD and "d_mass" in P.peek_last_error()
