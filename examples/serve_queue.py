@@ -32,7 +32,7 @@ from paper_2607_02525_amd.runner import HotPath  # noqa: E402
 
 
 class Pages:
-    """Which page holds what: free ones, users of each, and the page of a cached block by the page before it and its tokens."""
+    """Which page holds what: free ones, users of each, the page of a cached block by the page before and its tokens."""
 
     def __init__(self, count: int):
         self.free = list(range(count - 1, -1, -1))

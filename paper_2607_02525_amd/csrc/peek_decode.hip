@@ -59,7 +59,7 @@ struct Decode {
   float* mass;
   float* part_out;       // [n][q_heads][splits][D]: a chunk's sum of weight * value / its sum of weights
   float* part_lse;       // [n][q_heads][splits]: base-2 logarithm of its sum of weights
-  float* weights;        // [n][kv_heads][row_tiles][grains][16]: base-2 logarithm of the weight on every grain of tokens
+  float* weights;        // [n][kv_heads][row_tiles][grains][16]: base-2 logarithm of the weight on a grain of tokens
   int64_t grains;
   int32_t log_grain;
   int32_t n, group, row_tiles, chunk, splits;
@@ -507,8 +507,11 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
     set_scale(scale, &a.scale, &a.q_flip, &a.q_mask);
     with_types(type, pool->type, pool->head_dim, [&](auto t, auto m, auto d) {
       auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kThreads), 0, st, a); };
-      if (a.pool.log_block >= 4) d_mass ? go(k_decode<t(), m(), d(), true, true>) : go(k_decode<t(), m(), d(), false, true>);
-      else d_mass ? go(k_decode<t(), m(), d(), true, false>) : go(k_decode<t(), m(), d(), false, false>);
+      if (a.pool.log_block >= 4) {
+        d_mass ? go(k_decode<t(), m(), d(), true, true>) : go(k_decode<t(), m(), d(), false, true>);
+      } else {
+        d_mass ? go(k_decode<t(), m(), d(), true, false>) : go(k_decode<t(), m(), d(), false, false>);
+      }
     });
     hipError_t err = hipGetLastError();
     if (err == hipSuccess && outs + masses > 0) {

@@ -75,8 +75,7 @@ __device__ __forceinline__ uint32_t codes_of(const float* x, float scale, float 
     uint32_t u[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) u[i] = __builtin_bit_cast(uint32_t, y[i] + 12582912.0f);
-    const uint32_t ab = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400), cd = __builtin_amdgcn_perm(u[3], u[2], 0x04000c0c);
-    return ab | cd;
+    return __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400) | __builtin_amdgcn_perm(u[3], u[2], 0x04000c0c);
   }
 }
 
@@ -174,7 +173,8 @@ __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, in
       if (p < pieces) {
         float y[8];
         spread8<TYPE>(w[i], y);
-        *(u2*)(codes + old * D + p * 8) = (u2){codes_of<FMT>(y, scale, inv, plain), codes_of<FMT>(y + 4, scale, inv, plain)};
+        *(u2*)(codes + old * D + p * 8) =
+            (u2){codes_of<FMT>(y, scale, inv, plain), codes_of<FMT>(y + 4, scale, inv, plain)};
       }
     }
   }
@@ -436,7 +436,8 @@ peek_status validate_kv(int32_t n, const int64_t* d_offsets, int64_t num_tokens,
 
 peek_status check_pool(const peek_kv_pool* p, Pool* out) {
   if (!p) return fail(PEEK_ERR_INVALID_ARGUMENT, "pool is NULL");
-  if (!p->d_pages || !p->d_scales) return fail(PEEK_ERR_INVALID_ARGUMENT, "the pool's d_pages and d_scales must not be NULL");
+  if (!p->d_pages || !p->d_scales)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "the pool's d_pages and d_scales must not be NULL");
   if ((reinterpret_cast<uintptr_t>(p->d_pages) & 15) != 0)
     return fail(PEEK_ERR_INVALID_ARGUMENT, "the pool's d_pages must be 16-byte aligned");
   if (p->num_pages < 1 || p->num_pages > INT32_MAX)
@@ -532,7 +533,8 @@ peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_toke
       return fail(PEEK_ERR_INVALID_ARGUMENT, "d_offsets and d_context must not be NULL");
     const int64_t slots = (num_tokens >> p.log_block) + 2 * (int64_t)n;
     const int64_t groups = (slots * 2 * p.heads + 3) / 4;
-    if (groups >= (1 << 24)) return fail(PEEK_ERR_INVALID_ARGUMENT, "too many tokens for one call (%lld)", (long long)num_tokens);
+    if (groups >= (1 << 24))
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "too many tokens for one call (%lld)", (long long)num_tokens);
     hipStream_t st = (hipStream_t)stream;
     s = validate_kv(n, d_offsets, num_tokens, d_context, true, d_block_table, max_blocks, table_stride,
                     pool->block_size, pool->num_pages, st);
@@ -589,12 +591,14 @@ peek_status peek_kv_evict(int32_t n, int32_t kv_heads, int32_t block_size, const
         return fail(PEEK_ERR_INVALID_ARGUMENT, "d_workspace must be 256-byte aligned");
     }
     hipStream_t st = (hipStream_t)stream;
-    s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, block_size, INT32_MAX, st);
+    s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, block_size, INT32_MAX,
+                    st);
     if (s != PEEK_OK) return s;
     const bool in_lds = max_blocks <= kEvictLdsKeys;
     auto go = [&](auto kernel, int threads) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(threads), in_lds ? max_blocks * sizeof(uint32_t) : 0, st, kv_heads,
-                         __builtin_ctz((unsigned)block_size), d_context, Table{d_block_table, table_stride, max_blocks},
+      hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(threads), in_lds ? max_blocks * sizeof(uint32_t) : 0, st,
+                         kv_heads, __builtin_ctz((unsigned)block_size), d_context,
+                         Table{d_block_table, table_stride, max_blocks},
                          d_mass, d_keep, sink, recent, d_context_out, d_table_out, d_mass_out, d_freed, d_num_freed,
                          (uint32_t*)d_workspace, in_lds ? 1 : 0);
     };

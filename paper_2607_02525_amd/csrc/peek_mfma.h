@@ -114,8 +114,8 @@ __device__ __forceinline__ float row_log_sum(const float* __restrict__ p, int32_
 // A row's parts [parts][D] joined by a wavefront, a lane to each part for its
 // weight and to D / 64 elements (at `out`) for the sum.
 template <int TYPE, int D>
-__device__ __forceinline__ void join_parts(const float* __restrict__ part_out, const float* __restrict__ lse, int32_t parts,
-                                           int lane, uint16_t* out, float* log_sum) {
+__device__ __forceinline__ void join_parts(const float* __restrict__ part_out, const float* __restrict__ lse,
+                                           int32_t parts, int lane, uint16_t* out, float* log_sum) {
   constexpr int kEach = D / 64;
   const float l2 = row_log_sum(lse, parts, lane);
   float o[kEach] = {};

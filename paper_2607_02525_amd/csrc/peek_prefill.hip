@@ -169,8 +169,8 @@ struct Tile {
 #pragma unroll
       for (int p = 0; p < kParts; ++p) acc[p] *= fall;
     };
-    if constexpr (CACHED) {      // keys 4 g .. 4 g + 3 share a scale of logits, and its values' logarithm and reciprocal
-      f4 by[8];
+    if constexpr (CACHED) {
+      f4 by[8];                  // of keys 4 g .. 4 g + 3: the logits' scale, the values' logarithm and reciprocal
 #pragma unroll
       for (int g = 0; g < 8; ++g) by[g] = scales[2 * g + half];
       auto scaled = [&](const f16* from, f16* to, float less) {
@@ -254,8 +254,8 @@ struct Tile {
   // Adds the infinite and NaN values of own keys [t0, end) to the rows, of which
   // each sees the first `seen`: one key at a time, so that a row takes only what
   // it sees. With the final maximum; the sum has their weights already.
-  __device__ __forceinline__ void add_seen(const uint16_t* k, int64_t k_token, const uint16_t* v, int64_t v_token, int32_t t0,
-                                           int32_t end, int half, float scale, int32_t seen) {
+  __device__ __forceinline__ void add_seen(const uint16_t* k, int64_t k_token, const uint16_t* v, int64_t v_token,
+                                           int32_t t0, int32_t end, int half, float scale, int32_t seen) {
     for (int32_t t = t0; t < end; ++t) {
       float dot = 0.0f;
 #pragma unroll
@@ -360,18 +360,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     for (int i = 0; i < kLoads; ++i) {
       const uint32_t base = (i * kWaves + wave) * kWave;
       uint32_t back = 0;
-      if (t0 + kKeys > own) back = max(0, t0 + (int32_t)((base + lane) / T::kPieces) - (own - 1));   // the last token again
+      if (t0 + kKeys > own)                              // past the end: the last token again
+        back = max(0, t0 + (int32_t)((base + lane) / T::kPieces) - (own - 1));
       to_lds(k0, from_k[i] - back * (uint32_t)a.k.token * 2, lds_k + buf * T::kBytes + base * 16);
       to_lds(v0, from_v[i] - back * (uint32_t)a.v.token * 2, lds_v + buf * T::kBytes + base * 16);
     }
   };
-  // a cached tile's 16-code units of this thread: unit u of K (then of V) is codes 16 (u % (D / 16)) of key u / (D / 16)
+  // a cached tile's 16-code units of this thread: unit u of K (then of V) is
+  // codes 16 (u % (D / 16)) of key u / (D / 16)
   u4 codes[T::kUnitsEach];
   float scale_k = 1.0f, scale_v = 1.0f;
   int32_t page = 0;      // as the table has it: looked at only when it is used, a tile later
   const int32_t unit_key = (tid % (kKeys * (D / 16))) / (D / 16), unit_at = tid % (D / 16);
-  const bool leads = tid < kKeys * (D / 16) && unit_at == 0 && (unit_key & 3) == 0;     // of four keys: fetches their scales
-  const uint32_t half_bytes = ((uint32_t)a.pool.heads << a.pool.log_block) * D;         // of a page's keys, or values: <= 32 MB
+  const bool leads = tid < kKeys * (D / 16) && unit_at == 0 && (unit_key & 3) == 0;     // four keys: fetches their scales
+  const uint32_t half_bytes = ((uint32_t)a.pool.heads << a.pool.log_block) * D;         // a page's keys, or values
   const uint8_t* head_pages = a.pool.pages + ((int64_t)head << a.pool.log_block) * D;
   const int32_t* ids = a.table.ids + (int64_t)r * a.table.stride;
   auto key_of = [&](int32_t j) { return min(j * kKeys + unit_key, held - 1); };
@@ -404,7 +406,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       *(u4*)(to + 16 * p0) = (u4){x0[0], x0[1], x1[0], x1[1]};
       *(u4*)(to + 16 * p1) = (u4){x2[0], x2[1], x3[0], x3[1]};
     }
-    if (leads) s_scale[buf][unit_key / 4] = (f4){scale_k * a.scale, log2_fast(scale_v), __builtin_amdgcn_rcpf(scale_v), 0.0f};
+    if (leads)
+      s_scale[buf][unit_key / 4] =
+          (f4){scale_k * a.scale, log2_fast(scale_v), __builtin_amdgcn_rcpf(scale_v), 0.0f};
   };
 
   if (tid == 0) s_odd = 0;
@@ -431,7 +435,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       load_own(0, buf ^ 1);
     }
     const int32_t left = held - j * kKeys;
-    if (active) tile.template step<true>(lds_k + buf * T::kBytes, lds_v + buf * T::kBytes, s_scale[buf], lane, a.scale, left < kKeys, left);
+    if (active)
+      tile.template step<true>(lds_k + buf * T::kBytes, lds_v + buf * T::kBytes, s_scale[buf], lane, a.scale,
+                               left < kKeys, left);
     if (j + 1 < cached_end) store(buf ^ 1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -448,7 +454,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       __syncthreads();
     }
     if (active && t0 < most)
-      tile.template step<false>(lds_k + buf * T::kBytes, lds_v + buf * T::kBytes, nullptr, lane, a.scale, t0 + kKeys > least, token + 1 - t0);
+      tile.template step<false>(lds_k + buf * T::kBytes, lds_v + buf * T::kBytes, nullptr, lane, a.scale,
+                                t0 + kKeys > least, token + 1 - t0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
@@ -605,7 +612,8 @@ peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t 
     with_types(type, pool ? pool->type : PEEK_TYPE_F8E4M3, head_dim, [&](auto t, auto m, auto d) {
       hipLaunchKernelGGL((k_prefill<t(), m(), d()>), dim3((unsigned)(tiles * a.splits)), dim3(kThreads), 0, st, a);
       if (a.splits > 1)
-        hipLaunchKernelGGL((k_prefill_join<t(), d()>), dim3((unsigned)((num_tokens * q_heads + 3) / 4)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((k_prefill_join<t(), d()>), dim3((unsigned)((num_tokens * q_heads + 3) / 4)), dim3(256), 0, st,
+                           a);
     });
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return fail(PEEK_ERR_DEVICE, "prefill launch failed: %s", hipGetErrorString(err));

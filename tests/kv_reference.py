@@ -60,16 +60,16 @@ def logit_error(reach, dim):
 
 def out_bound(out, spread, reach, dtype, tokens=0, most=0.0):
     """|computed - exact| of an output element: the output's own rounding, the rounding of each weight to the type, the
-    weights' error through their logits (twice: above and below the fraction), and 2^-18 for sums, exponentials and scales
-    in 32 bits. A weight below the type's normal range is off by up to SMALLEST of the largest: `tokens` of them, times the
-    largest value that any scale lets a code stand for (`most`)."""
+    weights' error through their logits (twice: above and below the fraction), and 2^-18 for sums, exponentials and
+    scales in 32 bits. A weight below the type's normal range is off by up to SMALLEST of the largest: `tokens` of them,
+    times the largest value that any scale lets a code stand for (`most`)."""
     u = ROUNDOFF[dtype]
     delta = logit_error(reach, out.shape[-1])[..., None]
     return u * out.abs() + (1 + u) * (u + 2.1 * delta + 2.0 ** -18) * spread + SMALLEST[dtype] * (1 + tokens * most)
 
 
 def most_of(scales, fmt):
-    """The largest value that a code of this pool can stand for (unused pages have NaN for a scale), or 8 of fresh rows."""
+    """The largest value that a code of this pool can stand for (unused pages' scales are NaN), or 8 of fresh rows."""
     live = scales[~scales.isnan()]
     return max(8.0, float(live.max()) * (448 if fmt == torch.float8_e4m3fn else 127) if live.numel() else 0.0)
 

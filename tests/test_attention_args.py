@@ -1,5 +1,5 @@
-"""Host-only checks of the calls on the cache's contents: what they refuse, before any GPU work, and how much scratch they
-ask for. Fake device pointers are never read."""
+"""Host-only checks of the calls on the cache's contents: what they refuse, before any GPU work, and how much scratch
+they ask for. Fake device pointers are never read."""
 import ctypes
 
 import pytest
@@ -44,8 +44,8 @@ def decode(p, n=2, type=0, hq=4, q=FAKE, qs=(512, 128), ctx=FAKE, table=FAKE, bl
                                      stride, scale, out, *os, None, mass_in, mass, ws, size, None)
 
 
-def evict(n=2, h=2, block=16, ctx=FAKE, table=FAKE, blocks=4, stride=4, mass=ctypes.c_void_p(0x20000), keep=FAKE, sink=0,
-          recent=1, ctx_out=FAKE, table_out=ctypes.c_void_p(0x30000), mass_out=ctypes.c_void_p(0x40000),
+def evict(n=2, h=2, block=16, ctx=FAKE, table=FAKE, blocks=4, stride=4, mass=ctypes.c_void_p(0x20000), keep=FAKE,
+          sink=0, recent=1, ctx_out=FAKE, table_out=ctypes.c_void_p(0x30000), mass_out=ctypes.c_void_p(0x40000),
           freed=ctypes.c_void_p(0x50000), num=FAKE, ws=FAKE, size=1 << 40):
     return LIB.peek_kv_evict(n, h, block, ctx, table, blocks, stride, mass, keep, sink, recent, ctx_out, table_out,
                              mass_out, freed, num, ws, size, None)

@@ -215,7 +215,7 @@ PREFILL = [
     ([(0, 700)], 1, 7, 16, 128, BF, F8),
     ([(100, 1), (3, 1), (0, 1)], 1, 33, 16, 128, BF, F8),
     ([(0, 0), (16, 0)], 1, 4, 16, 128, BF, F8),
-    ([(0, 2100)], 1, 1, 16, 64, BF, F8),                                # few tiles: keys in parts, of which early rows see one
+    ([(0, 2100)], 1, 1, 16, 64, BF, F8),       # few tiles: keys in parts, of which early rows see one
     ([(1500, 600), (0, 40)], 1, 2, 16, 128, HF, F8),
 ]
 
