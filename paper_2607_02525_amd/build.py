@@ -21,7 +21,7 @@ FORCED = ["-DPEEK_SAMPLE_SEED=0", "-DPEEK_WAIT_SPINS=0"]
 BUILD_DIR = os.path.join(HERE, "_build")
 
 # Nothing of these depends on FORCED: compiled once, linked into both libraries
-UNFORCED = ["peek_kv.hip", "peek_prefill.hip", "peek_decode.hip"]
+UNFORCED = ["peek_kv.hip", "peek_kv_evict.hip", "peek_prefill.hip", "peek_decode.hip"]
 SOURCES = ["peek_host.hip", "peek_walk.hip", "peek_signals.hip", "peek_evict.hip", "peek_blocks.hip",
            "peek_noalloc.hip", *UNFORCED]
 

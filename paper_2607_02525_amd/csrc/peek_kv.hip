@@ -1,5 +1,5 @@
 // The cache's contents on gfx950: quantising new tokens into 8-bit pages, and
-// evicting the blocks of a sequence that attention hardly reads.
+// the checks that the calls on pages share.
 #include "peek_internal.h"
 #include "peek_kv.h"
 #include "peek_validate.h"
@@ -181,205 +181,6 @@ __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, in
   if (lane == 0) pool.scales[at] = scale;
 }
 
-// ---------------------------------------------------------------- eviction
-//
-// One workgroup per sequence. Scores become keys whose unsigned order is
-// theirs, kept in LDS (in the workspace, where a table is too wide for that);
-// three counting passes of 11, 11 and 10 bits find the key of the last block to
-// go. The blocks below it go, and the first `equal` of those that equal
-// it, so the number gone before a block is (lower keys before it) +
-// min(equal keys before it, equal): one sum over 64-block segments places
-// every block.
-
-constexpr int kEvictBins = 2048;
-constexpr int kEvictLdsKeys = 32768;      // 128 KB
-
-__device__ __forceinline__ uint32_t score_key(float x) {
-  if (x != x) return 0xffffffffu;
-  const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);   // -0 counts as 0
-  return (u >> 31) ? ~u : u | 0x80000000u;
-}
-
-typedef float f4 __attribute__((ext_vector_type(4)));
-typedef float f4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
-
-__device__ __forceinline__ f4 load4(const float* __restrict__ p, int32_t at, int32_t end) {
-  if (at + 4 <= end) return *(const f4_unaligned*)(p + at);
-  f4 x = {};
-  for (int i = 0; i < 3; ++i)
-    if (at + i < end) x[i] = p[at + i];
-  return x;
-}
-
-// Exclusive sum over the workgroup of two counts at once; *total gets the wholes.
-template <int THREADS>
-__device__ __forceinline__ int2 group_sum(int2 x, int2* s_part, int2* total) {
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  int2 inc = x;
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int a = __shfl_up(inc.x, d), b = __shfl_up(inc.y, d);
-    if (lane >= d) { inc.x += a; inc.y += b; }
-  }
-  if (lane == kWave - 1) s_part[wave] = inc;
-  __syncthreads();
-  int2 before{0, 0}, all{0, 0};
-#pragma unroll
-  for (int w = 0; w < THREADS / kWave; ++w) {
-    const int2 p = s_part[w];
-    if (w < wave) { before.x += p.x; before.y += p.y; }
-    all.x += p.x;
-    all.y += p.y;
-  }
-  __syncthreads();
-  *total = all;
-  return int2{before.x + inc.x - x.x, before.y + inc.y - x.y};
-}
-
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void k_kv_evict(
-    int32_t heads, int32_t log_block, const int32_t* context, Table table, const float* __restrict__ mass,
-    const int32_t* __restrict__ keep, int32_t sink, int32_t recent, int32_t* context_out,
-    int32_t* __restrict__ table_out, float* __restrict__ mass_out, int32_t* __restrict__ freed,
-    int32_t* __restrict__ num_freed, uint32_t* __restrict__ workspace, int32_t keys_in_lds) {
-  extern __shared__ uint32_t s_keys[];
-  __shared__ int32_t s_count[kEvictBins];
-  __shared__ int2 s_part[THREADS / kWave];
-  __shared__ int2 s_wave[THREADS / kWave];
-  __shared__ uint32_t s_prefix;
-  __shared__ int32_t s_left;
-  const int32_t r = blockIdx.x, t = threadIdx.x, width = table.width;
-  const int lane = t & (kWave - 1), wave = t / kWave;
-  const int32_t* ids = table.ids + (int64_t)r * table.stride;
-  const float* m = mass + (int64_t)r * heads * width;
-  uint32_t* key = keys_in_lds ? s_keys : workspace + (int64_t)r * width;
-  const int32_t ctx = context[r];
-  const int32_t nb = (int32_t)(((int64_t)kv::clip_tokens(ctx, width, log_block) + (1 << log_block) - 1) >> log_block);
-  const int32_t lo = min(sink, nb), hi = (int32_t)max((int64_t)lo, (int64_t)nb - recent);
-  const int32_t drop = (int32_t)min((int64_t)(hi - lo), max((int64_t)0, (int64_t)nb - max(0, keep[r])));
-
-  uint32_t last = 0;       // key of the last block to go
-  int32_t equal = 0;       // how many of that key go
-  if (drop > 0) {
-    // four blocks a thread: a row of masses begins at any multiple of 4 bytes
-    for (int32_t b = (lo & ~3) + 4 * t; b < hi; b += 4 * THREADS) {
-      f4 s = load4(m, b, width);
-      int32_t h = 1;
-      for (; h + 8 <= heads; h += 8) {
-        f4 x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = load4(m + (int64_t)(h + i) * width, b, width);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += x[i];
-      }
-#pragma unroll 7
-      for (; h < heads; ++h) s += load4(m + (int64_t)h * width, b, width);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (b + i >= lo && b + i < hi) key[b + i] = score_key(s[i]);
-    }
-    if (t == 0) { s_prefix = 0; s_left = drop; }
-#pragma unroll
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-      for (int32_t i = t; i < kEvictBins; i += THREADS) s_count[i] = 0;
-      __syncthreads();
-      const uint32_t prefix = s_prefix, above = pass == 0 ? 0u : 0xffffffffu << (shift + bits);
-      const int32_t left = s_left;
-      for (int32_t b = lo + t; b < hi; b += THREADS) {
-        const uint32_t k = key[b];
-        if ((k & above) == prefix) atomicAdd(&s_count[(k >> shift) & ((1 << bits) - 1)], 1);
-      }
-      __syncthreads();
-      constexpr int kEach = kEvictBins / THREADS;
-      int32_t c[kEach], sum = 0;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) sum += c[i] = s_count[t * kEach + i];
-      int2 all;
-      int32_t before = group_sum<THREADS>(int2{sum, 0}, s_part, &all).x;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        if (before < left && left <= before + c[i]) {
-          s_prefix = prefix | ((uint32_t)(t * kEach + i) << shift);
-          s_left = left - before;
-        }
-        before += c[i];
-      }
-      __syncthreads();
-    }
-    last = s_prefix;
-    equal = s_left;
-  }
-
-  // A wavefront places a run of 64-block segments; what lies before the run first
-  const int32_t segments = (width + kWave - 1) / kWave, each = (segments + THREADS / kWave - 1) / (THREADS / kWave);
-  const int32_t seg0 = min(segments, wave * each), seg1 = min(segments, seg0 + each);
-  auto votes = [&](int32_t seg, uint64_t* lower, uint64_t* same) {
-    const int32_t b = seg * kWave + lane;
-    const bool able = drop > 0 && b >= lo && b < hi;
-    const uint32_t k = able ? key[b] : 0xffffffffu;
-    *lower = __ballot(able && k < last);
-    *same = __ballot(able && k == last);
-  };
-  int2 mine{0, 0};
-  if (drop > 0) {
-    for (int32_t seg = seg0; seg < seg1; ++seg) {
-      uint64_t lower, same;
-      votes(seg, &lower, &same);
-      mine.x += __popcll(lower);
-      mine.y += __popcll(same);
-    }
-    if (lane == 0) s_wave[wave] = mine;
-    __syncthreads();
-    mine = int2{0, 0};
-    for (int w = 0; w < wave; ++w) {
-      mine.x += s_wave[w].x;
-      mine.y += s_wave[w].y;
-    }
-  }
-  int32_t* out_ids = table_out + (int64_t)r * width;
-  float* out_mass = mass_out + (int64_t)r * heads * width;
-  if (drop > 0) {      // a block's key becomes its place, or -1
-    for (int32_t seg = seg0; seg < seg1; ++seg) {
-      uint64_t lower, same;
-      votes(seg, &lower, &same);
-      const uint64_t under = ((uint64_t)1 << lane) - 1;
-      const int32_t b = seg * kWave + lane, ties = mine.y + __popcll(same & under);
-      const int32_t gone = mine.x + __popcll(lower & under) + min(ties, equal);
-      const bool goes = ((lower >> lane) & 1) || (((same >> lane) & 1) && ties < equal);
-      if (b < width) {
-        if (goes) freed[(int64_t)r * width + gone] = ids[b];
-        key[b] = goes ? 0xffffffffu : (uint32_t)(b - gone);
-      }
-      mine.x += __popcll(lower);
-      mine.y += __popcll(same);
-    }
-    __syncthreads();
-  }
-  for (int32_t b = t; b < width; b += THREADS) {
-    const int32_t to = drop > 0 ? (int32_t)key[b] : b;
-    if (to < 0) continue;
-    out_ids[to] = ids[b];
-    int32_t h = 0;
-    for (; h + 8 <= heads; h += 8) {
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = m[(int64_t)(h + i) * width + b];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) out_mass[(int64_t)(h + i) * width + to] = x[i];
-    }
-    for (; h < heads; ++h) out_mass[(int64_t)h * width + to] = m[(int64_t)h * width + b];
-  }
-  for (int32_t b = drop + t; b < width; b += THREADS) freed[(int64_t)r * width + b] = -1;
-  for (int32_t b = width - drop + t; b < width; b += THREADS) {
-    out_ids[b] = -1;
-    for (int32_t h = 0; h < heads; ++h) out_mass[(int64_t)h * width + b] = 0.0f;
-  }
-  if (t == 0) {
-    num_freed[r] = drop;
-    context_out[r] = ctx - (drop << log_block);
-  }
-}
-
 // -------------------------------------------------------------- validation
 __global__ void k_validate_kv(int32_t n, const int64_t* __restrict__ offsets, int64_t num_tokens,
                               const int32_t* __restrict__ len, bool appends, Table table, int32_t log_block,
@@ -495,14 +296,6 @@ peek_status check_workspace(const void* d_workspace, size_t bytes, size_t need) 
   return PEEK_OK;
 }
 
-namespace {
-
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
-}
-
-}  // namespace
 }  // namespace peek
 
 using namespace peek;
@@ -548,64 +341,6 @@ peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_toke
     with_types(type, pool->type, pool->head_dim, [&](auto e, auto f, auto d) { go(k_kv_append<e(), f(), d()>); });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "append launch failed: %s", hipGetErrorString(e));
-    return PEEK_OK;
-  });
-}
-
-size_t peek_kv_evict_workspace(int32_t n, int32_t kv_heads, int32_t max_blocks) {
-  if (n < 0 || kv_heads < 1 || max_blocks <= kEvictLdsKeys) return 0;
-  return ((size_t)n * max_blocks * sizeof(uint32_t) + 255) & ~(size_t)255;
-}
-
-peek_status peek_kv_evict(int32_t n, int32_t kv_heads, int32_t block_size, const int32_t* d_context,
-                          const int32_t* d_block_table, int32_t max_blocks, int64_t table_stride, const float* d_mass,
-                          const int32_t* d_keep, int32_t sink, int32_t recent, int32_t* d_context_out,
-                          int32_t* d_table_out, float* d_mass_out, int32_t* d_freed, int32_t* d_num_freed,
-                          void* d_workspace, size_t workspace_bytes, void* stream) {
-  return guarded([&]() -> peek_status {
-    clear_error();
-    if (n < 0 || n >= (1 << 22)) return fail(PEEK_ERR_INVALID_ARGUMENT, "n must be in [0, 2^22) (got %d)", n);
-    if (kv_heads < 1 || kv_heads > 1024)
-      return fail(PEEK_ERR_INVALID_ARGUMENT, "kv_heads must be in [1, 1024] (got %d)", kv_heads);
-    if (block_size < 4 || block_size > 256 || (block_size & (block_size - 1)) != 0)
-      return fail(PEEK_ERR_INVALID_ARGUMENT, "block_size must be a power of two in [4, 256] (got %d)", block_size);
-    if (sink < 0 || recent < 1)
-      return fail(PEEK_ERR_INVALID_ARGUMENT, "sink must be >= 0 and recent >= 1 (got %d, %d)", sink, recent);
-    peek_status s = check_table(d_block_table, max_blocks, table_stride, block_size);
-    if (s != PEEK_OK) return s;
-    if (n == 0) return PEEK_OK;
-    if (!d_context || !d_keep || !d_context_out || !d_num_freed)
-      return fail(PEEK_ERR_INVALID_ARGUMENT, "d_context, d_keep, d_context_out and d_num_freed must not be NULL");
-    if (max_blocks > 0 && (!d_mass || !d_table_out || !d_mass_out || !d_freed))
-      return fail(PEEK_ERR_INVALID_ARGUMENT, "d_mass, d_table_out, d_mass_out and d_freed must not be NULL");
-    const size_t row = (size_t)n * max_blocks * 4, in_row = ((size_t)(n - 1) * table_stride + max_blocks) * 4;
-    if (overlap(d_table_out, row, d_block_table, in_row) || overlap(d_freed, row, d_block_table, in_row) ||
-        overlap(d_mass_out, row * kv_heads, d_mass, row * kv_heads))
-      return fail(PEEK_ERR_INVALID_ARGUMENT, "the outputs must not overlap the table and the masses they are made from");
-    const size_t need = peek_kv_evict_workspace(n, kv_heads, max_blocks);
-    if (need > 0) {
-      if (!d_workspace) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_workspace is NULL");
-      if (workspace_bytes < need)
-        return fail(PEEK_ERR_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes, got %zu", need, workspace_bytes);
-      if ((reinterpret_cast<uintptr_t>(d_workspace) & 255) != 0)
-        return fail(PEEK_ERR_INVALID_ARGUMENT, "d_workspace must be 256-byte aligned");
-    }
-    hipStream_t st = (hipStream_t)stream;
-    s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, block_size, INT32_MAX,
-                    st);
-    if (s != PEEK_OK) return s;
-    const bool in_lds = max_blocks <= kEvictLdsKeys;
-    auto go = [&](auto kernel, int threads) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(threads), in_lds ? max_blocks * sizeof(uint32_t) : 0, st,
-                         kv_heads, __builtin_ctz((unsigned)block_size), d_context,
-                         Table{d_block_table, table_stride, max_blocks},
-                         d_mass, d_keep, sink, recent, d_context_out, d_table_out, d_mass_out, d_freed, d_num_freed,
-                         (uint32_t*)d_workspace, in_lds ? 1 : 0);
-    };
-    if (max_blocks > 1024) go(k_kv_evict<1024>, 1024);
-    else go(k_kv_evict<256>, 256);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "eviction launch failed: %s", hipGetErrorString(e));
     return PEEK_OK;
   });
 }

@@ -513,6 +513,11 @@ def test_evict(case, kind):
     run_evict(*EVICT[case], kind, seed=case)
 
 
+@pytest.mark.parametrize("kind", ["ties", "sparse", "odd"])
+def test_evict_of_wide_tables(kind):
+    run_evict([36000, 0, 33001, 8, 34500], 9, 4, [4000, 1, 8250, 1, 0], 3, 2, kind)
+
+
 def test_evict_of_a_row_of_a_million_tokens():
     run_evict([1000000, 5], 2, 4, [70000, 1], 1, 4, "plain")
 
