@@ -354,36 +354,38 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
 }
 
 // ------------------------------------------------------------------- join
-// Workgroups below `outs` join the chunks of four rows, a wavefront to a row
-// and a lane to a chunk for its weight; the others turn kept logarithms into
-// the weights of kThreads blocks of a (sequence, kv head).
+// Workgroups below `outs` join the chunks of rows, WAVES wavefronts to a row
+// (THREADS / 64 to all of them); the others turn kept logarithms into the weights
+// of THREADS blocks of a (sequence, kv head).
 
-template <int TYPE, int D>
-__global__ __launch_bounds__(kThreads) void k_decode_join(Decode a, uint32_t outs) {
+template <int TYPE, int D, int THREADS, int WAVES>
+__global__ __launch_bounds__(THREADS) void k_decode_join(Decode a, uint32_t outs) {
+  constexpr int kWaves = THREADS / kWave;
+  __shared__ float s_sum[WAVES > 1 ? WAVES * D : 1];
   const int32_t tid = threadIdx.x, q_heads = a.group * a.pool.heads, lb = a.pool.log_block;
   const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   if (blockIdx.x < outs) {
-    const int64_t at = (int64_t)blockIdx.x * kWaves + wave;
+    const int64_t at = (int64_t)blockIdx.x * (kWaves / WAVES) + wave / WAVES;
     if (at >= (int64_t)a.n * q_heads) return;
     const int32_t r = (int32_t)(at / q_heads), q_head = (int32_t)(at % q_heads);
     const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb), parts = (held + a.chunk - 1) / a.chunk;
     if (parts < 2) return;
     float l2;
-    uint16_t* out = a.out + (int64_t)r * a.out_token + q_head * a.out_head + lane * (D / kWave);
-    join_parts<TYPE, D>(a.part_out + at * a.splits * D, a.part_lse + at * a.splits, parts, lane, out, &l2);
-    if (a.lse && lane == 0) a.lse[at] = l2 * 0.69314718055994531f;
+    join_parts<TYPE, D, WAVES>(a.part_out + at * a.splits * D, a.part_lse + at * a.splits, parts, wave % WAVES, lane,
+                               s_sum, a.out + (int64_t)r * a.out_token + q_head * a.out_head, &l2);
+    if (a.lse && lane == 0 && wave % WAVES == 0) a.lse[at] = l2 * 0.69314718055994531f;
     return;
   }
   __shared__ float s_lse[kRows];
-  const int32_t width = a.table.width, spans = (width + kThreads - 1) / kThreads;
+  const int32_t width = a.table.width, spans = (width + THREADS - 1) / THREADS;
   const uint32_t unit = blockIdx.x - outs;
   const int32_t span = unit % spans, head = unit / spans % a.pool.heads, r = unit / spans / a.pool.heads;
   const int32_t held = kv::clip_tokens(a.context[r], width, lb), parts = (held + a.chunk - 1) / a.chunk;
-  const int32_t sub = 1 << (lb - a.log_grain), b = span * kThreads + tid;
+  const int32_t sub = 1 << (lb - a.log_grain), b = span * THREADS + tid;
   const int64_t mass_at = ((int64_t)r * a.pool.heads + head) * width + b;
   const int32_t grains = min(sub, (int32_t)(((int64_t)held + (1 << a.log_grain) - 1) >> a.log_grain) - b * sub);
   float w = 0.0f;
-  if (span * kThreads * (int64_t)sub << a.log_grain < held) {
+  if (span * THREADS * (int64_t)sub << a.log_grain < held) {
     for (int32_t tile = 0; tile < a.row_tiles; ++tile) {
       const int32_t rows = min(kRows, a.group - tile * kRows);
       __syncthreads();
@@ -411,6 +413,7 @@ struct Plan {
 
 // Tokens of a chunk: as many as leave about kGroups workgroups, from 256 on.
 constexpr int64_t kGroups = 8192;
+constexpr int32_t kManyParts = 32;
 
 Plan plan_for(const peek_kv_pool& pool, int32_t n, int32_t q_heads, int32_t max_blocks, bool with_mass) {
   Plan p{};
@@ -479,8 +482,10 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
     a.group = q_heads / a.pool.heads;
     a.row_tiles = (a.group + kRows - 1) / kRows;
     const int64_t groups = (int64_t)n * a.pool.heads * a.row_tiles * p.splits;
-    const int64_t outs = p.splits > 1 ? ((int64_t)n * q_heads + kWaves - 1) / kWaves : 0;
-    const int64_t masses = d_mass ? (int64_t)n * a.pool.heads * ((max_blocks + kThreads - 1) / kThreads) : 0;
+    const bool many = p.splits >= kManyParts;
+    const int32_t threads = many ? 1024 : kThreads, rows = many ? 1 : kWaves;      // of a joining workgroup
+    const int64_t outs = p.splits > 1 ? ((int64_t)n * q_heads + rows - 1) / rows : 0;
+    const int64_t masses = d_mass ? (int64_t)n * a.pool.heads * ((max_blocks + threads - 1) / threads) : 0;
     if (groups >= (1 << 24) || outs + masses >= (1 << 24))
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
     hipStream_t st = (hipStream_t)stream;
@@ -516,8 +521,10 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
     hipError_t err = hipGetLastError();
     if (err == hipSuccess && outs + masses > 0) {
       with_types(type, PEEK_TYPE_I8, pool->head_dim, [&](auto t, auto, auto d) {
-        hipLaunchKernelGGL((k_decode_join<t(), d()>), dim3((unsigned)(outs + masses)), dim3(kThreads), 0, st, a,
-                           (uint32_t)outs);
+        auto go = [&](auto kernel) {
+          hipLaunchKernelGGL(kernel, dim3((unsigned)(outs + masses)), dim3(threads), 0, st, a, (uint32_t)outs);
+        };
+        many ? go(k_decode_join<t(), d(), 1024, 16>) : go(k_decode_join<t(), d(), kThreads, 1>);
       });
       err = hipGetLastError();
     }

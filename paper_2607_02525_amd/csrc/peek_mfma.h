@@ -111,17 +111,21 @@ __device__ __forceinline__ float row_log_sum(const float* __restrict__ p, int32_
   return top + log2_fast(sum);
 }
 
-// A row's parts [parts][D] joined by a wavefront, a lane to each part for its
-// weight and to D / 64 elements (at `out`) for the sum.
-template <int TYPE, int D>
+// A row's parts [parts][D] joined by WAVES wavefronts of a workgroup, this one
+// the wave-th with its share of them: a lane to each part for its weight and to
+// D / 64 elements for the sum. `out` is the row's; s_sum, for WAVES > 1, has
+// WAVES * D floats.
+template <int TYPE, int D, int WAVES>
 __device__ __forceinline__ void join_parts(const float* __restrict__ part_out, const float* __restrict__ lse,
-                                           int32_t parts, int lane, uint16_t* out, float* log_sum) {
+                                           int32_t parts, int wave, int lane, float* s_sum, uint16_t* out,
+                                           float* log_sum) {
   constexpr int kEach = D / 64;
   const float l2 = row_log_sum(lse, parts, lane);
   float o[kEach] = {};
   const float* from = part_out + lane * kEach;
-  for (int32_t s0 = 0; s0 < parts; s0 += 64) {
-    const int32_t count = min(64, parts - s0);
+  const int32_t share = (parts + WAVES - 1) / WAVES, end = min(parts, (wave + 1) * share);
+  for (int32_t s0 = wave * share; s0 < end; s0 += 64) {
+    const int32_t count = min(64, end - s0);
     const float mine = lane < count ? exp2_fast(lse[s0 + lane] - l2) : 0.0f;
     for (int32_t s1 = 0; s1 < count; s1 += 8) {
 #pragma unroll
@@ -133,9 +137,22 @@ __device__ __forceinline__ void join_parts(const float* __restrict__ part_out, c
       }
     }
   }
-  if constexpr (kEach == 2) *(uint32_t*)out = pack2<TYPE>(o[0], o[1]);
-  else *out = kv::from_float<TYPE>(o[0]);
   *log_sum = l2;
+  if constexpr (WAVES == 1) {
+    if constexpr (kEach == 2) *(uint32_t*)(out + 2 * lane) = pack2<TYPE>(o[0], o[1]);
+    else out[lane] = kv::from_float<TYPE>(o[0]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) s_sum[wave * D + lane * kEach + e] = o[e];
+    __syncthreads();
+    const int d = wave * 64 + lane;
+    if (d < D) {
+      float x = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) x += s_sum[w * D + d];
+      out[d] = kv::from_float<TYPE>(x);
+    }
+  }
 }
 
 }  // namespace mm

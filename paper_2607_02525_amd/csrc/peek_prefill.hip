@@ -45,7 +45,8 @@ constexpr int kWaves = 8;
 constexpr int kThreads = kWave * kWaves;
 constexpr int kRows = 32 * kWaves;    // rows of a tile
 constexpr int kKeys = 64;             // keys of a tile
-constexpr int64_t kTargetGroups = 256;
+constexpr int64_t kTargetGroups = 256;   // of tiles in parts: 128 take 81 us where 256 take 50, 512 the same
+constexpr int32_t kCounted = kWave;   // sequences, at most, whose tiles are counted
 
 struct Prefill {
   Pool pool;
@@ -59,7 +60,8 @@ struct Prefill {
   float* part_out;                    // [rows][splits][D]: a part's sum of weight * value / its sum of weights
   float* part_lse;                    // [rows][splits]: base-2 logarithm of its sum of weights, -infinity for none
   int64_t num_tokens;
-  int32_t n, group, kv_heads, splits;
+  int32_t n, group, kv_heads;
+  int32_t splits;                     // room for parts of a row
   float scale;                        // of logits, in powers of two: >= 0
   uint32_t q_flip;                    // sign bits to flip in q, where the caller's scale is negative
   uint32_t q_mask;                    // 0 where the caller's scale is 0
@@ -285,6 +287,65 @@ struct Tile {
   }
 };
 
+// Tiles of sequence i's rows; 0 where its offsets are none.
+__device__ __forceinline__ uint32_t tiles_of(const Prefill& a, int32_t i) {
+  const int64_t first = a.offsets[i], end = min(a.num_tokens, a.offsets[i + 1]);
+  return first < 0 || end <= first ? 0u : (uint32_t)(((end - first) * a.group + kRows - 1) / kRows);
+}
+
+// Parts that every tile's keys are split into: as many as leave a workgroup to a compute unit.
+__device__ __forceinline__ int32_t parts_for(const Prefill& a, uint32_t tiles) {
+  const uint32_t groups = min(tiles, (uint32_t)kTargetGroups) * (uint32_t)a.kv_heads;
+  return max(1, min(a.splits, (int32_t)((uint32_t)kTargetGroups / max(1u, groups))));
+}
+
+// A workgroup's tile: of sequence r, from row row0 on, its part of the keys.
+struct Work {
+  int32_t r, split, parts;
+  int64_t row0;
+};
+
+// Tiles of up to kCounted sequences: *mine is lane i's sequence's, the result those of the first to the i-th.
+__device__ __forceinline__ uint32_t count_tiles(const Prefill& a, int lane, uint32_t* mine) {
+  uint32_t sum = *mine = lane < a.n ? tiles_of(a, lane) : 0u;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const uint32_t x = __shfl_up(sum, d);
+    if (lane >= d) sum += x;
+  }
+  return sum;
+}
+
+// Work `unit` from the end: the last rows of the last sequences come first, they
+// have the most keys. Up to kCounted sequences the tiles are counted, so that
+// workgroups without work are the last ones: among the others, dealt out in turn over the
+// shader engines, they left some of these with twice the work of others (16
+// prompts of one tile each after 8000 tokens 259 -> 186 us, 64 chats 364 -> 353).
+// More sequences would cost each workgroup more than that saves (250 short prompts 230
+// -> 241 us, 1000 0.90 -> 1.28 ms): they have a slot for each tile and one
+// more, numbered without counting, sequence r's from offsets[r] * group / kRows + r on.
+__device__ __forceinline__ bool find_work(const Prefill& a, uint32_t unit, uint32_t units, int lane, Work* w) {
+  if (a.n > kCounted) {
+    const int64_t slot = units - 1 - unit;
+    w->r = kv::last_at_most(a.n, slot, lane, [&](int32_t i) { return a.offsets[i] * a.group / kRows + i; });
+    w->row0 = (slot - (a.offsets[w->r] * a.group / kRows + w->r)) * kRows;
+    w->split = 0;
+    w->parts = 1;
+    return true;
+  }
+  uint32_t mine;
+  const uint32_t sum = count_tiles(a, lane, &mine), tiles = __builtin_amdgcn_readlane(sum, kWave - 1);
+  w->parts = parts_for(a, tiles);
+  if (unit >= tiles * (uint32_t)w->parts) return false;
+  const uint32_t from_first = tiles * w->parts - 1 - unit, slot = from_first / w->parts;
+  w->split = from_first % w->parts;
+  const uint64_t past = __ballot(sum > slot);
+  if (past == 0) return false;
+  w->r = __builtin_ctzll(past);
+  w->row0 = (int64_t)(slot - (uint32_t)__builtin_amdgcn_readlane(sum - mine, w->r)) * kRows;
+  return true;
+}
+
 template <int TYPE, int FMT, int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_prefill(Prefill a) {
   using T = Tile<TYPE, FMT, D>;
@@ -294,24 +355,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   __shared__ uint32_t s_odd;
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  // kv heads side by side (each on XCDs of its own where there are eight), the
-  // last rows of the last sequences first: they have the most keys
+  // kv heads side by side: each on XCDs of its own where there are eight
   const int32_t head = blockIdx.x % a.kv_heads;
-  const uint32_t unit = (gridDim.x - 1 - blockIdx.x) / a.kv_heads;
-  const int32_t split = unit % a.splits;
-  const int64_t slot = unit / a.splits;
-  // the last sequence r with offsets[r] * group / kRows + r <= slot: every
-  // sequence has a slot for each of its tiles, some one more
-  const int32_t r = kv::last_at_most(a.n, slot, lane, [&](int32_t i) { return a.offsets[i] * a.group / kRows + i; });
-  const int64_t first = a.offsets[r], end = min(a.num_tokens, a.offsets[r + 1]);
-  const int64_t row0 = (slot - (first * a.group / kRows + r)) * kRows;
+  Work w;
+  if (!find_work(a, blockIdx.x / a.kv_heads, gridDim.x / a.kv_heads, lane, &w)) return;
+  const int32_t r = __builtin_amdgcn_readfirstlane(w.r), split = w.split;
+  const int64_t row0 = w.row0, first = a.offsets[r], end = min(a.num_tokens, a.offsets[r + 1]);
   if (first < 0 || end <= first || row0 < 0 || row0 >= (end - first) * a.group) return;
   const int64_t rows = (end - first) * a.group;
   const int32_t held = a.prefix ? kv::clip_tokens(a.prefix[r], a.table.width, a.pool.log_block) : 0;
   const int32_t cached = (held + kKeys - 1) / kKeys;
   const int32_t last_row_token = (int32_t)((min(row0 + kRows, rows) - 1) / a.group);
   // this part's tiles of all (the cached ones, then the sequence's own)
-  const int32_t all_tiles = cached + last_row_token / kKeys + 1, each = (all_tiles + a.splits - 1) / a.splits;
+  const int32_t all_tiles = cached + last_row_token / kKeys + 1, each = (all_tiles + w.parts - 1) / w.parts;
   const int32_t tile0 = min(split * each, all_tiles), tiles = min(tile0 + each, all_tiles);
 
   // this lane's row
@@ -372,7 +428,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   float scale_k = 1.0f, scale_v = 1.0f;
   int32_t page = 0;      // as the table has it: looked at only when it is used, a tile later
   const int32_t unit_key = (tid % (kKeys * (D / 16))) / (D / 16), unit_at = tid % (D / 16);
-  const bool leads = tid < kKeys * (D / 16) && unit_at == 0 && (unit_key & 3) == 0;     // four keys: fetches their scales
+  const bool leads = tid < kKeys * (D / 16) && unit_at == 0 && (unit_key & 3) == 0;   // fetches four keys' scales
   const uint32_t half_bytes = ((uint32_t)a.pool.heads << a.pool.log_block) * D;         // a page's keys, or values
   const uint8_t* head_pages = a.pool.pages + ((int64_t)head << a.pool.log_block) * D;
   const int32_t* ids = a.table.ids + (int64_t)r * a.table.stride;
@@ -467,7 +523,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (!active || wave_row + col >= rows) return;
   const float sum = sum_halves(tile.sum);
   const int64_t out_row = (first + token) * a.kv_heads * a.group + q_head;
-  if (a.splits > 1) {
+  if (w.parts > 1) {
     const bool none = sum == 0.0f;      // this part has no key that the row sees
     const float over = none ? 0.0f : 1.0f / sum;
     float* out = a.part_out + (out_row * a.splits + split) * D + half * 4;
@@ -476,7 +532,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const f16& x = tile.acc[p];
-        *(f4*)(out + 32 * p + 8 * e) = (f4){x[4 * e] * over, x[4 * e + 1] * over, x[4 * e + 2] * over, x[4 * e + 3] * over};
+        *(f4*)(out + 32 * p + 8 * e) =
+            (f4){x[4 * e] * over, x[4 * e + 1] * over, x[4 * e + 2] * over, x[4 * e + 3] * over};
       }
     if (half == 0) a.part_lse[out_row * a.splits + split] = none ? -__builtin_inff() : tile.top + log2_fast(sum);
     return;
@@ -501,25 +558,37 @@ __global__ __launch_bounds__(256) void k_prefill_join(Prefill a) {
   const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int64_t token = row / q_heads;
   if (token >= a.num_tokens) return;
+  uint32_t mine;
+  const uint32_t tiles = __builtin_amdgcn_readlane(count_tiles(a, lane, &mine), kWave - 1);
+  const int32_t parts = parts_for(a, tiles);
+  if (parts < 2) return;
   const int32_t q_head = (int32_t)(row - token * q_heads);
   const int32_t r = kv::last_at_most(a.n, token, lane, [&](int32_t i) { return a.offsets[i]; });
   if (a.offsets[r] > token || token >= a.offsets[r + 1]) return;
   float l2;
-  uint16_t* out = a.out + token * a.out_token + q_head * a.out_head + lane * (D / kWave);
-  join_parts<TYPE, D>(a.part_out + row * a.splits * D, a.part_lse + row * a.splits, a.splits, lane, out, &l2);
+  join_parts<TYPE, D, 1>(a.part_out + row * a.splits * D, a.part_lse + row * a.splits, parts, 0, lane, nullptr,
+                         a.out + token * a.out_token + q_head * a.out_head, &l2);
   if (a.lse && lane == 0) a.lse[row] = l2 * 0.69314718055994531f;
 }
 
-// Parts of a tile's keys, where there are too few tiles for the device's 256
-// compute units: about one workgroup each, and eight tiles of keys at least, as a
-// part costs each row 2 KB of traffic.
-int32_t splits_for(int64_t groups, int64_t num_tokens, int64_t max_context) {
-  const int64_t tiles = (max_context + num_tokens + kKeys - 1) / kKeys;
-  return (int32_t)std::max<int64_t>(1, std::min(kTargetGroups / std::max<int64_t>(1, groups), tiles / 8));
+// Tiles of rows, for all kv heads: no fewer and no more than these.
+int64_t least_groups(int64_t num_tokens, int32_t q_heads, int32_t kv_heads) {
+  return (num_tokens * (q_heads / kv_heads) + kRows - 1) / kRows * kv_heads;
+}
+int64_t most_groups(int32_t n, int64_t num_tokens, int32_t q_heads, int32_t kv_heads) {
+  return (num_tokens * (q_heads / kv_heads) / kRows + n) * kv_heads;
 }
 
-int64_t groups_for(int32_t n, int64_t num_tokens, int32_t q_heads, int32_t kv_heads) {
-  return (num_tokens * (q_heads / kv_heads) / kRows + n) * kv_heads;
+// Room for parts of a tile's keys, where there may be fewer tiles than the
+// device's 256 compute units (one agent's turn of 37 tokens after 23552: 49 us, with
+// no parts 490). A part has two tiles of the longest prefix at least (a turn after 800
+// tokens 15.5 us, with eight tiles a part 27), or eight of own tokens, of which
+// a row sees half (700 tokens alone 25 us, in parts of two 27.5).
+int32_t splits_for(int32_t n, int64_t num_tokens, int32_t q_heads, int32_t kv_heads, int64_t max_context) {
+  if (n > kCounted) return 1;
+  const int64_t groups = std::max<int64_t>(1, least_groups(num_tokens, q_heads, kv_heads));
+  const int64_t parts = max_context / (2 * kKeys) + num_tokens / (8 * kKeys);
+  return (int32_t)std::max<int64_t>(1, std::min(kTargetGroups / groups, parts));
 }
 
 }  // namespace
@@ -534,7 +603,7 @@ size_t peek_prefill_attention_workspace(int32_t n, int64_t num_tokens, int32_t q
   if (n < 1 || num_tokens < 1 || kv_heads < 1 || q_heads < kv_heads || (head_dim != 64 && head_dim != 128) ||
       max_context < 0 || num_tokens >= ((int64_t)1 << 40))
     return 0;
-  const int32_t splits = splits_for(groups_for(n, num_tokens, q_heads, kv_heads), num_tokens, max_context);
+  const int32_t splits = splits_for(n, num_tokens, q_heads, kv_heads, max_context);
   if (splits < 2) return 0;
   return ((size_t)num_tokens * q_heads * splits * (head_dim + 1) * sizeof(float) + 255) & ~(size_t)255;
 }
@@ -584,10 +653,12 @@ peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t 
                         peek_prefill_attention_workspace(n, num_tokens, q_heads, kv_heads, head_dim, context));
     if (s != PEEK_OK) return s;
     const int32_t group = q_heads / kv_heads;
-    const int64_t tiles = num_tokens < ((int64_t)1 << 40) ? groups_for(n, num_tokens, q_heads, kv_heads) : INT64_MAX;
+    const int64_t tiles = num_tokens < ((int64_t)1 << 40) ? most_groups(n, num_tokens, q_heads, kv_heads) : INT64_MAX;
     if (tiles >= (1 << 22))
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many rows for one call (%lld)", (long long)num_tokens);
-    a.splits = splits_for(tiles, num_tokens, context);
+    a.splits = splits_for(n, num_tokens, q_heads, kv_heads, context);
+    // in parts there are kTargetGroups workgroups at most
+    const int64_t groups = std::max(tiles, std::min(tiles * a.splits, kTargetGroups));
     hipStream_t st = (hipStream_t)stream;
     s = validate_kv(n, d_offsets, num_tokens, d_prefix, false, d_block_table, max_blocks, table_stride,
                     pool ? pool->block_size : 4, pool ? pool->num_pages : 0, st);
@@ -610,10 +681,10 @@ peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t 
     a.part_out = (float*)d_workspace;
     a.part_lse = a.part_out + num_tokens * q_heads * a.splits * head_dim;
     with_types(type, pool ? pool->type : PEEK_TYPE_F8E4M3, head_dim, [&](auto t, auto m, auto d) {
-      hipLaunchKernelGGL((k_prefill<t(), m(), d()>), dim3((unsigned)(tiles * a.splits)), dim3(kThreads), 0, st, a);
+      hipLaunchKernelGGL((k_prefill<t(), m(), d()>), dim3((unsigned)groups), dim3(kThreads), 0, st, a);
       if (a.splits > 1)
-        hipLaunchKernelGGL((k_prefill_join<t(), d()>), dim3((unsigned)((num_tokens * q_heads + 3) / 4)), dim3(256), 0, st,
-                           a);
+        hipLaunchKernelGGL((k_prefill_join<t(), d()>), dim3((unsigned)((num_tokens * q_heads + 3) / 4)), dim3(256), 0,
+                           st, a);
     });
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return fail(PEEK_ERR_DEVICE, "prefill launch failed: %s", hipGetErrorString(err));

@@ -217,6 +217,8 @@ PREFILL = [
     ([(0, 0), (16, 0)], 1, 4, 16, 128, BF, F8),
     ([(0, 2100)], 1, 1, 16, 64, BF, F8),       # few tiles: keys in parts, of which early rows see one
     ([(1500, 600), (0, 40)], 1, 2, 16, 128, HF, F8),
+    ([(0, 0), (6000, 3), (0, 0), (500, 9), (0, 1), (2300, 260), (0, 0)], 2, 2, 16, 128, BF, I8),
+    ([(48 * i, i % 3) for i in range(64)], 1, 4, 16, 64, BF, F8),
 ]
 
 
