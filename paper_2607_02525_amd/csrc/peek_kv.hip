@@ -23,10 +23,12 @@ constexpr int kWave = 64;
 // sequence's last block has nothing to do.
 //
 // Bound by memory: 16-byte loads of eight elements, which stay in registers
-// from the maximum to the rounding up to kHeld of them a lane (blocks of 16
-// tokens of 128); larger blocks are read again, from L2.
-
-constexpr int kHeld = 4;
+// from the maximum to the rounding up to HELD of them a lane, as many as a block has,
+// 16 at most; larger blocks are read again, from L2. Measured, 72000 tokens of 8 heads
+// of 128, 439 MB: 91 to 98 us, 4.5 to 4.8 TB/s, in blocks of 16 tokens (a large copy
+// reaches 4.95); of 32 87 us (104 with four a lane), of 64 99 (116), of 256 137 (158);
+// blocks of 16 with eight a lane 107. 64 single tokens 5.3 us: the waits for
+// offsets, page id, old scale and codes, one after the other.
 
 __device__ __forceinline__ float wave_max(float x) {
   for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
@@ -92,7 +94,7 @@ __device__ __forceinline__ void spread8(const u4 w, float* x) {
   }
 }
 
-template <int TYPE, int FMT, int D>
+template <int TYPE, int FMT, int D, int HELD>
 __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, int32_t n, int64_t num_tokens,
                                                    const int64_t* __restrict__ offsets,
                                                    const int32_t* __restrict__ context, Table table, int64_t slots) {
@@ -122,20 +124,20 @@ __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, in
   uint8_t* codes = pool.pages + (at << lb) * D;
   const float held = old > 0 ? pool.scales[at] : 0.0f;
 
-  u4 w[kHeld];
+  u4 w[HELD];
   auto load = [&](int32_t p0) {
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
+    for (int i = 0; i < HELD; ++i) {
       const int32_t p = p0 + i * kWave + lane;
       w[i] = p < pieces ? *(const u4*)(x + (int64_t)(p / kPieces) * src.token + p % kPieces * 8) : (u4){};
     }
   };
   float most = 0.0f;
   bool plain = true;
-  for (int32_t p0 = 0; p0 < pieces; p0 += kHeld * kWave) {
+  for (int32_t p0 = 0; p0 < pieces; p0 += HELD * kWave) {
     load(p0);
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
+    for (int i = 0; i < HELD; ++i) {
       float y[8];
       spread8<TYPE>(w[i], y);
 #pragma unroll
@@ -165,10 +167,10 @@ __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, in
       *(u2*)(codes + p * 8) = c;
     }
   }
-  for (int32_t p0 = 0; p0 < pieces; p0 += kHeld * kWave) {
-    if (pieces > kHeld * kWave) load(p0);
+  for (int32_t p0 = 0; p0 < pieces; p0 += HELD * kWave) {
+    if (pieces > HELD * kWave) load(p0);
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
+    for (int i = 0; i < HELD; ++i) {
       const int32_t p = p0 + i * kWave + lane;
       if (p < pieces) {
         float y[8];
@@ -338,7 +340,12 @@ peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_toke
       hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, st, p, k, v, n, num_tokens, d_offsets, d_context,
                          t, slots);
     };
-    with_types(type, pool->type, pool->head_dim, [&](auto e, auto f, auto d) { go(k_kv_append<e(), f(), d()>); });
+    with_types(type, pool->type, pool->head_dim, [&](auto e, auto f, auto d) {
+      const int32_t pieces = pool->block_size * d() / 8;      // of a block, K or V
+      if (pieces <= 4 * kWave) go(k_kv_append<e(), f(), d(), 4>);
+      else if (pieces <= 8 * kWave) go(k_kv_append<e(), f(), d(), 8>);
+      else go(k_kv_append<e(), f(), d(), 16>);
+    });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "append launch failed: %s", hipGetErrorString(e));
     return PEEK_OK;
