@@ -24,6 +24,12 @@
 // that is smaller) is kept as a logarithm, which needs no maximum to go with
 // it; the second kernel sums them over the rows once the rows' sums are known.
 // They take 4 bytes a row and 16 tokens, of the 4 KB that the tokens take.
+//
+// Measured: 192 sequences of 2000 to 24000 tokens, 8 kv heads of 128, int8, 5.5 GB:
+// 0.95 to 0.99 ms, 5.6 to 5.8 TB/s (a streaming read of memory reaches 6.3);
+// 64 sequences of up to 7400 tokens with weights, 0.56 GB: 115 us and 9 for the
+// second kernel; one of 5117 tokens: 5.4 us and 4.2, its page ids', scales' and
+// pages' waits one after the other.
 #include <algorithm>
 
 #include "peek_internal.h"
@@ -100,7 +106,8 @@ __device__ __forceinline__ void turn4(const uint32_t a, const uint32_t b, const 
 // WIDE: blocks of 16 tokens or more. Sixteen tokens that start at a multiple
 // of 16 then lie in one block, whose page and scales are the same for the whole
 // wavefront and come by scalar loads; smaller blocks are looked up by every
-// lane in LDS.
+// lane in LDS. (Blocks of 16 looked up in LDS: 64 sequences of 4000 tokens 112 us
+// where these take 106, one of 130000 24.0 where these take 21.7.)
 template <int TYPE, int FMT, int D, bool MASS, bool WIDE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ? 4 : 3))) void k_decode(Decode a) {
   constexpr int kSteps = D / 32;        // products of keys and queries a 16-token half
@@ -356,7 +363,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
 // ------------------------------------------------------------------- join
 // Workgroups below `outs` join the chunks of rows, WAVES wavefronts to a row
 // (THREADS / 64 to all of them); the others turn kept logarithms into the weights
-// of THREADS blocks of a (sequence, kv head).
+// of THREADS blocks of a (sequence, kv head). Bound by its waits: 4.2 us for one
+// sequence's 40 rows of 20 parts, 11 us for 192 sequences of 64 rows. A row of kManyParts
+// parts or more has 16 wavefronts: 390 parts of 96 rows 127 us for both kernels
+// instead of 140, 508 of 8 rows 22 instead of 46; of few parts they cost more
+// than they save (64 sequences of 8 parts 119 us instead of 106).
 
 template <int TYPE, int D, int THREADS, int WAVES>
 __global__ __launch_bounds__(THREADS) void k_decode_join(Decode a, uint32_t outs) {
@@ -411,7 +422,12 @@ struct Plan {
   size_t part_out, part_lse, weights, bytes;    // offsets into the workspace, and its size
 };
 
-// Tokens of a chunk: as many as leave about kGroups workgroups, from 256 on.
+// Tokens of a chunk: as many as leave about kGroups workgroups, from 256 on up to
+// kMaxChunk. Fewer workgroups leave compute units idle at the end where lengths differ
+// (64 sequences of 1100 to 7400 tokens with weights: 8192 124 us, 4096 135, 2048
+// 152), more have more parts to join (three sequences of 100000: 16384 137 us, 8192
+// 127, 4096 123). Chunks of 1024 at most cost the largest batches 7% (192 sequences of up
+// to 24000 tokens 1.06 ms instead of 0.99).
 constexpr int64_t kGroups = 8192;
 constexpr int32_t kManyParts = 32;
 
