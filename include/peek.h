@@ -13,6 +13,10 @@
  * being the cluster size) and the per-cache-node pending demand read by the
  * eviction score (Eq. 2).
  *
+ * What the hit is for follows at the end of this header: the K and V of
+ * cached tokens in 8-bit pages, attention that reads them, and the eviction
+ * of a sequence's blocks by the attention weight they get.
+ *
  * Conventions for every call:
  *  - Plain C ABI; no exceptions cross it; nothing aborts the process.
  *  - Errors return a negative peek_status; peek_last_error() then describes
@@ -34,7 +38,9 @@
  *    inputs on the device (offsets non-decreasing from >= 0, prompt lengths
  *    < 2^31, last nodes inside the cache, match lengths inside their
  *    prompts) and return INVALID_ARGUMENT before any other work if one
- *    fails. The check adds a small allocation, a launch and a stream
+ *    fails; so do peek_kv_append, peek_prefill_attention,
+ *    peek_decode_attention and peek_kv_evict (offsets, lengths, page ids).
+ *    The check adds a small allocation, a launch and a stream
  *    synchronization per call, so it is not for use under graph capture.
  */
 #ifndef PEEK_H

@@ -28,8 +28,8 @@
 // Bound, over own tokens, by the matrix cores and the power they draw: 5 prompts of
 // up to 24000 tokens, 32 query heads of 128, 4.98 TFLOP: 4.37 to 4.5 ms, 1.1
 // PFLOP/s (a library product of 8192^3 reaches 1.24), the clock held at 1.8 to 1.9 GHz.
-// Over cached tokens by the vector instructions that widen the codes, 9.5 to each
-// matrix instruction (two of which take as long as one of it), and by the last workgroups:
+// Over cached tokens by the vector instructions, which widen the codes too (8.5 to each
+// matrix instruction, four cycles each to its 32), and by the last workgroups:
 // 64 queries of up to 256 tokens after up to 7168, 40 query heads, 1.07 TFLOP:
 // 1.38 ms, 770 TFLOP/s. Few rows by the 2 us that 64 keys take a workgroup.
 // With 128 rows to a workgroup, two to a compute unit, tiles are loaded twice as
@@ -562,8 +562,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (a.lse && half == 0) a.lse[out_row] = (tile.top + log2_fast(sum)) * 0.69314718055994531f;
 }
 
-// Joins the parts of four rows, a wavefront to a row: 5 us for 296 rows of 32
-// parts, most of it waits (four wavefronts to a row take as long). Rows of no sequence are left alone.
+// Joins the parts of four rows, a wavefront to a row: 5 us for 37 tokens of 64
+// heads in 16 parts, most of it waits (four wavefronts to a row take as long).
+// Rows of no sequence are left alone.
 template <int TYPE, int D>
 __global__ __launch_bounds__(256) void k_prefill_join(Prefill a) {
   const int lane = threadIdx.x & (kWave - 1), q_heads = a.kv_heads * a.group;
