@@ -473,9 +473,11 @@ def _table(t, n: int):
     width = t.shape[1]
     if width > 1 and t.stride(1) != 1:
         raise ValueError("block_table's rows must be contiguous")
+    if n > 1 and width > 0 and t.stride(0) < width:      # (one row expanded to all sequences, for one)
+        raise ValueError("block_table's rows must not overlap")
     if not t.is_cuda:
         raise ValueError("block_table must be a device tensor")
-    return t.data_ptr(), width, max(t.stride(0), width) if n > 1 else width
+    return t.data_ptr(), width, t.stride(0) if n > 1 and width > 0 else width
 
 
 def _ws(workspace):
