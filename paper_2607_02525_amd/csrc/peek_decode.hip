@@ -92,6 +92,11 @@ __device__ __forceinline__ float swap16_sum(float x) {
   return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
 
+// Chunks of a sequence (lengths up to 2^31 - 1).
+__device__ __forceinline__ int32_t parts_of(int32_t tokens, int32_t chunk) {
+  return tokens > 0 ? (tokens - 1) / chunk + 1 : 0;
+}
+
 // Four tokens of four bytes each -> four bytes' worth of four tokens.
 __device__ __forceinline__ void turn4(const uint32_t a, const uint32_t b, const uint32_t c, const uint32_t d,
                                       uint32_t* r) {
@@ -126,7 +131,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
   const int32_t split = unit % a.splits, r = unit / a.splits;
   const int32_t q_heads = a.group * a.pool.heads, lb = a.pool.log_block;
   const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb);
-  const int32_t from = split * a.chunk, to = min(held, from + a.chunk);
+  const int32_t from = split * a.chunk, to = from + min(a.chunk, held - from);   // (no sum passes `held`, nor 2^31)
   const int32_t row = row_tile * kRows + (lane & 15), rows = min(kRows, a.group - row_tile * kRows);
   if (from >= to) {
     if (split == 0) {        // no tokens at all
@@ -231,7 +236,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
     }
   };
   // One tile; the next one's keys are fetched as soon as this one's are used, then its values.
-  auto step = [&](int32_t t0, int32_t next) {
+  auto step = [&](int32_t t0) {
+    const bool more = to - t0 > kWaves * kTile;
+    const int32_t next = more ? t0 + kWaves * kTile : 0;
     f4 s[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -253,11 +260,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[h][e] = fmaf(s[h][e], scale[h], log_v[h]);
-    if (next < to) {
+    if (more) {
       place(next);
       load_keys(next);
     }
-    if (t0 + kTile > to) {
+    if (to - t0 < kTile) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -303,20 +310,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
         acc[4 * p + e] = mul16<TYPE>((u4){y[0], y[1], z[0], z[1]}, w, acc[4 * p + e]);
       }
     }
-    if (next < to) load_values(next);
+    if (more) load_values(next);
   };
 
   {
-    int32_t t = from + wave * kTile;
-    if (t < to) {
-      place(t);
-      load_keys(t);
-      load_values(t);
+    const int32_t mine = to - from - wave * kTile;      // tokens from this wavefront's first one on
+    if (mine > 0) {
+      place(to - mine);
+      load_keys(to - mine);
+      load_values(to - mine);
     }
-    while (t < to) {
-      step(t, t + kWaves * kTile);
-      t += kWaves * kTile;
-    }
+    for (int32_t left = mine; left > 0; left -= kWaves * kTile) step(to - left);
   }
 
   // the wavefronts' results, joined: acc register v of part p is row col, element (4 grp + v) kParts + p
@@ -379,7 +383,7 @@ __global__ __launch_bounds__(THREADS) void k_decode_join(Decode a, uint32_t outs
     const int64_t at = (int64_t)blockIdx.x * (kWaves / WAVES) + wave / WAVES;
     if (at >= (int64_t)a.n * q_heads) return;
     const int32_t r = (int32_t)(at / q_heads), q_head = (int32_t)(at % q_heads);
-    const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb), parts = (held + a.chunk - 1) / a.chunk;
+    const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb), parts = parts_of(held, a.chunk);
     if (parts < 2) return;
     float l2;
     join_parts<TYPE, D, WAVES>(a.part_out + at * a.splits * D, a.part_lse + at * a.splits, parts, wave % WAVES, lane,
@@ -391,7 +395,7 @@ __global__ __launch_bounds__(THREADS) void k_decode_join(Decode a, uint32_t outs
   const int32_t width = a.table.width, spans = (width + THREADS - 1) / THREADS;
   const uint32_t unit = blockIdx.x - outs;
   const int32_t span = unit % spans, head = unit / spans % a.pool.heads, r = unit / spans / a.pool.heads;
-  const int32_t held = kv::clip_tokens(a.context[r], width, lb), parts = (held + a.chunk - 1) / a.chunk;
+  const int32_t held = kv::clip_tokens(a.context[r], width, lb), parts = parts_of(held, a.chunk);
   const int32_t sub = 1 << (lb - a.log_grain), b = span * THREADS + tid;
   const int64_t mass_at = ((int64_t)r * a.pool.heads + head) * width + b;
   const int32_t grains = min(sub, (int32_t)(((int64_t)held + (1 << a.log_grain) - 1) >> a.log_grain) - b * sub);

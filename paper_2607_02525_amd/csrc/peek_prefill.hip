@@ -375,7 +375,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (first < 0 || end <= first || row0 < 0 || row0 >= (end - first) * a.group) return;
   const int64_t rows = (end - first) * a.group;
   const int32_t held = a.prefix ? kv::clip_tokens(a.prefix[r], a.table.width, a.pool.log_block) : 0;
-  const int32_t cached = (held + kKeys - 1) / kKeys;
+  const int32_t cached = (int32_t)(((uint32_t)held + kKeys - 1) / kKeys);
   const int32_t last_row_token = (int32_t)((min(row0 + kRows, rows) - 1) / a.group);
   // this part's tiles of all (the cached ones, then the sequence's own)
   const int32_t all_tiles = cached + last_row_token / kKeys + 1, each = (all_tiles + w.parts - 1) / w.parts;
