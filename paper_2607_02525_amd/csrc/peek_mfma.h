@@ -129,11 +129,14 @@ __device__ __forceinline__ void join_parts(const float* __restrict__ part_out, c
     const float mine = lane < count ? exp2_fast(lse[s0 + lane] - l2) : 0.0f;
     for (int32_t s1 = 0; s1 < count; s1 += 8) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {      // those past the last have weight 0, and read the last again
+      for (int i = 0; i < 8; ++i) {      // those past the last read the last again, as 0 (it may be infinite)
         const int32_t s = s1 + i;
         const float part = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, mine), s));
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) o[e] = fmaf(part, from[(int64_t)(s0 + min(s, count - 1)) * D + e], o[e]);
+        for (int e = 0; e < kEach; ++e) {
+          const float x = from[(int64_t)(s0 + min(s, count - 1)) * D + e];
+          o[e] = fmaf(part, s < count ? x : 0.0f, o[e]);
+        }
       }
     }
   }
