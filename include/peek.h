@@ -39,7 +39,8 @@
  *    < 2^31, last nodes inside the cache, match lengths inside their
  *    prompts) and return INVALID_ARGUMENT before any other work if one
  *    fails; so do peek_kv_append, peek_prefill_attention,
- *    peek_decode_attention and peek_kv_evict (offsets, lengths, page ids).
+ *    peek_decode_attention and peek_kv_evict (offsets, lengths, page ids,
+ *    scales).
  *    The check adds a small allocation, a launch and a stream
  *    synchronization per call, so it is not for use under graph capture.
  */
@@ -358,7 +359,10 @@ peek_status peek_offline_order(int32_t n, const int32_t* d_tokens, const int64_t
  *
  * Pool: pages[num_pages][2][kv_heads][block_size][head_dim] of 8-bit codes
  * (K at 0, V at 1), scales[num_pages][2][kv_heads] float32. A value is its
- * code times its scale. Formats: PEEK_TYPE_F8E4M3 (OCP e4m3) and
+ * code times its scale. Scales of keys are finite, those of values 0 to 2^60, of
+ * which smaller ones than 2^-60 (0 among them) count as 2^-60; peek_kv_append
+ * leaves 2^-60 to 2^60 and asks for 0 to 2^60 of a block that it adds to
+ * (PEEK_VALIDATE reports others). Formats: PEEK_TYPE_F8E4M3 (OCP e4m3) and
  * PEEK_TYPE_I8. block_size is a power of two in [4, 256], as of a block
  * table; head_dim is 64 or 128; kv_heads is in [1, 1024].
  *
@@ -383,7 +387,7 @@ peek_status peek_offline_order(int32_t n, const int32_t* d_tokens, const int64_t
  * it); memory outside the pool is not touched: peek_kv_append leaves such a
  * block out, attention reads page 0 in its place. Lengths beyond the table
  * (max_blocks * block_size tokens) and negative ones are cut to it.
- * PEEK_VALIDATE checks offsets, lengths and page ids of these calls.
+ * PEEK_VALIDATE checks offsets, lengths, page ids and scales of these calls.
  * ---------------------------------------------------------------------- */
 typedef enum peek_type {
   PEEK_TYPE_BF16 = 0,

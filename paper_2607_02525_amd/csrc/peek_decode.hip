@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
     for (int32_t i = tid; i < blocks; i += kThreads) {
       const uint32_t page = kv::page_of(a.table, a.pool, r, block0 + i);
       const int64_t at = (int64_t)page * 2 * a.pool.heads + head;
-      const float k = a.pool.scales[at], v = a.pool.scales[at + a.pool.heads];
+      const float k = a.pool.scales[at], v = kv::value_scale(a.pool.scales[at + a.pool.heads]);
       s_block[i] = Block{k * a.scale, log2_fast(v), __builtin_amdgcn_rcpf(v), page};
     }
   }
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
         const int64_t at = (int64_t)page * 2 * a.pool.heads + head;
         base[h] = a.pool.pages + ((at << lb) + (t & ((1 << lb) - 1))) * D;
         limit[h] = to - 1 - t;
-        const float v = scales[at + a.pool.heads];
+        const float v = kv::value_scale(scales[at + a.pool.heads]);
         scale[h] = scales[at] * a.scale;
         log_v[h] = log2_fast(v);
         inv_v[h] = __builtin_amdgcn_rcpf(v);
@@ -510,7 +510,7 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
     hipStream_t st = (hipStream_t)stream;
     s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, pool->block_size,
-                    pool->num_pages, st);
+                    &a.pool, st);
     if (s != PEEK_OK) return s;
     char* ws = (char*)d_workspace;
     a.q = Rows{d_q, q_token_stride, q_head_stride};

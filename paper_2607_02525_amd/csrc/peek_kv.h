@@ -13,10 +13,14 @@
 namespace peek {
 namespace kv {
 
-// Scales stay within 2^-60 .. 2^60: their reciprocals and logarithms are then
-// ordinary floats, and a weight times a scale cannot leave float32's range.
+// Appended scales stay within 2^-60 .. 2^60, and attention brings V's there (a
+// pool may come with others, 0 among them): their reciprocals and logarithms are
+// then ordinary floats, and a weight times a scale cannot leave float32's range.
 constexpr float kScaleMin = 0x1p-60f;
 constexpr float kScaleMax = 0x1p60f;
+__device__ __forceinline__ float value_scale(float s) {     // (NaN stays)
+  return s < kScaleMin ? kScaleMin : s > kScaleMax ? kScaleMax : s;
+}
 
 // A pool as kernels see it.
 struct Pool {
@@ -110,7 +114,8 @@ peek_status check_workspace(const void* d_workspace, size_t bytes, size_t need);
 
 // A caller's scale as the kernels take it: a factor >= 0 of base-2 logits, and
 // what to do to q's bits so that it is one. With a factor of at least 2^-100,
-// a masked logit of -infinity stays one.
+// a masked logit of -infinity stays one (own keys: a cached key's own scale may be
+// anything, and is applied before the mask).
 inline void set_scale(float scale, float* factor, uint32_t* q_flip, uint32_t* q_mask) {
   const float f = std::fabs(scale) * 1.44269504088896341f;
   const bool none = f < 0x1p-100f;
@@ -136,9 +141,10 @@ void with_types(int32_t type, int32_t format, int32_t dim, F&& f) {
 
 // With PEEK_VALIDATE: offsets (nullable) non-decreasing within num_tokens,
 // lengths within the table, the pages that they reach (with the new tokens,
-// where `appends`) inside the pool. Waits for `st`. PEEK_OK when off.
+// where `appends`) inside the pool, and where `pool` is given the scales of the
+// blocks that hold tokens within their range. Waits for `st`. PEEK_OK when off.
 peek_status validate_kv(int32_t n, const int64_t* d_offsets, int64_t num_tokens, const int32_t* d_len, bool appends,
                         const int32_t* d_table, int32_t max_blocks, int64_t table_stride, int32_t block_size,
-                        int64_t num_pages, hipStream_t st);
+                        const kv::Pool* pool, hipStream_t st);
 
 }  // namespace peek

@@ -186,7 +186,7 @@ __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, in
 // -------------------------------------------------------------- validation
 __global__ void k_validate_kv(int32_t n, const int64_t* __restrict__ offsets, int64_t num_tokens,
                               const int32_t* __restrict__ len, bool appends, Table table, int32_t log_block,
-                              int64_t num_pages, int32_t* __restrict__ bad) {
+                              Pool pool, int32_t* __restrict__ bad) {
   const int32_t r = blockIdx.x;
   int32_t f = 0;
   int64_t fresh = 0;
@@ -204,7 +204,16 @@ __global__ void k_validate_kv(int32_t n, const int64_t* __restrict__ offsets, in
       const int32_t to = (int32_t)((all + (1 << log_block) - 1) >> log_block);
       for (int32_t b = from + (int32_t)threadIdx.x; b < to; b += (int32_t)blockDim.x) {
         const int32_t id = table.ids[(int64_t)r * table.stride + b];
-        if (id < 0 || id >= num_pages) f |= 4;
+        if (id < 0 || (uint32_t)id >= pool.num_pages) {
+          f |= 4;
+        } else if (pool.scales != nullptr && (int64_t)b << log_block < held) {       // the block holds tokens
+          const float* x = pool.scales + (int64_t)id * 2 * pool.heads;
+          for (int32_t h = 0; h < pool.heads; ++h) {
+            const bool k_fits = appends ? x[h] >= 0 && x[h] <= kv::kScaleMax : fabsf(x[h]) < __builtin_inff();
+            const float v = x[pool.heads + h];
+            if (!k_fits || !(v >= 0 && v <= kv::kScaleMax)) f |= 8;
+          }
+        }
       }
     }
   }
@@ -217,14 +226,16 @@ __global__ void k_clear_flag(int32_t* flag) { *flag = 0; }
 
 peek_status validate_kv(int32_t n, const int64_t* d_offsets, int64_t num_tokens, const int32_t* d_len, bool appends,
                         const int32_t* d_table, int32_t max_blocks, int64_t table_stride, int32_t block_size,
-                        int64_t num_pages, hipStream_t st) {
+                        const Pool* pool, hipStream_t st) {
   if (!validation_enabled() || n <= 0) return PEEK_OK;
   int32_t* d_bad = nullptr;
   PEEK_HIP_TRY(hipMalloc((void**)&d_bad, sizeof(int32_t)));
   int32_t bad = 0;
   hipLaunchKernelGGL(k_clear_flag, dim3(1), dim3(1), 0, st, d_bad);
+  const Pool any{nullptr, nullptr, INT32_MAX, 0, 0};
   hipLaunchKernelGGL(k_validate_kv, dim3((unsigned)n), dim3(64), 0, st, n, d_offsets, num_tokens, d_len, appends,
-                     Table{d_table, table_stride, max_blocks}, __builtin_ctz((unsigned)block_size), num_pages, d_bad);
+                     Table{d_table, table_stride, max_blocks}, __builtin_ctz((unsigned)block_size), pool ? *pool : any,
+                     d_bad);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) e = hipMemcpyAsync(&bad, d_bad, sizeof(int32_t), hipMemcpyDeviceToHost, st);
   if (e == hipSuccess) e = hipStreamSynchronize(st);
@@ -234,6 +245,9 @@ peek_status validate_kv(int32_t n, const int64_t* d_offsets, int64_t num_tokens,
     return fail(PEEK_ERR_INVALID_ARGUMENT, "d_offsets must be non-decreasing from 0 or more and end within num_tokens");
   if (bad & 2) return fail(PEEK_ERR_INVALID_ARGUMENT, "a sequence has fewer than 0 tokens or more than its table holds");
   if (bad & 4) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_block_table names pages outside the pool");
+  if (bad & 8)
+    return fail(PEEK_ERR_INVALID_ARGUMENT,
+                "a block's scales are out of range (keys: finite; values, and what an append adds to: 0 to 2^60)");
   return PEEK_OK;
 }
 
@@ -332,7 +346,7 @@ peek_status peek_kv_append(const peek_kv_pool* pool, int32_t n, int64_t num_toke
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many tokens for one call (%lld)", (long long)num_tokens);
     hipStream_t st = (hipStream_t)stream;
     s = validate_kv(n, d_offsets, num_tokens, d_context, true, d_block_table, max_blocks, table_stride,
-                    pool->block_size, pool->num_pages, st);
+                    pool->block_size, &p, st);
     if (s != PEEK_OK) return s;
     const Rows k{d_k, k_token_stride, k_head_stride}, v{d_v, v_token_stride, v_head_stride};
     const Table t{d_block_table, table_stride, max_blocks};

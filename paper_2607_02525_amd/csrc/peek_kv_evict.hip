@@ -475,8 +475,7 @@ peek_status peek_kv_evict(int32_t n, int32_t kv_heads, int32_t block_size, const
     s = check_workspace(d_workspace, workspace_bytes, peek_kv_evict_workspace(n, kv_heads, max_blocks));
     if (s != PEEK_OK) return s;
     hipStream_t st = (hipStream_t)stream;
-    s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, block_size, INT32_MAX,
-                    st);
+    s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, block_size, nullptr, st);
     if (s != PEEK_OK) return s;
     Evict a{Table{d_block_table, table_stride, max_blocks}, d_context, d_mass, d_keep, d_context_out, d_table_out,
             d_mass_out, d_freed, d_num_freed, kv_heads, __builtin_ctz((unsigned)block_size), sink, recent};

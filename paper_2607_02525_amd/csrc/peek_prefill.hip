@@ -107,6 +107,14 @@ __device__ __forceinline__ void to_lds(const uint16_t* base, uint32_t offset, ui
                : "memory");
 }
 
+// Waits for them, and for this wavefront's other loads: the builtin, so that the
+// compiler knows it and waits for none of these again in a loop.
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0), the other counters as they are
+  asm volatile("" ::: "memory");
+}
+
 // What sched_group_barrier calls them.
 constexpr int kProducts = 0x8, kLdsReads = 0x100;
 
@@ -162,13 +170,13 @@ struct Tile {
       __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 0);
     }
     if constexpr (CACHED) __builtin_amdgcn_sched_barrier(0);      // the scales are read after them
-    if (masked) {                // (a logit's scale is at least 2^-100: -infinity stays)
+    auto mask = [&]() {
       const int32_t left = seen - 4 * half;
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[j][e] = 32 * j + 8 * (e >> 2) + (e & 3) < left ? s[j][e] : -__builtin_inff();
-    }
+    };
     auto largest = [&]() {
       float most = s[0][0];
 #pragma unroll
@@ -197,10 +205,13 @@ struct Tile {
       };
       const f16 raw[2] = {s[0], s[1]};
       scaled(raw, s, top);       // less the maximum so far: most often that is all
-      if (__any(largest() > kSlack)) {
+      if ((int)masked | __any(largest() > kSlack)) {
         scaled(raw, s, 0.0f);    // (beside kNone nothing is left of a logit)
         raise(largest());
         scaled(raw, s, top);
+        // keys past the end are the last one again, so the maximum was right; a key's scale may be 0, so the mask
+        // comes after it
+        if (masked) mask();
       }
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
@@ -208,6 +219,7 @@ struct Tile {
         sum = fmaf(s[e >> 4][e & 15], by[e >> 2][2], sum);
       }
     } else {
+      if (masked) mask();        // (the call's scale is at least 2^-100: -infinity stays)
       const float most = largest() * scale;
       if (__any(most > top + kSlack)) raise(most);
 #pragma unroll
@@ -473,9 +485,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       *(u4*)(to + 16 * p0) = (u4){x0[0], x0[1], x1[0], x1[1]};
       *(u4*)(to + 16 * p1) = (u4){x2[0], x2[1], x3[0], x3[1]};
     }
-    if (leads)
-      s_scale[buf][unit_key / 4] =
-          (f4){scale_k * a.scale, log2_fast(scale_v), __builtin_amdgcn_rcpf(scale_v), 0.0f};
+    if (leads) {
+      const float v = kv::value_scale(scale_v);
+      s_scale[buf][unit_key / 4] = (f4){scale_k * a.scale, log2_fast(v), __builtin_amdgcn_rcpf(v), 0.0f};
+    }
   };
 
   if (tid == 0) s_odd = 0;
@@ -488,7 +501,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   } else if (tile0 < tiles) {
     load_own((tile0 - cached) * kKeys, tile0 & 1);
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  wait_loads();
   __syncthreads();
 
   // a loop for the cached tiles and one for the sequence's own, so that each
@@ -506,7 +519,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       tile.template step<true>(lds_k + buf * T::kBytes, lds_v + buf * T::kBytes, s_scale[buf], lane, a.scale,
                                left < kKeys, left);
     if (j + 1 < cached_end) store(buf ^ 1);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    wait_loads();
     __syncthreads();
   }
   // from here on, some row must not see all of a tile, and 0 times a NaN or an
@@ -523,7 +536,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (active && t0 < most)
       tile.template step<false>(lds_k + buf * T::kBytes, lds_v + buf * T::kBytes, nullptr, lane, a.scale,
                                 t0 + kKeys > least, token + 1 - t0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    wait_loads();
     __syncthreads();
   }
   // (a tile of rows spans 256 tokens at most: five tiles of keys)
@@ -674,7 +687,7 @@ peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t 
     const int64_t groups = std::max(tiles, std::min(tiles * a.splits, kTargetGroups));
     hipStream_t st = (hipStream_t)stream;
     s = validate_kv(n, d_offsets, num_tokens, d_prefix, false, d_block_table, max_blocks, table_stride,
-                    pool ? pool->block_size : 4, pool ? pool->num_pages : 0, st);
+                    pool ? pool->block_size : 4, pool ? &a.pool : nullptr, st);
     if (s != PEEK_OK) return s;
     a.q = Rows{d_q, q_token_stride, q_head_stride};
     a.k = Rows{d_k, k_token_stride, k_head_stride};

@@ -52,6 +52,101 @@ def prefill(q, k, v, new, scale, codes=None, scales=None, table=None, held=None)
     return out, lse
 
 
+# ------------------------------------------------------------------- scales
+SCALED = [(BF, F8, 16, 128), (BF, I8, 16, 64), (HF, F8, 4, 64), (HF, I8, 8, 128), (HF, F8, 64, 128)]
+
+
+@pytest.mark.parametrize("which", ["k", "v", "both"])
+@pytest.mark.parametrize("dtype,fmt,B,D", SCALED)
+def test_blocks_of_scale_zero(dtype, fmt, B, D, which):
+    """Keys of scale 0 are 0, and so are values but for the 2^-60 that stands for a smaller scale: other blocks and the
+    sums of weights stay right, in tiles that a sequence ends in too."""
+    gen = torch.Generator().manual_seed(4)
+    contexts, H, G = [1, 5, 63, 64, 100, 333, 700], 2, 3
+    codes, scales, table = make_pool(gen, contexts, H, B, D, fmt)
+    live = ~scales.isnan()
+    zero = live & (torch.rand(scales.shape, generator=gen) < 0.4)
+    if which != "both":
+        zero[:, 1 if which == "k" else 0] = False
+    scales[zero] = 0
+    if which != "k":
+        scales[table[0, 0].long(), 1] = 0                   # a sequence of nothing else
+    check(gen, contexts, H, G, codes, scales, table, dtype, D, D ** -0.5)
+
+
+def check(gen, contexts, H, G, codes, scales, table, dtype, D, scale, q_spread=1.0, new=2):
+    n, W, B = len(contexts), table.shape[1], codes.shape[3]
+    fmt, most = codes.dtype, R.most_of(scales, codes.dtype)
+    q = (torch.randn(n, H * G, D, generator=gen) * q_spread).to(dtype)
+    out, lse, mass = decode(q, codes, scales, table, contexts, scale, with_mass=True)
+    meant = scales.clone()
+    meant[:, 1] = scales[:, 1].clamp(min=2.0 ** -60)
+    kv = [R.cached(codes, meant, table[r], c) for r, c in enumerate(contexts)]
+    for r, c in enumerate(contexts):
+        want, wl, w, spread, reach = R.attend(q[r:r + 1], *kv[r], scale, c)
+        near(out[r:r + 1], want, R.out_bound(want, spread, reach, dtype, c, most), f"decode of {c} tokens")
+        near(lse[r:r + 1], wl, R.lse_bound(wl, reach, D), f"decode's lse of {c} tokens")
+        share = torch.zeros(H * G, W * B, dtype=torch.float64)
+        share[:, :c] = w[:, 0]
+        share = share.view(H, G, W, B).sum((1, 3))
+        near(mass[r], share, R.mass_bound(share, reach.view(H, G).amax(1)[:, None], share), f"mass of {c} tokens")
+    rows = (torch.randn(n * new, H * G, D, generator=gen) * q_spread).to(dtype)
+    k, v = (torch.randn(n * new, H, D, generator=gen).to(dtype) for _ in range(2))
+    out, lse = prefill(rows, k, v, [new] * n, scale, codes, scales, table, contexts)
+    for r, c in enumerate(contexts):
+        a, b = r * new, (r + 1) * new
+        want, wl, _, spread, reach = R.attend(rows[a:b], torch.cat([kv[r][0], k[a:b].double()]),
+                                              torch.cat([kv[r][1], v[a:b].double()]), scale, c + 1)
+        near(out[a:b], want, R.out_bound(want, spread, reach, dtype, c + new, most), f"prefill after {c} tokens")
+        near(lse[a:b], wl, R.lse_bound(wl, reach, D), f"prefill's lse after {c} tokens")
+
+
+@pytest.mark.parametrize("fmt", [F8, I8])
+def test_scales_at_their_limits(fmt):
+    """The smallest and the largest scale that an append leaves (2^-60 of a block of zeros, 2^60), and a call's scale
+    that takes a key's below the range of 32 bits."""
+    gen = torch.Generator().manual_seed(5)
+    contexts = [7, 90, 300]
+    for k_scale, v_scale, scale in ((2.0 ** -60, 2.0 ** -60, 0.125), (2.0 ** -60, 0.01, 1e-30), (2.0 ** 40, 2.0 ** 60, 1e-14),
+                                    (0.01, 2.0 ** 60, 0.125)):
+        codes, scales, table = make_pool(gen, contexts, 2, 16, 64, fmt)
+        live = ~scales.isnan()
+        scales[:, 0] = torch.where(live[:, 0], k_scale, scales[:, 0])
+        scales[:, 1] = torch.where(live[:, 1], v_scale, scales[:, 1])
+        check(gen, contexts, 2, 4, codes, scales, table, BF, 64, scale)
+
+
+def test_validation_reports_scales_out_of_range(monkeypatch):
+    import paper_2607_02525_amd as P
+    monkeypatch.setenv("PEEK_VALIDATE", "1")
+    H, B, D = 2, 16, 64
+    q, out = (torch.zeros(1, 2 * H, D, dtype=BF, device="cuda") for _ in range(2))
+    k = torch.zeros(1, H, D, dtype=BF, device="cuda")
+    one, table = torch.tensor([0, 1], device="cuda"), torch.tensor([[0, 2]], dtype=torch.int32, device="cuda")
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    # (K's, V's scale, where it is, the tokens held) and whether attention, and an append, may see it
+    for part, x, page, held, seen, added in ((0, 0.0, 2, 20, True, True), (1, 0.0, 2, 20, True, True),
+                                             (0, -1.0, 2, 20, True, False), (1, -1.0, 2, 20, False, False),
+                                             (0, math.nan, 2, 20, False, False), (1, math.nan, 2, 20, False, False),
+                                             (0, math.inf, 2, 20, False, False), (1, 2.0 ** 61, 2, 20, False, False),
+                                             (1, math.nan, 0, 20, False, True), (1, math.nan, 2, 16, True, True),
+                                             (1, math.nan, 1, 20, True, True)):
+        scales = torch.ones(4, 2, H)
+        scales[page, part, 1] = x
+        pool = P.KVPool(torch.zeros(4, 2, H, B, D, dtype=torch.int8).cuda(), scales.cuda())
+        ctx = torch.tensor([held], dtype=torch.int32).cuda()
+        for right, call in ((seen, lambda: P.peek_decode_attention(pool, q, ctx, table, out, ws)),
+                            (seen, lambda: P.peek_prefill_attention(q, k, k, one, out, ws, pool=pool, prefix=ctx,
+                                                                    block_table=table)),
+                            (added, lambda: P.peek_kv_append(pool, k, k, one, ctx, table))):
+            if right:
+                call()
+                continue
+            with pytest.raises(P.PeekError, match="scales") as e:
+                call()
+            assert e.value.status == P.PEEK_ERR_INVALID_ARGUMENT
+
+
 # --------------------------------------------------- infinities and NaN by place
 @pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 64)])
 @pytest.mark.parametrize("kind", ["cached", "parts", "many"])
