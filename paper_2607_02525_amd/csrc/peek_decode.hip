@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
   if constexpr (!WIDE) __syncthreads();
 
   f4 acc[kParts] = {};
-  float top = kNone, sum = 0.0f;
+  float top = kNone, peak = kNone, sum = 0.0f;
   uint32_t kw[2][kKeyWords];        // keys, and values, of the tile at hand, then of the next
   uint32_t vw[8][kParts / 4];
   float scale[2], log_v[2], inv_v[2];
@@ -273,13 +273,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
     float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                        fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     most = max_halves(swap16_max(most));
-    if (__any(most > top + kSlack)) {
-      const float higher = most > top + kSlack ? most : top;
-      const float fall = exp2_fast(top - higher);
-      top = higher;
-      sum *= fall;
+    if (__any(moves<TYPE>(most, top))) {
+      const float by = move_top<TYPE>(most, top, peak);
+      sum *= by;
 #pragma unroll
-      for (int p = 0; p < kParts; ++p) acc[p] *= fall;
+      for (int p = 0; p < kParts; ++p) acc[p] *= by;
     }
     u4 w;
 #pragma unroll

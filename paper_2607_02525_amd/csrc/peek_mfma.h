@@ -86,13 +86,56 @@ __device__ __forceinline__ float sum_halves(float x) {
 }
 
 // ------------------------------------------- running softmax, parts of a row
-// How far (in powers of two) a row's maximum may rise before what it has
-// summed is scaled down: weights stay below 2^8, and most tiles scale nothing.
+// A row's weights are 2^(x - top), of 16 bits where they meet the values. Where a
+// tile's largest x lies too far from `top`, top moves and what the row has
+// summed is scaled along; most tiles move nothing.
+//
+// bfloat16 has float32's range: top is the largest x, or one up to 2^8 smaller.
+//
+// float16 ends at 2^16 and loses bits below 2^-14, nearly all of them at 2^-24.
+// Small weights are often many, and together as much as the largest: all that
+// lies 14 nats below one key is a tenth of the sum from 130000 keys on, more
+// than that of the numerator where its V scale is smaller. So a
+// move puts a tile's largest weight at 2^7, up to 2^15 are let pass, and
+// top also moves down, when a tile's largest falls below 2^-8: rounding takes
+// from a weight 2^-11 of itself or 2^-17 of its own tile's largest at most, down
+// to kDeep + 15 below the row's (no further: the sum must stay within float32,
+// weights being divided by scales of 2^-60 and more). top is a whole number,
+// and every move exact. (Moves below 2^-2 came often where keys' scales differ by
+// 4 from block to block: 64 prompts over such a cache 1.25 ms, 1.18 with 2^-8, 1.15 where top only rises.)
 constexpr float kSlack = 8.0f;
+constexpr float kLeast = -8.0f, kMost = 15.0f, kMiddle = 7.0f, kDeep = 24.0f;
 constexpr float kNone = -1e30f;       // a maximum of nothing; finite, so that differences are numbers
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
+
+// Whether a tile whose largest x is `most` moves top.
+template <int TYPE>
+__device__ __forceinline__ bool moves(float most, float top) {
+  if constexpr (TYPE == PEEK_TYPE_BF16) return most > top + kSlack;
+  else return fabsf(most - top - (kMost + kLeast) / 2) > (kMost - kLeast) / 2;
+}
+
+// Moves top for such a tile (or leaves it, for another); what to scale sums by. `peak` is the highest top so far.
+template <int TYPE>
+__device__ __forceinline__ float move_top(float most, float& top, float& peak) {
+  float next = top;
+  if constexpr (TYPE == PEEK_TYPE_BF16) {
+    if (most > top + kSlack) next = most;
+    const float by = exp2_fast(top - next);
+    top = next;
+    return by;
+  } else {
+    const float here = floorf(most) - kMiddle;
+    if (most > top + kMost) next = here;
+    else if (most < top + kLeast && most > -__builtin_inff()) next = fminf(top, fmaxf(here, peak - kDeep));
+    const float by = __builtin_ldexpf(1.0f, (int)fmaxf(top - next, -1000.0f));
+    top = next;
+    peak = fmaxf(peak, top);
+    return by;
+  }
+}
 
 // Base-2 logarithm of a row's sum of weights from its parts' (-infinity: none), by a whole wavefront.
 __device__ __forceinline__ float row_log_sum(const float* __restrict__ p, int32_t parts, int lane) {

@@ -18,8 +18,8 @@
 // bits on the way, which is exact, and their scales never touch them: K's
 // multiplies the logit, and V's goes into the weight as an exponent,
 //   w_j s_j = 2^(x_j + log2 s_j - m),   sum of weights = sum_j (w_j s_j) / s_j,
-// with m the running maximum of x_j + log2 s_j, so weights times scales stay
-// within [0, 2^8] in either 16-bit type.
+// with m near the running maximum of x_j + log2 s_j (peek_mfma.h), so weights times
+// scales stay within the range of either 16-bit type.
 //
 // Rows and keys past the end: rows are clamped to the last one and not
 // stored; keys are clamped to the last one and masked, so nothing outside the
@@ -129,7 +129,7 @@ struct Tile {
 
   u4 q[kSteps];
   f16 acc[kParts];
-  float top, sum;
+  float top, peak, sum;
 
   // Where lane l begins to read a tile of K, and of V, at `tile` of LDS. From
   // there, k step i is at ^ 32 i and part p of the output at ^ 64 p: addresses
@@ -183,12 +183,11 @@ struct Tile {
       for (int e = 1; e < 32; ++e) most = fmaxf(most, s[e >> 4][e & 15]);
       return max_halves(most);
     };
-    auto raise = [&](float most) {
-      const float next = most > top + kSlack ? most : top, fall = exp2_fast(top - next);
-      top = next;
-      sum *= fall;
+    auto move = [&](float most) {
+      const float by = move_top<TYPE>(most, top, peak);
+      sum *= by;
 #pragma unroll
-      for (int p = 0; p < kParts; ++p) acc[p] *= fall;
+      for (int p = 0; p < kParts; ++p) acc[p] *= by;
     };
     if constexpr (CACHED) {
       f4 by[8];                  // of keys 4 g .. 4 g + 3: the logits' scale, the values' logarithm and reciprocal
@@ -204,10 +203,10 @@ struct Tile {
         }
       };
       const f16 raw[2] = {s[0], s[1]};
-      scaled(raw, s, top);       // less the maximum so far: most often that is all
-      if ((int)masked | __any(largest() > kSlack)) {
+      scaled(raw, s, top);       // most often that is all
+      if ((int)masked | __any(moves<TYPE>(largest(), 0.0f))) {
         scaled(raw, s, 0.0f);    // (beside kNone nothing is left of a logit)
-        raise(largest());
+        move(largest());
         scaled(raw, s, top);
         // keys past the end are the last one again, so the maximum was right; a key's scale may be 0, so the mask
         // comes after it
@@ -221,7 +220,7 @@ struct Tile {
     } else {
       if (masked) mask();        // (the call's scale is at least 2^-100: -infinity stays)
       const float most = largest() * scale;
-      if (__any(most > top + kSlack)) raise(most);
+      if (__any(moves<TYPE>(most, top))) move(most);
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
         s[e >> 4][e & 15] = exp2_fast(fmaf(s[e >> 4][e & 15], scale, -top));
@@ -415,7 +414,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
 #pragma unroll
     for (int p = 0; p < T::kParts; ++p) tile.acc[p] = (f16){};
-    tile.top = kNone;
+    tile.top = tile.peak = kNone;
     tile.sum = 0.0f;
   }
 

@@ -52,6 +52,112 @@ def prefill(q, k, v, new, scale, codes=None, scales=None, table=None, held=None)
     return out, lse
 
 
+# ------------------------------------------- many small weights beside a large one
+def faint_bound(out, spread, reach, dtype, weights, values, scales):
+    """As kv_reference's out_bound, but what is lost of a weight below the type's normal range is held against the
+    64 keys around it, not against the row: a weight times its value's scale is off by at most 2^-17 of the largest such
+    product there. weights [T, S] of one head, values [S, D], scales [S] of the values."""
+    S = scales.numel()
+    u, delta = R.ROUNDOFF[dtype], R.logit_error(reach, out.shape[-1])[..., None]
+    product = torch.nn.functional.pad(weights * scales, (0, -S % 64)).view(weights.shape[0], -1, 64).amax(2)
+    codes = torch.nn.functional.pad((values / scales[:, None]).abs(), (0, 0, 0, -S % 64)).view(-1, 64, values.shape[1])
+    lost = 2.0 ** -17 * (product @ codes.sum(1))
+    return u * out.abs() + (1 + u) * (u + 2.1 * delta + 2.0 ** -18) * spread + lost[:, None] + R.SMALLEST[dtype]
+
+
+def faint_cache(gen, tokens, fmt, nats, ratio, B=16, D=128):
+    """One token of a large logit (nats above all others) and no value, in a first block whose V scale is `ratio` times
+    the others'; 63 more tokens without a value; and `tokens` in all."""
+    blocks = -(-tokens // B)
+    codes = torch.zeros(blocks, 2, 1, B, D)
+    codes[0, 0, 0, 0, 0] = nats
+    codes[64 // B:, 1] = (torch.rand(blocks - 64 // B, 1, B, D, generator=gen) * 60).round() + 60
+    scales = torch.ones(blocks, 2, 1)
+    scales[:, 1] = 1 / 64
+    scales[0, 1] = ratio / 64
+    codes = codes.to(F8) if fmt == F8 else codes.to(I8)
+    return codes, scales, torch.arange(blocks, dtype=torch.int32)[None]
+
+
+@pytest.mark.parametrize("fmt", [F8, I8])
+@pytest.mark.parametrize("ratio", [1.0, 16.0, 64.0, 4096.0])
+def test_faint_weights_of_f16_rows_over_a_cache(fmt, ratio):
+    """24000 keys 14 nats below one without a value: together they have 2% of the weight, and are all of the output."""
+    gen = torch.Generator().manual_seed(1)
+    T, D = 24000, 128
+    codes, scales, table = faint_cache(gen, T, fmt, 14.0, ratio)
+    q = torch.zeros(3, 2, D, dtype=HF)
+    q[..., 0] = 1
+    keys, values = R.cached(codes, scales, table[0], T)
+    per_key = scales[:, 1, 0].double().repeat_interleave(16)
+    want, wl, w, spread, reach = R.attend(q[:1], keys, values, 1.0, T)
+    bound = faint_bound(want, spread, reach, HF, w[0], values[:, 0], per_key)
+    assert (bound < 2.0 ** -9 * want).all()
+    out, lse = decode(q[:1], codes, scales, table, [T], 1.0)
+    near(out, want, bound, "decode")
+    near(lse, wl, R.lse_bound(wl, reach, D), "decode's lse")
+    own = torch.zeros(3, 1, D, dtype=HF)
+    out, lse = prefill(q, own, own, [3], 1.0, codes, scales, table, [T])
+    for i in range(3):
+        want, wl, w, spread, reach = R.attend(q[i:i + 1], torch.cat([keys, own[:i + 1].double()]),
+                                              torch.cat([values, own[:i + 1].double()]), 1.0, T + i + 1)
+        # (the own tokens' values are 0: they have a part in the sum of weights alone)
+        bound = faint_bound(want, spread, reach, HF, w[0, :, :T], values[:, 0], per_key)
+        near(out[i:i + 1], want, bound, f"prefill, row {i}")
+        near(lse[i:i + 1], wl, R.lse_bound(wl, reach, D), f"prefill's lse, row {i}")
+
+
+@pytest.mark.parametrize("nats", [10.0, 14.0, 16.0])
+def test_faint_weights_of_f16_rows_over_own_tokens(nats):
+    gen = torch.Generator().manual_seed(2)
+    T, D = 12000, 64
+    q, k, v = torch.zeros(T, 1, D, dtype=HF), torch.zeros(T, 1, D, dtype=HF), torch.zeros(T, 1, D, dtype=HF)
+    q[..., 0] = 1
+    k[0, 0, 0] = nats
+    v[64:] = (torch.rand(T - 64, 1, D, generator=gen) + 1).to(HF)
+    out, lse = prefill(q, k, v, [T], 1.0)
+    for i in (100, 1023, 5000, T - 1):
+        want, wl, w, spread, reach = R.attend(q[i:i + 1], k[:i + 1], v[:i + 1], 1.0, i + 1)
+        bound = faint_bound(want, spread, reach, HF, w[0], v[:i + 1, 0].double(), torch.ones(i + 1).double())
+        near(out[i:i + 1], want, bound, f"row {i}")
+        near(lse[i:i + 1], wl, R.lse_bound(wl, reach, D), f"lse of row {i}")
+
+
+def test_faint_weights_between_large_ones():
+    """Tiles of large and of small V scales by turns, 2^14 apart, and logits that lie far apart too: what a row has
+    summed is brought to the size of the tile at hand and back."""
+    gen = torch.Generator().manual_seed(3)
+    T, D, B = 3000, 128, 16
+    for fmt in (F8, I8):
+        codes, scales, table = make_pool(gen, [T], 1, B, D, fmt, spread=1)
+        turn = torch.arange(T).div(B, rounding_mode="floor") // 4 % 2
+        for b in range(table.shape[1]):
+            scales[table[0, b].long(), 1] *= 2.0 ** (-12 if turn[b * B] else 2)
+        for q_spread in (1.0, 12.0):
+            q = (torch.randn(1, 4, D, generator=gen) * q_spread).to(HF)
+            keys, values = R.cached(codes, scales, table[0], T)
+            s = D ** -0.5
+            want, wl, w, spread, reach = R.attend(q, keys, values, s, T)
+            per_key = scales[table[0].long(), 1, 0].double().repeat_interleave(B)[:T]
+            bound = torch.cat([faint_bound(want[:, h:h + 1], spread[:, h:h + 1], reach[:, h:h + 1], HF, w[h],
+                                           values[:, 0], per_key) for h in range(4)], 1)
+            out, lse, mass = decode(q, codes, scales, table, [T], s, with_mass=True)
+            near(out, want, bound, "decode")
+            near(lse, wl, R.lse_bound(wl, reach, D), "decode's lse")
+            share = torch.zeros(table.shape[1] * B, dtype=torch.float64)
+            share[:T] = w[:, 0].sum(0)
+            share = share.view(-1, B).sum(1)
+            near(mass[0, 0], share, R.mass_bound(share, reach.amax(), share), "mass")
+            own = torch.zeros(1, 1, D, dtype=HF)
+            out, lse = prefill(q, own, own, [1], s, codes, scales, table, [T])
+            want, wl, w, spread, reach = R.attend(q, torch.cat([keys, own.double()]),
+                                                  torch.cat([values, own.double()]), s, T + 1)
+            bound = torch.cat([faint_bound(want[:, h:h + 1], spread[:, h:h + 1], reach[:, h:h + 1], HF, w[h][:, :T],
+                                           values[:, 0], per_key) for h in range(4)], 1)
+            near(out, want, bound, "prefill")
+            near(lse, wl, R.lse_bound(wl, reach, D), "prefill's lse")
+
+
 # ------------------------------------------------------------------- scales
 SCALED = [(BF, F8, 16, 128), (BF, I8, 16, 64), (HF, F8, 4, 64), (HF, I8, 8, 128), (HF, F8, 64, 128)]
 
