@@ -105,7 +105,10 @@ __device__ __forceinline__ float sum_halves(float x) {
 // 4 from block to block: 64 prompts over such a cache 1.25 ms, 1.18 with 2^-8, 1.15 where top only rises.)
 constexpr float kSlack = 8.0f;
 constexpr float kLeast = -8.0f, kMost = 15.0f, kMiddle = 7.0f, kDeep = 24.0f;
-constexpr float kNone = -1e30f;       // a maximum of nothing; finite, so that differences are numbers
+constexpr float kNone = -3.402823466e38f;      // a maximum of nothing: no logit is lower, and differences are numbers
+// Beyond this, x - top is a difference of numbers rounded alike, not the rounded difference of x's product: that may be
+// off by half a unit of top's, and 2^ that out of any range.
+constexpr float kFar = 0x1p22f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }

@@ -130,6 +130,7 @@ struct Tile {
   u4 q[kSteps];
   f16 acc[kParts];
   float top, peak, sum;
+  uint64_t far;        // of the wavefront: lanes whose row's top is beyond kFar
 
   // Where lane l begins to read a tile of K, and of V, at `tile` of LDS. From
   // there, k step i is at ^ 32 i and part p of the output at ^ 64 p: addresses
@@ -188,6 +189,7 @@ struct Tile {
       sum *= by;
 #pragma unroll
       for (int p = 0; p < kParts; ++p) acc[p] *= by;
+      far = __ballot(fabsf(top) > kFar);
     };
     if constexpr (CACHED) {
       f4 by[8];                  // of keys 4 g .. 4 g + 3: the logits' scale, the values' logarithm and reciprocal
@@ -204,10 +206,11 @@ struct Tile {
       };
       const f16 raw[2] = {s[0], s[1]};
       scaled(raw, s, top);       // most often that is all
-      if ((int)masked | __any(moves<TYPE>(largest(), 0.0f))) {
-        scaled(raw, s, 0.0f);    // (beside kNone nothing is left of a logit)
+      if ((int)masked | (int)(far != 0) | __any(moves<TYPE>(largest(), 0.0f))) {
+        scaled(raw, s, 0.0f);
         move(largest());
-        scaled(raw, s, top);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) s[e >> 4][e & 15] -= top;
         // keys past the end are the last one again, so the maximum was right; a key's scale may be 0, so the mask
         // comes after it
         if (masked) mask();
@@ -221,9 +224,16 @@ struct Tile {
       if (masked) mask();        // (the call's scale is at least 2^-100: -infinity stays)
       const float most = largest() * scale;
       if (__any(moves<TYPE>(most, top))) move(most);
+      float by = scale;
+      if (far != 0) {
+#pragma clang fp contract(off)
+        by = 1.0f;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) s[e >> 4][e & 15] *= scale;
+      }
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
-        s[e >> 4][e & 15] = exp2_fast(fmaf(s[e >> 4][e & 15], scale, -top));
+        s[e >> 4][e & 15] = exp2_fast(fmaf(s[e >> 4][e & 15], by, -top));
         sum += s[e >> 4][e & 15];
       }
     }
@@ -248,6 +258,13 @@ struct Tile {
 #pragma unroll
       for (int p = 0; p < kParts; ++p) acc[p] = mul32<TYPE>(values(i, p), w, acc[p]);
     }
+  }
+
+  // A product's logit, less top.
+  __device__ __forceinline__ float logit(float dot, float scale) const {
+#pragma clang fp contract(off)
+    const float rounded = dot * scale;
+    return far != 0 ? rounded - top : fmaf(dot, scale, -top);
   }
 
   // An element that is infinite or NaN, and eight of them with only those or without.
@@ -292,7 +309,7 @@ struct Tile {
           dot = fmaf(kv::to_float<TYPE>((uint16_t)(a >> 16)), kv::to_float<TYPE>((uint16_t)(b >> 16)), dot);
         }
       }
-      const float w = exp2_fast(fmaf(sum_halves(dot), scale, -top));
+      const float w = exp2_fast(logit(sum_halves(dot), scale));
       if (t >= seen) continue;
 #pragma unroll
       for (int p = 0; p < kParts; ++p)
@@ -415,6 +432,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
     for (int p = 0; p < T::kParts; ++p) tile.acc[p] = (f16){};
     tile.top = tile.peak = kNone;
+    tile.far = ~0ull;
     tile.sum = 0.0f;
   }
 

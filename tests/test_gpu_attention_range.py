@@ -213,8 +213,8 @@ def test_scales_at_their_limits(fmt):
     that takes a key's below the range of 32 bits."""
     gen = torch.Generator().manual_seed(5)
     contexts = [7, 90, 300]
-    for k_scale, v_scale, scale in ((2.0 ** -60, 2.0 ** -60, 0.125), (2.0 ** -60, 0.01, 1e-30), (2.0 ** 40, 2.0 ** 60, 1e-14),
-                                    (0.01, 2.0 ** 60, 0.125)):
+    for k_scale, v_scale, scale in ((2.0 ** -60, 2.0 ** -60, 0.125), (2.0 ** -60, 0.01, 1e-30),
+                                    (2.0 ** 40, 2.0 ** 60, 1e-14), (0.01, 2.0 ** 60, 0.125)):
         codes, scales, table = make_pool(gen, contexts, 2, 16, 64, fmt)
         live = ~scales.isnan()
         scales[:, 0] = torch.where(live[:, 0], k_scale, scales[:, 0])
@@ -253,6 +253,83 @@ def test_validation_reports_scales_out_of_range(monkeypatch):
             assert e.value.status == P.PEEK_ERR_INVALID_ARGUMENT
 
 
+# ------------------------------------------------------------------- logits
+def steep(T, H, D, size, dtype, gen):
+    """Keys whose logits are -size .. -2 size, each far from the next, the largest somewhere in the middle."""
+    k = torch.zeros(T, H, D, dtype=dtype)
+    order = torch.randperm(T, generator=gen)
+    k[:, :, 0] = -(size * (1 + order.float() / T))[:, None].to(dtype)
+    return k
+
+
+SIZES = [3e7, 1e9, 1e12, 1e20, 1e29, 1e31, 1e36]
+
+
+@pytest.mark.parametrize("dtype,size", [(HF, 3e7), (HF, 1e9), *((BF, x) for x in SIZES)])
+def test_logits_of_any_size_over_own_tokens(dtype, size):
+    """A row's sum of weights is at least that of its largest key, however large or far below 0 all of its logits are:
+    the output is a value of the row's, or between several."""
+    gen = torch.Generator().manual_seed(6)
+    T, H, D = 200, 2, 64
+    root = math.sqrt(size)
+    k = steep(T, H, D, root, dtype, gen)
+    v = (torch.rand(T, H, D, generator=gen) + 1).to(dtype)
+    for sign in (1, -1):
+        q = torch.zeros(T, H * 2, D, dtype=dtype)
+        q[..., 0] = sign * root
+        for new in ([T], [100, 0, 100]):
+            out, lse = prefill(q, k, v, new, 1.0)
+            a = 0
+            for t in new:
+                want, wl, w, _, reach = R.attend(q[a:a + t], k[a:a + t], v[a:a + t], 1.0, 1)
+                want = want / w.sum(2).T[..., None]      # (64 bits too lose the logarithm of a sum beside 1e20)
+                # a key's logit is the product of two numbers, rounded once, and times a power of two: keys that
+                # differ in 8 bits stay in order, and equal ones share the weight
+                near(out[a:a + t], want, 2.0 ** -7 * want.abs(), f"rows of {t} tokens")
+                near(lse[a:a + t], wl, R.lse_bound(wl, reach, D), f"lse of {t} tokens")
+                a += t
+
+
+@pytest.mark.parametrize("dtype,fmt", [(BF, F8), (BF, I8), (HF, F8)])
+@pytest.mark.parametrize("size", SIZES)
+def test_logits_of_any_size_over_a_cache(size, dtype, fmt):
+    gen = torch.Generator().manual_seed(7)
+    B, D, contexts = 16, 64, [1, 50, 64, 300]
+    codes, scales, table = make_pool(gen, contexts, 1, B, D, fmt)
+    x = torch.zeros(codes.shape[0], 1, B, D)
+    x[..., 0] = -96
+    for r, c in enumerate(contexts):                         # one key above the others, one below
+        for t, code in ((c // 2, -64), (c // 3, -120)):
+            if c > 1:
+                x[table[r, t // B].long(), 0, t % B, 0] = code
+    ids = torch.cat([table[r, :-(-c // B)].long() for r, c in enumerate(contexts)])
+    codes.view(torch.uint8)[ids, 0] = x.to(fmt).view(torch.uint8)[ids]
+    root = 2.0 ** min(round(math.log2(size) / 2), 60)
+    row = 2.0 ** round(math.log2(size / 64 / root)) if dtype == BF else 2.0 ** 10
+    call = size / 64 / root / row if dtype == HF else 1.0
+    scales[ids, 0] = root
+    for sign in (1, -1):
+        q = torch.zeros(len(contexts), 2, D, dtype=dtype)
+        q[..., 0] = sign * row
+        out, lse, mass = decode(q, codes, scales, table, contexts, call, with_mass=True)
+        rows = torch.zeros(len(contexts), 2, D, dtype=dtype)
+        rows[..., 0] = sign * row
+        far = torch.zeros(len(contexts), 1, D, dtype=dtype)      # an own key below all cached ones (float16: at 0)
+        if dtype == BF:
+            far[..., 0] = -sign * 448.0 * root
+        pre, pre_lse = prefill(rows, far, far, [1] * len(contexts), call, codes, scales, table, contexts)
+        for r, c in enumerate(contexts):
+            keys, values = R.cached(codes, scales, table[r], c)
+            want, wl, w, spread, reach = R.attend(q[r:r + 1], keys, values, call, c)
+            near(out[r:r + 1], want, 2.0 ** -7 * spread, f"decode of {c} tokens")
+            near(lse[r:r + 1], wl, R.lse_bound(wl, reach, D), f"decode's lse of {c} tokens")
+            near(mass[r].sum(), torch.tensor(2.0).double(), torch.tensor(1e-4).double(), f"mass of {c} tokens")
+            want, wl, w, spread, reach = R.attend(rows[r:r + 1], torch.cat([keys, far[r:r + 1].double()]),
+                                                  torch.cat([values, far[r:r + 1].double()]), call, c + 1)
+            near(pre[r:r + 1], want, 2.0 ** -7 * spread, f"prefill after {c} tokens")
+            near(pre_lse[r:r + 1], wl, R.lse_bound(wl, reach, D), f"prefill's lse after {c} tokens")
+
+
 # --------------------------------------------------- infinities and NaN by place
 @pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 64)])
 @pytest.mark.parametrize("kind", ["cached", "parts", "many"])
@@ -261,7 +338,8 @@ def test_values_that_are_no_numbers_reach_the_rows_that_see_them(kind, dtype, D)
     parts (one of which has the odd value), and with more sequences than are counted."""
     gen = torch.Generator().manual_seed(16)
     H, G, B = 2, 3, 16
-    held, new = {"cached": ([300, 64], [150, 70]), "parts": ([0], [2100]), "many": ([0, 16, 40] * 24, [33, 9, 70] * 24)}[kind]
+    held, new = {"cached": ([300, 64], [150, 70]), "parts": ([0], [2100]),
+                 "many": ([0, 16, 40] * 24, [33, 9, 70] * 24)}[kind]
     T, at = sum(new), [0]
     for x in new:
         at.append(at[-1] + x)
