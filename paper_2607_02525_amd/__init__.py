@@ -12,6 +12,7 @@ no CPU fallback: importing this module fails if libpeek.so is not built.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import numpy as np
@@ -140,6 +141,16 @@ def _arg(t, name: str, dtype=None, count: int | None = None):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     return t.data_ptr()
+
+
+def _row_arg(t, name: str, dtype, n: int, *row: int):
+    """As _arg, of n rows that are each [*row] (a tensor of one dimension is taken by its elements): rows of any other
+    shape would be read and written at the wrong places."""
+    if t is None:
+        return None
+    if t.dim() > 1 and (t.dim() != 1 + len(row) or tuple(t.shape[1:]) != row or t.shape[0] < n):
+        raise ValueError(f"{name} must be {[n, *row]}, got {list(t.shape)}")
+    return _arg(t, name, dtype, n * math.prod(row))
 
 
 def _queue_n(offsets) -> int:
@@ -519,7 +530,7 @@ def peek_prefill_attention(q, k, v, offsets, out, workspace, pool: KVPool | None
         *_rows(k, "k", q.dtype, None, dim, tokens), *_rows(v, "v", q.dtype, kv_heads, dim, tokens),
         _arg(offsets, "offsets"), _arg(prefix, "prefix", torch.int32, n), *table,
         dim ** -0.5 if scale is None else scale, *_rows(out, "out", q.dtype, q_heads, dim, tokens),
-        _arg(lse, "lse", torch.float32, tokens * q_heads), *_ws(workspace), _stream(stream)))
+        _row_arg(lse, "lse", torch.float32, tokens, q_heads), *_ws(workspace), _stream(stream)))
 
 
 def peek_decode_attention_workspace(pool: KVPool, n: int, q_heads: int, max_blocks: int, mass: bool = False) -> int:
@@ -535,13 +546,13 @@ def peek_decode_attention(pool: KVPool, q, context, block_table, out, workspace,
     kind = _row_type(q, "q")
     q_heads = q.shape[1] if q.dim() == 3 else 0
     table = _table(block_table, n)
-    masses = n * pool.kv_heads * table[1]
+    masses = pool.kv_heads, table[1]
     _check(_lib.peek_decode_attention(
         pool._ref, n, kind, q_heads, *_rows(q, "q", q.dtype, None, pool.head_dim),
         _arg(context, "context", torch.int32, n), *table, pool.head_dim ** -0.5 if scale is None else scale,
-        *_rows(out, "out", q.dtype, q_heads, pool.head_dim, n), _arg(lse, "lse", torch.float32, n * q_heads),
-        _arg(mass_in, "mass_in", torch.float32, masses), _arg(mass, "mass", torch.float32, masses), *_ws(workspace),
-        _stream(stream)))
+        *_rows(out, "out", q.dtype, q_heads, pool.head_dim, n), _row_arg(lse, "lse", torch.float32, n, q_heads),
+        _row_arg(mass_in, "mass_in", torch.float32, n, *masses), _row_arg(mass, "mass", torch.float32, n, *masses),
+        *_ws(workspace), _stream(stream)))
 
 
 def peek_kv_evict_workspace(n: int, kv_heads: int, max_blocks: int) -> int:
@@ -563,7 +574,7 @@ def peek_kv_evict(context, block_table, mass, keep, block_size: int, sink: int, 
     _check(_lib.peek_kv_evict(n, heads, int(block_size), _arg(context, "context", i32, n), *table,
                               _arg(mass, "mass", torch.float32), _arg(keep, "keep", i32, n), int(sink), int(recent),
                               _arg(context_out, "context_out", i32, n),
-                              _arg(block_table_out, "block_table_out", i32, n * width),
-                              _arg(mass_out, "mass_out", torch.float32, n * heads * width),
-                              _arg(freed, "freed", i32, n * width), _arg(num_freed, "num_freed", i32, n),
+                              _row_arg(block_table_out, "block_table_out", i32, n, width),
+                              _row_arg(mass_out, "mass_out", torch.float32, n, heads, width),
+                              _row_arg(freed, "freed", i32, n, width), _arg(num_freed, "num_freed", i32, n),
                               *_ws(workspace), _stream(stream)))

@@ -19,3 +19,20 @@ def test_tables_whose_rows_overlap_are_refused():
     for t in (wide, wide[:, :4], wide[::2], wide[:1, :4], row[None].expand(1, -1), torch.zeros(3, 0, dtype=i32)):
         with pytest.raises(ValueError, match="device tensor"):
             P._table(t, t.shape[0])
+
+
+def test_rows_of_another_shape_are_refused():
+    """Enough elements are not enough: a weight per block of another width would be read and written at wrong places."""
+    f32 = torch.float32
+    for shape in ((3, 2, 9), (3, 2, 4), (3, 5, 2), (2, 2, 5), (6, 5), (3, 1, 2, 5)):
+        with pytest.raises(ValueError, match="mass must be"):
+            P._row_arg(torch.zeros(shape), "mass", f32, 3, 2, 5)
+    with pytest.raises(ValueError, match="at least 30"):
+        P._row_arg(torch.zeros(29), "mass", f32, 3, 2, 5)
+    with pytest.raises(TypeError, match="mass must be"):
+        P._row_arg(torch.zeros(3, 2, 5).double(), "mass", f32, 3, 2, 5)
+    assert P._row_arg(None, "mass", f32, 3, 2, 5) is None
+    # the shape itself, more rows of it (a buffer for a larger batch), and one dimension get as far as the device check
+    for t in (torch.zeros(3, 2, 5), torch.zeros(4, 2, 5), torch.zeros(30), torch.zeros(64)):
+        with pytest.raises(ValueError, match="device tensor"):
+            P._row_arg(t, "mass", f32, 3, 2, 5)

@@ -395,3 +395,33 @@ def test_lengths_and_pages_that_there_are_not(B):
                                               torch.cat([values, v[r:r + 1].double()]), D ** -0.5, c + 1)
         near(pre[r:r + 1], want, R.out_bound(want, spread, reach, BF, c + 1, most), f"prefill of sequence {r}")
         near(pre_lse[r:r + 1], wl, R.lse_bound(wl, reach, D), f"prefill's lse of sequence {r}")
+
+
+# ------------------------------------------------------------ what else is refused
+def test_outputs_of_other_shapes_are_refused():
+    """Masses of a wider table than the call's, which a view of its leading columns makes easy, and the like."""
+    import paper_2607_02525_amd as P
+    H, B, D, n, W = 2, 16, 64, 3, 4
+    f32, i32 = dict(dtype=torch.float32, device="cuda"), dict(dtype=torch.int32, device="cuda")
+    pool = P.KVPool(torch.zeros(W, 2, H, B, D, dtype=torch.int8).cuda(), torch.ones(W, 2, H).cuda())
+    q = torch.zeros(n, 2 * H, D, dtype=BF).cuda()
+    k, out = torch.zeros(n, H, D, dtype=BF).cuda(), torch.empty_like(q)
+    ctx, offsets = torch.full((n,), 40, **i32), torch.arange(n + 1).cuda()
+    wide = torch.arange(W, **i32).repeat(n, 2)
+    table, ws = wide[:, :W], torch.empty(1 << 16, dtype=torch.uint8).cuda()
+    good, bad = torch.zeros(n, H, W, **f32), torch.zeros(n, H, 2 * W, **f32)
+    P.peek_decode_attention(pool, q, ctx, table, out, ws, mass=good, mass_in=good, lse=torch.empty(n, 2 * H, **f32))
+    for kw in (dict(mass=bad), dict(mass=good, mass_in=bad), dict(lse=torch.empty(2 * H, n, **f32))):
+        with pytest.raises(ValueError, match="must be"):
+            P.peek_decode_attention(pool, q, ctx, table, out, ws, **kw)
+    with pytest.raises(ValueError, match="lse must be"):
+        P.peek_prefill_attention(q, k, k, offsets, out, ws, lse=torch.empty(2 * H, n, **f32))
+    keep, count, held = torch.full((n,), 2, **i32), torch.empty(n, **i32), torch.empty(n, **i32)
+    outs = [torch.empty(n, W, **i32), torch.empty(n, H, W, **f32), torch.empty(n, W, **i32)]
+    P.peek_kv_evict(ctx, table, good, keep, B, 0, 1, held, *outs, count, ws)
+    for i, name in enumerate(("block_table_out", "mass_out", "freed")):
+        other = list(outs)
+        other[i] = torch.empty(*outs[i].shape[:-1], 2 * W, dtype=outs[i].dtype, device="cuda")
+        with pytest.raises(ValueError, match=f"{name} must be"):
+            P.peek_kv_evict(ctx, table, good, keep, B, 0, 1, held, *other, count, ws)
+    torch.cuda.synchronize()
