@@ -375,8 +375,9 @@ peek_status peek_offline_order(int32_t n, const int32_t* d_tokens, const int64_t
  * t * token_stride + j * head_stride + i, in elements of type
  * PEEK_TYPE_BF16 or PEEK_TYPE_F16, so slices of a fused projection need no
  * copy. Base pointers are 16-byte aligned, strides multiples of 8 that are
- * not negative. Query heads are a multiple of the kv heads, at most 65536;
- * query head j reads kv head j / (q_heads / kv_heads).
+ * not negative; no two rows of out share an element. Query heads are a
+ * multiple of the kv heads, at most 65536; query head j reads kv head
+ * j / (q_heads / kv_heads).
  *
  * Sums, maxima and weights are held in 32 bits; weights are rounded to the
  * query's type where they meet the values, the output once at the end.

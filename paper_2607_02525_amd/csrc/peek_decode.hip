@@ -491,7 +491,8 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
     if (d_mass_in && !d_mass) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_mass_in needs d_mass");
     if (n == 0) return PEEK_OK;
     if ((s = check_rows("d_q", d_q, q_token_stride, q_head_stride)) != PEEK_OK) return s;
-    if ((s = check_rows("d_out", d_out, out_token_stride, out_head_stride)) != PEEK_OK) return s;
+    s = check_out_rows("d_out", d_out, out_token_stride, out_head_stride, n, q_heads, pool->head_dim);
+    if (s != PEEK_OK) return s;
     if (!d_context) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_context must not be NULL");
     const Plan p = plan_for(*pool, n, q_heads, max_blocks, d_mass != nullptr);
     s = check_workspace(d_workspace, workspace_bytes, p.bytes);

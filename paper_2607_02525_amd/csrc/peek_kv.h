@@ -107,6 +107,9 @@ __device__ __forceinline__ int32_t last_at_most(int32_t n, int64_t x, int lane, 
 // Argument checks shared by the entry points (peek_kv.hip).
 peek_status check_pool(const peek_kv_pool* pool, kv::Pool* out);
 peek_status check_rows(const char* what, const void* data, int64_t token_stride, int64_t head_stride);
+// The same for rows that a call writes: no two of them share an element.
+peek_status check_out_rows(const char* what, const void* data, int64_t token_stride, int64_t head_stride,
+                           int64_t tokens, int32_t heads, int32_t dim);
 peek_status check_table(const int32_t* table, int32_t max_blocks, int64_t stride, int32_t block_size);
 
 peek_status check_heads(int32_t type, int32_t q_heads, int32_t kv_heads, float scale);

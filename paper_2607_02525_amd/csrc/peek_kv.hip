@@ -282,6 +282,27 @@ peek_status check_rows(const char* what, const void* data, int64_t token_stride,
   return PEEK_OK;
 }
 
+peek_status check_out_rows(const char* what, const void* data, int64_t token_stride, int64_t head_stride,
+                           int64_t tokens, int32_t heads, int32_t dim) {
+  const peek_status s = check_rows(what, data, token_stride, head_stride);
+  if (s != PEEK_OK) return s;
+  typedef __int128 wide;
+  const wide t = token_stride, h = head_stride;
+  bool overlap = (tokens > 1 && t < dim) || (heads > 1 && h < dim);
+  // tokens whole one after the other, or heads: most layouts. Otherwise head j of a
+  // token must not meet the first of one nearby.
+  if (!overlap && tokens > 1 && heads > 1 && (heads - 1) * h + dim > t && (tokens - 1) * t + dim > h) {
+    for (int32_t j = 1; j < heads && !overlap; ++j) {
+      const wide below = j * h / t, off = j * h - below * t;
+      overlap = (below >= 1 && below < tokens && off < dim) || (below + 1 < tokens && t - off < dim);
+    }
+  }
+  if (overlap)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "%s: rows of %d elements overlap at strides %lld (tokens) and %lld (heads)",
+                what, dim, (long long)token_stride, (long long)head_stride);
+  return PEEK_OK;
+}
+
 peek_status check_table(const int32_t* table, int32_t max_blocks, int64_t stride, int32_t block_size) {
   if (max_blocks < 0 || stride < max_blocks)
     return fail(PEEK_ERR_INVALID_ARGUMENT, "max_blocks must be >= 0 and table_stride at least that (got %d, %lld)",

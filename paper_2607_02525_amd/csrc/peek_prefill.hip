@@ -686,7 +686,8 @@ peek_status peek_prefill_attention(const peek_kv_pool* pool, int32_t n, int64_t 
     if ((s = check_rows("d_q", d_q, q_token_stride, q_head_stride)) != PEEK_OK) return s;
     if ((s = check_rows("d_k", d_k, k_token_stride, k_head_stride)) != PEEK_OK) return s;
     if ((s = check_rows("d_v", d_v, v_token_stride, v_head_stride)) != PEEK_OK) return s;
-    if ((s = check_rows("d_out", d_out, out_token_stride, out_head_stride)) != PEEK_OK) return s;
+    s = check_out_rows("d_out", d_out, out_token_stride, out_head_stride, num_tokens, q_heads, head_dim);
+    if (s != PEEK_OK) return s;
     if (k_token_stride >= (1 << 23) || v_token_stride >= (1 << 23))
       return fail(PEEK_ERR_INVALID_ARGUMENT, "the token strides of d_k and d_v must be below 2^23 (got %lld, %lld)",
                   (long long)k_token_stride, (long long)v_token_stride);

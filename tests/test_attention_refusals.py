@@ -36,3 +36,38 @@ def test_rows_of_another_shape_are_refused():
     for t in (torch.zeros(3, 2, 5), torch.zeros(4, 2, 5), torch.zeros(30), torch.zeros(64)):
         with pytest.raises(ValueError, match="device tensor"):
             P._row_arg(t, "mass", f32, 3, 2, 5)
+
+
+FAKE = 0x10000
+
+
+def attend(call, out_strides, tokens, heads, dim):
+    """What the entry point says to an output of this layout; the workspace is too small, so that nothing is run."""
+    p = P._PoolStruct(FAKE, FAKE, 8, 1, 16, dim, P.PEEK_TYPE_I8)
+    ref = P.ctypes.byref(p)
+    if call == "decode":
+        return P._lib.peek_decode_attention(ref, tokens, 0, heads, FAKE, heads * dim, dim, FAKE, FAKE, 1 << 20, 1 << 20,
+                                            1.0, FAKE, *out_strides, None, None, None, FAKE, 0, None)
+    return P._lib.peek_prefill_attention(ref, 1, tokens, 0, heads, 1, dim, FAKE, heads * dim, dim, FAKE, dim, 0, FAKE,
+                                         dim, 0, FAKE, FAKE, FAKE, 1 << 20, 1 << 20, 1.0, FAKE, *out_strides, None, FAKE,
+                                         0, None)
+
+
+def test_outputs_whose_rows_overlap_are_refused():
+    """Against a count of the elements that rows share; strides in units of 8 over heads of 64."""
+    seen = set()
+    for call in ("decode", "prefill"):
+        for tokens, heads in ((1, 1), (1, 3), (3, 1), (2, 2), (3, 4), (5, 3)):
+            for ts in (0, 8, 56, 64, 72, 128, 192, 200, 256, 320, 100 * 8):
+                for hs in (0, 8, 64, 72, 104, 128, 136, 192, 256, 320, 960):
+                    places = {t * ts + h * hs + i for t in range(tokens) for h in range(heads) for i in range(64)}
+                    apart = len(places) == tokens * heads * 64
+                    status = attend(call, (ts, hs), tokens, heads, 64)
+                    seen.add(apart)
+                    if apart:
+                        assert status == P.PEEK_ERR_WORKSPACE_TOO_SMALL, (call, tokens, heads, ts, hs)
+                    else:
+                        assert status == P.PEEK_ERR_INVALID_ARGUMENT and "overlap" in P.peek_last_error()
+    assert seen == {True, False}
+    for strides in ((1 << 62, 64), (64, 1 << 62)):
+        assert attend("decode", strides, 1 << 16, 1 << 16, 64) == P.PEEK_ERR_WORKSPACE_TOO_SMALL
