@@ -472,8 +472,22 @@ peek_status peek_kv_evict(int32_t n, int32_t kv_heads, int32_t block_size, const
         overlap(d_mass_out, row * kv_heads, d_mass, row * kv_heads))
       return fail(PEEK_ERR_INVALID_ARGUMENT,
                   "the outputs must not overlap the table and the masses they are made from");
-    s = check_workspace(d_workspace, workspace_bytes, peek_kv_evict_workspace(n, kv_heads, max_blocks));
+    const size_t need = peek_kv_evict_workspace(n, kv_heads, max_blocks);
+    s = check_workspace(d_workspace, workspace_bytes, need);
     if (s != PEEK_OK) return s;
+    // every array that is written against every other, in place of which only the context may be
+    const struct {
+      const void* at;
+      size_t bytes;
+    } arrays[] = {{d_context_out, (size_t)n * 4}, {d_table_out, row}, {d_mass_out, row * kv_heads}, {d_freed, row},
+                  {d_num_freed, (size_t)n * 4}, {d_workspace, need},
+                  {d_context, (size_t)n * 4}, {d_block_table, in_row}, {d_mass, row * kv_heads}, {d_keep, (size_t)n * 4}};
+    constexpr int kWritten = 6, kContextOut = 0, kContext = 6;
+    for (int i = 0; i < kWritten; ++i)
+      for (int j = i + 1; j < (int)(sizeof(arrays) / sizeof(arrays[0])); ++j)
+        if (!(i == kContextOut && j == kContext && d_context_out == d_context) &&
+            overlap(arrays[i].at, arrays[i].bytes, arrays[j].at, arrays[j].bytes))
+          return fail(PEEK_ERR_INVALID_ARGUMENT, "the outputs must not overlap each other, the inputs or the workspace");
     hipStream_t st = (hipStream_t)stream;
     s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, block_size, nullptr, st);
     if (s != PEEK_OK) return s;

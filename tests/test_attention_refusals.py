@@ -71,3 +71,30 @@ def test_outputs_whose_rows_overlap_are_refused():
     assert seen == {True, False}
     for strides in ((1 << 62, 64), (64, 1 << 62)):
         assert attend("decode", strides, 1 << 16, 1 << 16, 64) == P.PEEK_ERR_WORKSPACE_TOO_SMALL
+
+
+def test_evictions_into_arrays_that_overlap_are_refused():
+    """Every output against every other array, by its first and its last bytes."""
+    n, heads, width, stride = 3, 2, 40000, 40010
+    row = n * width * 4
+    size = {"ctx": n * 4, "table": ((n - 1) * stride + width) * 4, "mass": row * heads, "keep": n * 4, "ctx_out": n * 4,
+            "table_out": row, "mass_out": row * heads, "freed": row, "num": n * 4,
+            "ws": P._lib.peek_kv_evict_workspace(n, heads, width)}
+    far = {name: (i + 1) << 32 for i, name in enumerate(size)}
+
+    def evict(at):
+        status = P._lib.peek_kv_evict(n, heads, 16, at["ctx"], at["table"], width, stride, at["mass"], at["keep"], 0, 1,
+                                      at["ctx_out"], at["table_out"], at["mass_out"], at["freed"], at["num"], at["ws"],
+                                      size["ws"], None)
+        return status, P.peek_last_error()
+
+    outputs = ("ctx_out", "table_out", "mass_out", "freed", "num")
+    for out in outputs:
+        for other in size:
+            if other == out:
+                continue
+            for at in (far[other], far[other] + size[other] - 4, far[other] - size[out] + 4):
+                if (out, other, at) == ("ctx_out", "ctx", far["ctx"]):
+                    continue
+                status, message = evict({**far, out: at})
+                assert status == P.PEEK_ERR_INVALID_ARGUMENT and "overlap" in message, (out, other)
