@@ -512,6 +512,7 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
  *   d_mass_out  float32[n][kv_heads][max_blocks], the rest 0
  *   d_freed     int32[n][max_blocks]: the evicted pages by position, then -1
  *   d_num_freed int32[n],  d_context_out[r] = context - block_size * freed
+ * (the context as it was cut to the table, where it was).
  * Keys carry their positions already, so attention over what stays needs
  * nothing else. Input and output arrays must not overlap, but d_context_out
  * may be d_context. Scratch comes only from d_workspace (device, 256-byte

@@ -270,7 +270,7 @@ __global__ __launch_bounds__(THREADS) void k_evict_one(Evict a) {
   __shared__ int2 s_wave[kWaves];
   const int32_t r = blockIdx.x, t = threadIdx.x, width = a.table.width;
   const int lane = t & (kWave - 1), wave = t / kWave;
-  const int32_t ctx = a.context[r];
+  const int32_t ctx = kv::clip_tokens(a.context[r], width, a.log_block);
   const Range g = range_of(a, r);
   uint32_t last = 0;
   int32_t equal = 0;
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(kPartThreads) void k_evict_move(Evict a) {
     __syncthreads();
     if (blockIdx.x == 0 && t == 0) {
       a.num_freed[r] = g.drop;
-      a.context_out[r] = a.context[r] - (g.drop << a.log_block);
+      a.context_out[r] = kv::clip_tokens(a.context[r], a.table.width, a.log_block) - (g.drop << a.log_block);
     }
   }
 }

@@ -425,3 +425,25 @@ def test_outputs_of_other_shapes_are_refused():
         with pytest.raises(ValueError, match=f"{name} must be"):
             P.peek_kv_evict(ctx, table, good, keep, B, 0, 1, held, *other, count, ws)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("W", [6, 9000])
+def test_eviction_of_lengths_that_there_are_not(W):
+    """Lengths are cut to 0 .. the table's tokens before blocks are counted, and so is the context that is left."""
+    import paper_2607_02525_amd as P
+    B, H, n = 16, 2, 5
+    told = [-1, W * B + 1, 2 ** 31 - 1, W * B - 3, -2 ** 31]
+    held = [0, W * B, W * B, W * B - 3, 0]
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table = torch.arange(n * W, **i32).view(n, W)
+    mass = torch.rand(n, H, W, device="cuda")
+    keep, res = torch.full((n,), 4, **i32), []
+    for lengths in (told, held):
+        ctx, count = torch.tensor(lengths, **i32), torch.empty(n, **i32)
+        outs = [torch.empty(n, W, **i32), torch.empty(n, H, W, device="cuda"), torch.empty(n, W, **i32)]
+        ws = torch.empty(max(256, P.peek_kv_evict_workspace(n, H, W)), dtype=torch.uint8, device="cuda")
+        P.peek_kv_evict(ctx, table, mass, keep, B, 1, 2, ctx, *outs, count, ws)
+        torch.cuda.synchronize()
+        res.append([ctx, *outs, count])
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+    assert res[0][0].tolist() == [0, 4 * B, 4 * B, 4 * B - 3, 0]
