@@ -427,7 +427,8 @@ class _PoolStruct(ctypes.Structure):
 
 class KVPool:
     """The cache's contents: pages [num_pages, 2, kv_heads, block_size, head_dim] of 8-bit codes (K at 0, V at 1;
-    torch.float8_e4m3fn or torch.int8) and scales float32 [num_pages, 2, kv_heads], tensors of the caller's."""
+    torch.float8_e4m3fn or torch.int8) and scales float32 [num_pages, 2, kv_heads], tensors of the caller's. They stay
+    the pool's: other tensors make another pool."""
 
     def __init__(self, pages, scales):
         if pages.dtype not in _PAGE_TYPES:
@@ -436,12 +437,20 @@ class KVPool:
             raise ValueError("pages must be [num_pages, 2, kv_heads, block_size, head_dim]")
         if scales.shape != pages.shape[:3]:
             raise ValueError(f"scales must be {tuple(pages.shape[:3])}, got {tuple(scales.shape)}")
-        self.pages, self.scales = pages, scales
+        self._pages, self._scales = pages, scales
         self.num_pages, _, self.kv_heads, self.block_size, self.head_dim = pages.shape
         p, s = _arg(pages, "pages"), _arg(scales, "scales", torch.float32)
         self._struct = _PoolStruct(p, s, self.num_pages, self.kv_heads, self.block_size, self.head_dim,
                                    _PAGE_TYPES[pages.dtype])
         self._ref = ctypes.addressof(self._struct)
+
+    @property
+    def pages(self):
+        return self._pages
+
+    @property
+    def scales(self):
+        return self._scales
 
     @classmethod
     def empty(cls, num_pages: int, kv_heads: int, block_size: int, head_dim: int, dtype=torch.float8_e4m3fn,

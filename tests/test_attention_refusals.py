@@ -98,3 +98,9 @@ def test_evictions_into_arrays_that_overlap_are_refused():
                     continue
                 status, message = evict({**far, out: at})
                 assert status == P.PEEK_ERR_INVALID_ARGUMENT and "overlap" in message, (out, other)
+
+
+def test_a_pool_keeps_its_tensors():
+    """Other pages or scales cannot be put into a pool, whose calls would go on with the memory of the first."""
+    for name in ("pages", "scales"):
+        assert isinstance(getattr(P.KVPool, name), property) and getattr(P.KVPool, name).fset is None

@@ -447,3 +447,15 @@ def test_eviction_of_lengths_that_there_are_not(W):
         res.append([ctx, *outs, count])
     assert all(torch.equal(a, b) for a, b in zip(*res))
     assert res[0][0].tolist() == [0, 4 * B, 4 * B, 4 * B - 3, 0]
+
+
+def test_a_pool_keeps_its_tensors():
+    """Other pages or scales cannot be put into a pool, whose calls would go on with the memory of the first."""
+    import paper_2607_02525_amd as P
+    pool = P.KVPool.empty(2, 1, 16, 64)
+    pages, scales = pool.pages, pool.scales
+    with pytest.raises(AttributeError):
+        pool.pages = pages.clone()
+    with pytest.raises(AttributeError):
+        pool.scales = scales.clone()
+    assert pool.pages is pages and pool.scales is scales and pool._struct.d_pages == pages.data_ptr()
