@@ -134,8 +134,10 @@ def serve(workload, steps=8, keep=24, q_heads=8, kv_heads=2, dim=64, dtype=torch
     peek_prefill_attention(q, k, v, offsets, out, ws, pool=pool, prefix=prefix, block_table=d_table)
     peek_kv_append(pool, k, v, offsets, prefix, d_table)
     # (a prompt that is cached whole has no row; its first token is that of its id)
-    last = (offsets[1:] - 1).clamp(min=0)
-    token = torch.where(offsets[1:] > offsets[:-1], layer.next(out[last]), _ints([w.prompt(r)[-1] for r in range(w.n)]))
+    token = _ints([w.prompt(r)[-1] for r in range(w.n)], torch.int64)
+    if len(out) > 0:
+        last = (offsets[1:] - 1).clamp(min=0)
+        token = torch.where(offsets[1:] > offsets[:-1], layer.next(out[last]), token)
 
     context = _ints(w.lengths)
     one = torch.arange(w.n + 1, device="cuda")
