@@ -510,9 +510,13 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
  * for tokens to come) included:
  *   d_table_out int32[n][max_blocks], the rest of a row -1
  *   d_mass_out  float32[n][kv_heads][max_blocks], the rest 0
- *   d_freed     int32[n][max_blocks]: the evicted pages by position, then -1
+ *   d_freed     int32[n][max_blocks]: the evicted entries by position, then -1
+ *               (d_num_freed counts them: an entry may itself be -1)
  *   d_num_freed int32[n],  d_context_out[r] = context - block_size * freed
  * (the context as it was cut to the table, where it was).
+ * A page that several sequences name is listed for each that lets go of it,
+ * and stays in the tables of the others: the caller counts a shared page's
+ * users before it takes one as free.
  * Keys carry their positions already, so attention over what stays needs
  * nothing else. Input and output arrays must not overlap, but d_context_out
  * may be d_context. Scratch comes only from d_workspace (device, 256-byte
