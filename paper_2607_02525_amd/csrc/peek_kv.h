@@ -115,13 +115,11 @@ peek_status check_table(const int32_t* table, int32_t max_blocks, int64_t stride
 peek_status check_heads(int32_t type, int32_t q_heads, int32_t kv_heads, float scale);
 peek_status check_workspace(const void* d_workspace, size_t bytes, size_t need);
 
-// A caller's scale as the kernels take it: a factor >= 0 of base-2 logits, and
-// what to do to q's bits so that it is one. With a factor of at least 2^-100,
-// a masked logit of -infinity stays one (own keys: a cached key's own scale may be
-// anything, and is applied before the mask).
+// A caller's scale as the kernels take it: a factor > 0 of base-2 logits, and
+// what to do to q's bits so that it is one (a masked logit of -infinity stays one).
 inline void set_scale(float scale, float* factor, uint32_t* q_flip, uint32_t* q_mask) {
   const float f = std::fabs(scale) * 1.44269504088896341f;
-  const bool none = f < 0x1p-100f;
+  const bool none = f == 0.0f;
   *factor = none ? 1.0f : std::fmin(f, 3e38f);
   *q_flip = !none && scale < 0 ? 0x80008000u : 0u;
   *q_mask = none ? 0u : 0xffffffffu;

@@ -221,7 +221,7 @@ struct Tile {
         sum = fmaf(s[e >> 4][e & 15], by[e >> 2][2], sum);
       }
     } else {
-      if (masked) mask();        // (the call's scale is at least 2^-100: -infinity stays)
+      if (masked) mask();        // (the call's scale is not 0: -infinity stays)
       const float most = largest() * scale;
       if (__any(moves<TYPE>(most, top))) move(most);
       float by = scale;

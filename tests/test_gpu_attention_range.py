@@ -459,3 +459,30 @@ def test_a_pool_keeps_its_tensors():
     with pytest.raises(AttributeError):
         pool.scales = scales.clone()
     assert pool.pages is pages and pool.scales is scales and pool._struct.d_pages == pages.data_ptr()
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -105, -1e-33, 2.0 ** -120])
+def test_scales_that_bring_large_products_down(scale):
+    """bfloat16 rows of a size that only a very small scale brings to logits of a few."""
+    gen = torch.Generator().manual_seed(8)
+    H, G, D, contexts = 2, 3, 64, [1, 40, 130]
+    codes, scales, table = make_pool(gen, contexts, H, 16, D, F8)
+    size = 2.0 ** round(-math.log2(abs(scale)) / 2)
+    scales[:, 0] *= size
+    n, new = len(contexts), 50
+    q = (torch.randn(n, H * G, D, generator=gen) * size / 8).to(BF)
+    out, lse = decode(q, codes, scales, table, contexts, scale)
+    rows = (torch.randn(n * new, H * G, D, generator=gen) * size / 8).to(BF)
+    k, v = ((torch.randn(n * new, H, D, generator=gen) * x).to(BF) for x in (size, 1.0))
+    pre, pre_lse = prefill(rows, k, v, [new] * n, scale, codes, scales, table, contexts)
+    most = R.most_of(scales[:, 1], F8)
+    for r, c in enumerate(contexts):
+        keys, values = R.cached(codes, scales, table[r], c)
+        want, wl, _, spread, reach = R.attend(q[r:r + 1], keys, values, scale, c)
+        near(out[r:r + 1], want, R.out_bound(want, spread, reach, BF, c, most), f"decode of {c} tokens")
+        near(lse[r:r + 1], wl, R.lse_bound(wl, reach, D), f"decode's lse of {c} tokens")
+        a, b = r * new, (r + 1) * new
+        want, wl, _, spread, reach = R.attend(rows[a:b], torch.cat([keys, k[a:b].double()]),
+                                              torch.cat([values, v[a:b].double()]), scale, c + 1)
+        near(pre[a:b], want, R.out_bound(want, spread, reach, BF, c + new, most), f"prefill after {c} tokens")
+        near(pre_lse[a:b], wl, R.lse_bound(wl, reach, D), f"prefill's lse after {c} tokens")
