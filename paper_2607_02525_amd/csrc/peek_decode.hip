@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
         const int32_t t = t0 + 16 * h + 4 * grp;
         if (t < to && (t & ((1 << a.log_grain) - 1)) == 0)
           a.weights[((((int64_t)r * a.pool.heads + head) * a.row_tiles + row_tile) * a.grains + (t >> a.log_grain)) * kRows +
-                    col] = log2_fast(add) + top;
+                    col] = log2_sum(top, add);
       }
     }
 #pragma unroll
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] += part * s_out[w][g][d + e];
     }
-    const float over = 1.0f / total, l2 = highest + log2_fast(total);
+    const float over = 1.0f / total, l2 = log2_sum(highest, total);
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] *= over;
     if (whole) {

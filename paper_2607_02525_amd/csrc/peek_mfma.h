@@ -113,6 +113,13 @@ constexpr float kFar = 0x1p22f;
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
+// top + log2(sum), the sum's power of two taken out first: the logarithm of a number near 2^7, where a float16 row's
+// largest weight lies, has a unit many times as large as its fraction's. (A block's weight and its row's sum take the
+// same one: beside a top of 1e9 other sums of the same parts differ by whole powers of two.)
+__device__ __forceinline__ float log2_sum(float top, float sum) {
+  return top + (float)__builtin_amdgcn_frexp_expf(sum) + log2_fast(__builtin_amdgcn_frexp_mantf(sum));
+}
+
 // Whether a tile whose largest x is `most` moves top.
 template <int TYPE>
 __device__ __forceinline__ bool moves(float most, float top) {
@@ -154,7 +161,7 @@ __device__ __forceinline__ float row_log_sum(const float* __restrict__ p, int32_
     sum = sum * exp2_fast(top - next) + y * exp2_fast(x - next);
     top = next;
   }
-  return top + log2_fast(sum);
+  return log2_sum(top, sum);
 }
 
 // A row's parts [parts][D] joined by WAVES wavefronts of a workgroup, this one

@@ -576,7 +576,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         *(f4*)(out + 32 * p + 8 * e) =
             (f4){x[4 * e] * over, x[4 * e + 1] * over, x[4 * e + 2] * over, x[4 * e + 3] * over};
       }
-    if (half == 0) a.part_lse[out_row * a.splits + split] = none ? -__builtin_inff() : tile.top + log2_fast(sum);
+    if (half == 0) a.part_lse[out_row * a.splits + split] = none ? -__builtin_inff() : log2_sum(tile.top, sum);
     return;
   }
   const float over = 1.0f / sum;
@@ -589,7 +589,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       *(u2*)(out + 32 * p + 8 * e) = (u2){pack2<TYPE>(x[4 * e] * over, x[4 * e + 1] * over),
                                           pack2<TYPE>(x[4 * e + 2] * over, x[4 * e + 3] * over)};
     }
-  if (a.lse && half == 0) a.lse[out_row] = (tile.top + log2_fast(sum)) * 0.69314718055994531f;
+  if (a.lse && half == 0) a.lse[out_row] = log2_sum(tile.top, sum) * 0.69314718055994531f;
 }
 
 // Joins the parts of four rows, a wavefront to a row: 5 us for 37 tokens of 64

@@ -486,3 +486,22 @@ def test_scales_that_bring_large_products_down(scale):
                                               torch.cat([values, v[a:b].double()]), scale, c + 1)
         near(pre[a:b], want, R.out_bound(want, spread, reach, BF, c + new, most), f"prefill after {c} tokens")
         near(pre_lse[a:b], wl, R.lse_bound(wl, reach, D), f"prefill's lse after {c} tokens")
+
+
+@pytest.mark.parametrize("fmt", [F8, I8])
+def test_lse_of_float16_rows_of_few_tokens(fmt):
+    """Many rows whose lse is near 0, where an error of the logarithm's parts shows."""
+    gen = torch.Generator().manual_seed(9)
+    H, G, D, contexts = 4, 8, 64, [1 + i % 40 for i in range(300)]
+    codes, scales, table = make_pool(gen, contexts, H, 16, D, fmt)
+    q = torch.randn(len(contexts), H * G, D, generator=gen).to(HF)
+    out, lse = decode(q, codes, scales, table, contexts, 1e-3)
+    k, v = (torch.randn(len(contexts), H, D, generator=gen).to(HF) for _ in range(2))
+    _, pre_lse = prefill(q, k, v, [1] * len(contexts), 1e-3, codes, scales, table, contexts)
+    for r, c in enumerate(contexts):
+        keys, values = R.cached(codes, scales, table[r], c)
+        _, wl, _, _, reach = R.attend(q[r:r + 1], keys, values, 1e-3, c)
+        near(lse[r:r + 1], wl, R.lse_bound(wl, reach, D), f"decode's lse of {c} tokens")
+        _, wl, _, _, reach = R.attend(q[r:r + 1], torch.cat([keys, k[r:r + 1].double()]),
+                                      torch.cat([values, v[r:r + 1].double()]), 1e-3, c + 1)
+        near(pre_lse[r:r + 1], wl, R.lse_bound(wl, reach, D), f"prefill's lse after {c} tokens")
