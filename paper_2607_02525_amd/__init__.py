@@ -148,6 +148,8 @@ def _row_arg(t, name: str, dtype, n: int, *row: int):
     shape would be read and written at the wrong places."""
     if t is None:
         return None
+    if t.shape == (n, *row):
+        return _arg(t, name, dtype)
     if t.dim() > 1 and (t.dim() != 1 + len(row) or tuple(t.shape[1:]) != row or t.shape[0] < n):
         raise ValueError(f"{name} must be {[n, *row]}, got {list(t.shape)}")
     return _arg(t, name, dtype, n * math.prod(row))
