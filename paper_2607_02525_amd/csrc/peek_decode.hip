@@ -4,7 +4,7 @@
 // group's query heads together, as 16 rows of the matrix products. A
 // workgroup of four wavefronts takes one chunk of one sequence's tokens for one
 // kv head and 16 of its rows; a wavefront takes every fourth tile of 32
-// tokens, on its own, with a running maximum and sum. Long sequences are split
+// tokens, on its own, with a running reference and sum. Long sequences are split
 // into chunks so that a few of them still fill the device; the chunks'
 // results are joined by a second kernel, in a fixed order.
 //

@@ -7,10 +7,10 @@
 // keys before it) + min(equal keys before it, equal): one sum over the blocks in
 // order places them all, without a sort.
 //
-// Bound by memory where there are many tables (the masses are read for the scores,
-// again from L2 or MALL for the move, and written): 192 tables of 250 to 8125 blocks
-// of 8 heads, 59 MB, 32 us; by the passes' waits where there are few: 64 tables of
-// up to 463 blocks 8.6 us.
+// Bound by the longest table's one workgroup, which scores, selects and moves all of
+// it: 192 tables of 250 to 8125 blocks of 8 heads, 59 MB, 42 us, 32 where the masses
+// are in the cache already (a copy of as much memory takes 12); by the passes' waits
+// where tables are short: 64 of up to 463 blocks 8.6 us.
 #include <algorithm>
 
 #include "peek_internal.h"
@@ -29,7 +29,7 @@ constexpr int kBins = 2048;
 // up to kSmallTable (1500 tables of up to 500 blocks 17 us, with 1024 threads 41; 64
 // of up to 1875 blocks 16.5 us, with 1024 threads 11). A wider one is spread
 // over workgroups, with one for the passes between scores and move (three tables of up
-// to 32500 blocks 39 us, with a workgroup each 112; of up to 8000 blocks 22 either
+// to 32500 blocks 37 us, with a workgroup each 112; of up to 8000 blocks 22 either
 // way, of up to 4000 14 with one workgroup and 20 spread).
 constexpr int32_t kSmallTable = 1024;
 constexpr int32_t kLdsTable = 8192;

@@ -4,8 +4,8 @@
 // sequence, a row being a (token, query head of the group) pair in that
 // order, so that a few new tokens of a wide group still fill a tile and every
 // row of it shares the keys. It goes over the keys in tiles of 64, first the
-// cached prefix, then the sequence's own tokens up to its last row, and keeps
-// the running maximum and sum of every row's softmax (one pass over the keys).
+// cached prefix, then the sequence's own tokens up to its last row, and keeps a
+// running reference and sum of every row's softmax (one pass over the keys).
 //
 // A wavefront has 32 rows. K times Q^T leaves lane l with keys of row l % 32
 // alone: its maximum and sum need one exchange with the lane 32 away,
@@ -18,20 +18,21 @@
 // bits on the way, which is exact, and their scales never touch them: K's
 // multiplies the logit, and V's goes into the weight as an exponent,
 //   w_j s_j = 2^(x_j + log2 s_j - m),   sum of weights = sum_j (w_j s_j) / s_j,
-// with m near the running maximum of x_j + log2 s_j (peek_mfma.h), so weights times
+// with m near the maximum of x_j + log2 s_j so far, or here (peek_mfma.h), so weights times
 // scales stay within the range of either 16-bit type.
 //
 // Rows and keys past the end: rows are clamped to the last one and not
 // stored; keys are clamped to the last one and masked, so nothing outside the
 // sequence is read.
 //
-// Bound, over own tokens, by the matrix cores and the power they draw: 5 prompts of
-// up to 24000 tokens, 32 query heads of 128, 4.98 TFLOP: 4.37 to 4.5 ms, 1.1
-// PFLOP/s (a library product of 8192^3 reaches 1.24), the clock held at 1.8 to 1.9 GHz.
-// Over cached tokens by the vector instructions, which widen the codes too (8.5 to each
+// Bound, over own tokens, by the power that the products draw: 5 prompts of
+// up to 24000 tokens, 32 query heads of 128, 4.98 TFLOP: 4.35 to 4.55 ms, 1.1
+// PFLOP/s (a library product of 8192^3 reaches 1.24), the clock held at 1.8 to
+// 1.9 of 2.4 GHz, the matrix cores busy 55% of the cycles.
+// Over cached tokens by the vector instructions, which widen the codes too (8.7 to each
 // matrix instruction, four cycles each to its 32), and by the last workgroups:
 // 64 queries of up to 256 tokens after up to 7168, 40 query heads, 1.07 TFLOP:
-// 1.38 ms, 770 TFLOP/s. Few rows by the 2 us that 64 keys take a workgroup.
+// 1.38 to 1.42 ms, 760 TFLOP/s. Few rows by the 2 us that 64 keys take a workgroup.
 // With 128 rows to a workgroup, two to a compute unit, tiles are loaded twice as
 // often (467 TFLOP/s where 256 rows had 716); two groups of wavefronts a phase
 // apart gained 3% on the first and lost 9% on the second.
