@@ -144,15 +144,21 @@ def _arg(t, name: str, dtype=None, count: int | None = None):
 
 
 def _row_arg(t, name: str, dtype, n: int, *row: int):
-    """As _arg, of n rows that are each [*row] (a tensor of one dimension is taken by its elements): rows of any other
-    shape would be read and written at the wrong places."""
+    """As _arg, of n rows that are each [*row]: rows of another shape would be read and written at the wrong places.
+    More rows are taken, as are the same elements in other numbers of dimensions."""
     if t is None:
         return None
     if t.shape == (n, *row):
         return _arg(t, name, dtype)
-    if t.dim() > 1 and (t.dim() != 1 + len(row) or tuple(t.shape[1:]) != row or t.shape[0] < n):
-        raise ValueError(f"{name} must be {[n, *row]}, got {list(t.shape)}")
-    return _arg(t, name, dtype, n * math.prod(row))
+    each = math.prod(row)
+    if t.dim() > 1:
+        if t.dim() == 1 + len(row):
+            fits = tuple(t.shape[1:]) == row and t.shape[0] >= n
+        else:
+            fits = t.numel() == n * each or (math.prod(t.shape[1:]) == each and t.shape[0] >= n)
+        if not fits:
+            raise ValueError(f"{name} must be {[n, *row]}, got {list(t.shape)}")
+    return _arg(t, name, dtype, n * each)
 
 
 def _queue_n(offsets) -> int:

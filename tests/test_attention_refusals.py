@@ -24,7 +24,7 @@ def test_tables_whose_rows_overlap_are_refused():
 def test_rows_of_another_shape_are_refused():
     """Enough elements are not enough: a weight per block of another width would be read and written at wrong places."""
     f32 = torch.float32
-    for shape in ((3, 2, 9), (3, 2, 4), (3, 5, 2), (2, 2, 5), (6, 5), (3, 1, 2, 5)):
+    for shape in ((3, 2, 9), (3, 2, 4), (3, 5, 2), (2, 2, 5), (6, 9), (3, 18), (3, 1, 2, 9), (2, 10)):
         with pytest.raises(ValueError, match="mass must be"):
             P._row_arg(torch.zeros(shape), "mass", f32, 3, 2, 5)
     with pytest.raises(ValueError, match="at least 30"):
@@ -32,8 +32,10 @@ def test_rows_of_another_shape_are_refused():
     with pytest.raises(TypeError, match="mass must be"):
         P._row_arg(torch.zeros(3, 2, 5).double(), "mass", f32, 3, 2, 5)
     assert P._row_arg(None, "mass", f32, 3, 2, 5) is None
-    # the shape itself, more rows of it (a buffer for a larger batch), and one dimension get as far as the device check
-    for t in (torch.zeros(3, 2, 5), torch.zeros(4, 2, 5), torch.zeros(30), torch.zeros(64)):
+    # the shape itself, more rows of it (a buffer for a larger batch), and the same elements in other numbers of
+    # dimensions get as far as the device check
+    for t in (torch.zeros(3, 2, 5), torch.zeros(4, 2, 5), torch.zeros(30), torch.zeros(64), torch.zeros(6, 5),
+              torch.zeros(3, 10), torch.zeros(5, 10), torch.zeros(3, 1, 2, 5)):
         with pytest.raises(ValueError, match="device tensor"):
             P._row_arg(t, "mass", f32, 3, 2, 5)
 
