@@ -359,10 +359,9 @@ peek_status peek_offline_order(int32_t n, const int32_t* d_tokens, const int64_t
  *
  * Pool: pages[num_pages][2][kv_heads][block_size][head_dim] of 8-bit codes
  * (K at 0, V at 1), scales[num_pages][2][kv_heads] float32. A value is its
- * code times its scale. Scales of keys are finite, those of values 0 to 2^60, of
- * which smaller ones than 2^-60 (0 among them) count as 2^-60; peek_kv_append
- * leaves 2^-60 to 2^60 and asks for 0 to 2^60 of a block that it adds to
- * (PEEK_VALIDATE reports others). Formats: PEEK_TYPE_F8E4M3 (OCP e4m3) and
+ * code times its scale. Scales of keys are finite, those of values 0 (which
+ * counts as 2^-60) or 2^-60 to 2^60; peek_kv_append leaves 2^-60 to 2^60 and
+ * asks for 0 to 2^60 of a block that it adds to (PEEK_VALIDATE reports others). Formats: PEEK_TYPE_F8E4M3 (OCP e4m3) and
  * PEEK_TYPE_I8. block_size is a power of two in [4, 256], as of a block
  * table; head_dim is 64 or 128; kv_heads is in [1, 1024].
  *

@@ -13,13 +13,15 @@
 namespace peek {
 namespace kv {
 
-// Appended scales stay within 2^-60 .. 2^60, and attention brings V's there (a
-// pool may come with others, 0 among them): their reciprocals and logarithms are
-// then ordinary floats, and a weight times a scale cannot leave float32's range.
+// Scales stay within 2^-60 .. 2^60: their reciprocals and logarithms are then
+// ordinary floats, and a weight times a scale cannot leave float32's range. A
+// pool may come with others. V's scales of 0, and those that a logarithm or a
+// reciprocal might not have, count as 2^-60, or 2^100 where they are larger;
+// between these they are as they are, and so is NaN.
 constexpr float kScaleMin = 0x1p-60f;
 constexpr float kScaleMax = 0x1p60f;
-__device__ __forceinline__ float value_scale(float s) {     // (NaN stays)
-  return s < kScaleMin ? kScaleMin : s > kScaleMax ? kScaleMax : s;
+__device__ __forceinline__ float value_scale(float s) {
+  return s < 0x1p-100f ? kScaleMin : s > 0x1p100f ? 0x1p100f : s;
 }
 
 // A pool as kernels see it.

@@ -208,6 +208,30 @@ def check(gen, contexts, H, G, codes, scales, table, dtype, D, scale, q_spread=1
 
 
 @pytest.mark.parametrize("fmt", [F8, I8])
+@pytest.mark.parametrize("size", [2.0 ** -90, 2.0 ** -70, 2.0 ** 75])
+def test_values_of_a_size_that_no_append_leaves(size, fmt):
+    """A pool of another maker's, whose values are all that small or large, has its scales as they are."""
+    gen = torch.Generator().manual_seed(10)
+    contexts, H, G, D = [7, 90, 300], 2, 4, 64
+    codes, scales, table = make_pool(gen, contexts, H, 16, D, fmt)
+    scales[:, 1] *= size
+    q = torch.randn(len(contexts), H * G, D, generator=gen).to(BF)
+    out, lse = decode(q, codes, scales, table, contexts, D ** -0.5)
+    k, v = torch.randn(3, H, D, generator=gen).to(BF), (torch.randn(3, H, D, generator=gen) * size).to(BF)
+    pre, _ = prefill(q, k, v, [1] * 3, D ** -0.5, codes, scales, table, contexts)
+    most = R.most_of(scales[:, 1], fmt) if size > 1 else 0.0
+    for r, c in enumerate(contexts):
+        keys, values = R.cached(codes, scales, table[r], c)
+        want, wl, _, spread, reach = R.attend(q[r:r + 1], keys, values, D ** -0.5, c)
+        near(out[r:r + 1], want, R.out_bound(want, spread, reach, BF, c, most), f"decode of {c} tokens")
+        near(lse[r:r + 1], wl, R.lse_bound(wl, reach, D), f"decode's lse of {c} tokens")
+        if size < 1:      # (an own value counts as of scale 1: beside it a cached one of 2^75 leaves nothing)
+            want, wl, _, spread, reach = R.attend(q[r:r + 1], torch.cat([keys, k[r:r + 1].double()]),
+                                                  torch.cat([values, v[r:r + 1].double()]), D ** -0.5, c + 1)
+            near(pre[r:r + 1], want, R.out_bound(want, spread, reach, BF, c + 1, most), f"prefill after {c} tokens")
+
+
+@pytest.mark.parametrize("fmt", [F8, I8])
 def test_scales_at_their_limits(fmt):
     """The smallest and the largest scale that an append leaves (2^-60 of a block of zeros, 2^60), and a call's scale
     that takes a key's below the range of 32 bits."""
