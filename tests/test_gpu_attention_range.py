@@ -529,3 +529,38 @@ def test_lse_of_float16_rows_of_few_tokens(fmt):
         _, wl, _, _, reach = R.attend(q[r:r + 1], torch.cat([keys, k[r:r + 1].double()]),
                                       torch.cat([values, v[r:r + 1].double()]), 1e-3, c + 1)
         near(pre_lse[r:r + 1], wl, R.lse_bound(wl, reach, D), f"prefill's lse after {c} tokens")
+
+
+def test_small_weights_of_f16_rows_beside_a_middling_one():
+    """Tiles whose largest weight is 2^-14 of the row's, and has no value, while the others are 2^-22 of it: below
+    float16's normal numbers, and all of the output."""
+    D, T = 64, 64 * 40
+    logit = torch.full((T,), -15.25)
+    logit[0], logit[64::64] = 0.0, -9.75
+    value = torch.ones(T)
+    value[:64], value[64::64] = 0.0, 0.0
+    q = torch.zeros(64, 1, D, dtype=HF)
+    q[..., 0] = 1
+    k, v = torch.zeros(T + 64, 1, D, dtype=HF), torch.zeros(T + 64, 1, D, dtype=HF)
+    k[:T, 0, 0], v[:T] = logit, value[:, None, None].to(HF)
+    keys, values, one = k[:T].double(), v[:T].double(), torch.ones(T).double()
+    want, wl, w, spread, reach = R.attend(q[:1], keys, values, 1.0, T)
+    bound = faint_bound(want, spread, reach, HF, w[0], values[:, 0], one)
+    rows = torch.zeros(T, 1, D, dtype=HF)
+    rows[..., 0] = 1
+    out, lse = prefill(rows, k[:T], v[:T], [T], 1.0)
+    near(out[-1:], want, bound, "own tokens")
+    near(lse[-1:], wl, R.lse_bound(wl, reach, D), "own tokens' lse")
+    for B in (4, 16):
+        codes = torch.zeros(T // B, 2, 1, B, D)
+        codes[:, 0, 0, :, 0], codes[:, 1, 0] = (logit * 8).view(-1, B), value.view(-1, B, 1)
+        scales = torch.ones(T // B, 2, 1)
+        scales[:, 0] = 0.125
+        table = torch.arange(T // B, dtype=torch.int32)[None]
+        out, lse = decode(q[:1], codes.to(I8), scales, table, [T], 1.0)
+        near(out, want, bound, "decode")
+        near(lse, wl, R.lse_bound(wl, reach, D), "decode's lse")
+        own = torch.zeros(64, 1, D, dtype=HF)
+        own[..., 0] = -16
+        out, lse = prefill(q, own, torch.zeros_like(own), [64], 1.0, codes.to(I8), scales, table, [T])
+        near(out[:1] * float((1 + math.exp(-16 - wl[0, 0]))), want, bound, "cached tokens")
