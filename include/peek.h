@@ -531,6 +531,180 @@ peek_status peek_kv_evict(int32_t n, int32_t kv_heads, int32_t block_size, const
                           int32_t* d_table_out, float* d_mass_out, int32_t* d_freed, int32_t* d_num_freed,
                           void* d_workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * peek_rotate_append: what stands between a projection and its attention.
+ * Every head of q and k is normed and rotated by its token's position, and
+ * K and V go into the pages as peek_kv_append puts them there.
+ *
+ * Sequence r's rows of q, k and v are d_offsets[r] .. d_offsets[r+1] of
+ * num_tokens; its i-th row has position p = d_context[r] + i (a negative
+ * context counts as 0). For every head of q and of k, x its head_dim numbers:
+ *   norm (where a weight w is given, of the rows' type):
+ *     x = x / sqrt(mean(x^2) + eps) * w          (the squares summed in 32 bits)
+ *   rotation of the first rot_dim of them, pair i with the angle p * freq[i]
+ *   (a product in 64 bits), c and s its cosine and sine times magnitude:
+ *     (x_i, x_{i + rot_dim/2}) -> (x_i c - x_{i + rot_dim/2} s, x_{i + rot_dim/2} c + x_i s),
+ *     interleaved: the same of (x_2i, x_2i+1)
+ *   rounded to the rows' type once.
+ * d_q_out and d_k_out receive the rows; d_k_out may be NULL where the pages
+ * are all that is wanted of K. With a pool, the pages receive K as d_k_out
+ * would hold it and V as it is, by peek_kv_append's rules: the codes and
+ * scales are those of that call on d_k_out and d_v. Without a pool, d_v and
+ * the table are NULL. q_heads may be 0 (only K and V; d_q and d_q_out are
+ * not looked at), else any number: it need not be a multiple of kv_heads.
+ *
+ * d_q_out may be d_q and d_k_out may be d_k, with the same strides; beyond
+ * that no output shares an element with an input or another output. Rows in no
+ * sequence are left as they are. Asynchronous on `stream`; no workspace.
+ * n = 0 or num_tokens = 0 is a no-op.
+ * Errors: INVALID_ARGUMENT, DEVICE.
+ * ---------------------------------------------------------------------- */
+typedef struct peek_rotary {
+  const double* d_freq;  /* [rot_dim / 2], radians a token */
+  int32_t rot_dim;       /* multiple of 16, 0 (no rotation) to head_dim */
+  int32_t interleaved;   /* 0: pairs (i, i + rot_dim / 2); else (2i, 2i + 1) */
+  float magnitude;       /* times the rotated numbers; finite */
+  float eps;             /* 0 or more */
+  const void* d_q_norm;  /* [head_dim] of the rows' type, 16-byte aligned, or NULL: no norm */
+  const void* d_k_norm;
+} peek_rotary;
+
+peek_status peek_rotate_append(const peek_kv_pool* pool, int32_t n, int64_t num_tokens, int32_t type, int32_t q_heads,
+                               int32_t kv_heads, int32_t head_dim, const peek_rotary* rotary, const void* d_q,
+                               int64_t q_token_stride, int64_t q_head_stride, const void* d_k, int64_t k_token_stride,
+                               int64_t k_head_stride, const void* d_v, int64_t v_token_stride, int64_t v_head_stride,
+                               const int64_t* d_offsets, const int32_t* d_context, const int32_t* d_block_table,
+                               int32_t max_blocks, int64_t table_stride, void* d_q_out, int64_t q_out_token_stride,
+                               int64_t q_out_head_stride, void* d_k_out, int64_t k_out_token_stride,
+                               int64_t k_out_head_stride, void* stream);
+
+/* Frequencies for it, on the host: out[i], i < rot_dim / 2 (rot_dim even, 2 to
+ * 128), from f_i = base^(-2i / rot_dim), for contexts `factor` times as long
+ * as those trained on:
+ *   PLAIN   f_i
+ *   LINEAR  f_i / factor
+ *   BASE    f_i with base * factor^(rot_dim / (rot_dim - 2))
+ *   TURNS   f_i g + f_i / factor (1 - g), g = (trained f_i / (2 pi) - low) /
+ *           (high - low) kept within 0 .. 1: by the turns over `trained` tokens
+ *   RAMP    the same with g falling evenly over the pairs, from 1 at the pair
+ *           that makes `high` turns (rounded down, 0 or more) to 0 at that of `low` turns (rounded up,
+ *           rot_dim - 1 at most)
+ * What a kind does not name is not looked at. Errors: INVALID_ARGUMENT. */
+typedef enum peek_rotary_scaling {
+  PEEK_ROTARY_PLAIN = 0,
+  PEEK_ROTARY_LINEAR = 1,
+  PEEK_ROTARY_BASE = 2,
+  PEEK_ROTARY_TURNS = 3,
+  PEEK_ROTARY_RAMP = 4
+} peek_rotary_scaling;
+
+peek_status peek_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double trained,
+                                    double low, double high, double* out);
+
+/* ------------------------------------------------------------------------
+ * peek_kv_read: tokens of the cache back as rows of 16 bits. Rows
+ * d_offsets[r] .. d_offsets[r+1] of d_k_out and d_v_out receive sequence r's
+ * tokens from d_first[r] on (negative: 0), code times scale in 32 bits,
+ * rounded to the rows' type once. Rows in no sequence, and those of tokens that
+ * the table cannot hold, are left as they are. The outputs share no element.
+ * Asynchronous on `stream`; no workspace. n = 0 or num_tokens = 0 is a no-op.
+ * Errors: INVALID_ARGUMENT, DEVICE.
+ * ---------------------------------------------------------------------- */
+peek_status peek_kv_read(const peek_kv_pool* pool, int32_t n, int64_t num_tokens, int32_t type,
+                         const int64_t* d_offsets, const int32_t* d_first, const int32_t* d_block_table,
+                         int32_t max_blocks, int64_t table_stride, void* d_k_out, int64_t k_token_stride,
+                         int64_t k_head_stride, void* d_v_out, int64_t v_token_stride, int64_t v_head_stride,
+                         void* stream);
+
+/* ------------------------------------------------------------------------
+ * peek_shared_decode_attention: peek_decode_attention (without masses) of a
+ * batch whose sequences have their first tokens in common, in groups (the
+ * clusters of peek_queue_signals): what a group shares is read once for all of
+ * its members.
+ *
+ * Group g is the sequences d_members[i], i from d_group_offsets[g] up to
+ * d_group_offsets[g+1] (int32[groups + 1], from 0, non-decreasing, to n); d_members
+ * int32[n] names every sequence once, NULL stands for 0, 1, ... n - 1. The first
+ * d_shared[g] tokens of its members, cut to whole blocks, are the same: they
+ * are read from the pages that the table names for the group's first member. A
+ * member with fewer tokens than that shares nothing and reads its own pages.
+ * Sequences past the last group's end share nothing either. Rows of sequences
+ * that d_members does not name are left as they are, and so are the outputs of
+ * an id outside 0 .. n - 1. Everything else is as in peek_decode_attention.
+ * Scratch comes only from d_workspace (device, 256-byte aligned, at least
+ * peek_shared_decode_attention_workspace bytes). Asynchronous on `stream`.
+ * n = 0 is a no-op.
+ * Errors: INVALID_ARGUMENT, WORKSPACE_TOO_SMALL, DEVICE.
+ * ---------------------------------------------------------------------- */
+size_t peek_shared_decode_attention_workspace(const peek_kv_pool* pool, int32_t n, int32_t q_heads, int32_t max_blocks,
+                                              int32_t groups);
+
+peek_status peek_shared_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t type, int32_t q_heads,
+                                         const void* d_q, int64_t q_token_stride, int64_t q_head_stride,
+                                         const int32_t* d_context, const int32_t* d_block_table, int32_t max_blocks,
+                                         int64_t table_stride, int32_t groups, const int32_t* d_members,
+                                         const int32_t* d_group_offsets, const int32_t* d_shared, float scale,
+                                         void* d_out, int64_t out_token_stride, int64_t out_head_stride, float* d_lse,
+                                         void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Attention of single tokens over the blocks of a long context that promise
+ * the largest logits, chosen for every sequence and kv head.
+ *
+ * peek_kv_bounds: d_bounds int8[num_pages][kv_heads][2][head_dim], 16-byte
+ * aligned, receives for every block of sequence r that holds one of its tokens
+ * d_first[r] .. d_context[r] - 1 (d_first NULL or negative: from 0 on) the
+ * largest (at 0) and the smallest (at 1) of the codes of its keys up to
+ * d_context[r], element by element: of int8 codes themselves, of float8 values v
+ * the next whole number above, and below, v / 4 (a NaN is the largest of its sign); within
+ * -127 .. 127; where the keys' scale is negative, those of the negated codes. After
+ * an append, first = the context before it brings the bounds up to date.
+ * Asynchronous on `stream`; no workspace. n = 0 is a no-op.
+ * Errors: INVALID_ARGUMENT, DEVICE.
+ *
+ * peek_block_select: a block's score for sequence r and kv head h, in 32 bits:
+ *   a = the largest finite magnitude of a query row q, a = m 2^e with
+ *       0.5 <= m < 1 (e = 0 for a = 0), w_d = q_d 2^(7 - e) rounded to the nearest whole
+ *       number, ties to even, kept within -127 .. 127 (NaN: 0)
+ *   score = |scale of the block's keys| (times 4 for float8) * max over the kv
+ *       head's query rows of 2^(e - 7) * sum_d max(w_d hi_d, w_d lo_d)
+ * which, times the attention's scale (above 0; for one below, give -q), no logit of
+ * the block is above, but for the rounding of w. Of the nb =
+ * ceil(context / block_size) blocks the first `sink` and the last `recent` (>= 1) stay,
+ * and of the others those of the largest scores (NaN above all; equal scores by position),
+ * `keep` in all, or all nb if there are no more:
+ *   d_table_out   int32[n][kv_heads][keep]: their entries of the table, in order of position, then -1
+ *   d_context_out int32[n][kv_heads]: the tokens in them
+ * sink + recent <= keep; keep * block_size below 2^31. Outputs share no element
+ * with inputs or each other. Scratch comes only from d_workspace (device,
+ * 256-byte aligned, at least peek_block_select_workspace bytes). Asynchronous
+ * on `stream`. n = 0 is a no-op.
+ * Errors: INVALID_ARGUMENT, WORKSPACE_TOO_SMALL, DEVICE.
+ *
+ * peek_sparse_decode_attention: peek_decode_attention (without masses) with a
+ * table and a length for every kv head, as peek_block_select leaves them:
+ * d_block_table int32[n][kv_heads][keep], d_context int32[n][kv_heads].
+ * ---------------------------------------------------------------------- */
+peek_status peek_kv_bounds(const peek_kv_pool* pool, int32_t n, const int32_t* d_first, const int32_t* d_context,
+                           const int32_t* d_block_table, int32_t max_blocks, int64_t table_stride, int8_t* d_bounds,
+                           void* stream);
+
+size_t peek_block_select_workspace(const peek_kv_pool* pool, int32_t n, int32_t max_blocks);
+
+peek_status peek_block_select(const peek_kv_pool* pool, const int8_t* d_bounds, int32_t n, int32_t type,
+                              int32_t q_heads, const void* d_q, int64_t q_token_stride, int64_t q_head_stride,
+                              const int32_t* d_context, const int32_t* d_block_table, int32_t max_blocks,
+                              int64_t table_stride, int32_t keep, int32_t sink, int32_t recent, int32_t* d_context_out,
+                              int32_t* d_table_out, void* d_workspace, size_t workspace_bytes, void* stream);
+
+size_t peek_sparse_decode_attention_workspace(const peek_kv_pool* pool, int32_t n, int32_t q_heads, int32_t keep);
+
+peek_status peek_sparse_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t type, int32_t q_heads,
+                                         const void* d_q, int64_t q_token_stride, int64_t q_head_stride,
+                                         const int32_t* d_context, const int32_t* d_block_table, int32_t keep,
+                                         float scale, void* d_out, int64_t out_token_stride, int64_t out_head_stride,
+                                         float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -91,6 +91,27 @@ EXPORTS = [
     ("peek_kv_evict", ctypes.c_int,
      [_i32, _i32, _i32, _vp, _vp, _i32, _i64, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t,
       _vp]),
+    ("peek_rotate_append", ctypes.c_int,
+     [_vp, _i32, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp,
+      _i32, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp]),
+    ("peek_rotary_frequencies", ctypes.c_int,
+     [_i32, ctypes.c_double, _i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+      ctypes.POINTER(ctypes.c_double)]),
+    ("peek_kv_read", ctypes.c_int,
+     [_vp, _i32, _i64, _i32, _vp, _vp, _vp, _i32, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp]),
+    ("peek_shared_decode_attention_workspace", ctypes.c_size_t, [_vp, _i32, _i32, _i32, _i32]),
+    ("peek_shared_decode_attention", ctypes.c_int,
+     [_vp, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _vp, _i32, _i64, _i32, _vp, _vp, _vp, ctypes.c_float, _vp, _i64,
+      _i64, _vp, _vp, ctypes.c_size_t, _vp]),
+    ("peek_kv_bounds", ctypes.c_int, [_vp, _i32, _vp, _vp, _vp, _i32, _i64, _vp, _vp]),
+    ("peek_block_select_workspace", ctypes.c_size_t, [_vp, _i32, _i32]),
+    ("peek_block_select", ctypes.c_int,
+     [_vp, _vp, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _vp, _i32, _i64, _i32, _i32, _i32, _vp, _vp, _vp,
+      ctypes.c_size_t, _vp]),
+    ("peek_sparse_decode_attention_workspace", ctypes.c_size_t, [_vp, _i32, _i32, _i32]),
+    ("peek_sparse_decode_attention", ctypes.c_int,
+     [_vp, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _vp, _i32, ctypes.c_float, _vp, _i64, _i64, _vp, _vp,
+      ctypes.c_size_t, _vp]),
 ]
 
 for _name, _res, _args in EXPORTS:
@@ -595,3 +616,178 @@ def peek_kv_evict(context, block_table, mass, keep, block_size: int, sink: int, 
                               _row_arg(mass_out, "mass_out", torch.float32, n, heads, width),
                               _row_arg(freed, "freed", i32, n, width), _arg(num_freed, "num_freed", i32, n),
                               *_ws(workspace), _stream(stream)))
+
+
+PEEK_ROTARY_PLAIN = 0
+PEEK_ROTARY_LINEAR = 1
+PEEK_ROTARY_BASE = 2
+PEEK_ROTARY_TURNS = 3
+PEEK_ROTARY_RAMP = 4
+
+
+class _RotaryStruct(ctypes.Structure):
+    _fields_ = [("d_freq", _vp), ("rot_dim", _i32), ("interleaved", _i32), ("magnitude", ctypes.c_float),
+                ("eps", ctypes.c_float), ("d_q_norm", _vp), ("d_k_norm", _vp)]
+
+
+def _here(*tensors):
+    """Refuses tensors of a device other than the current one, where the call's kernels run."""
+    now = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != now:
+            raise ValueError(f"tensors must be on the current device (cuda:{now}), got one on {t.device}")
+
+
+def _exact_arg(t, name: str, dtype, *shape: int):
+    """As _arg, of this shape and no other."""
+    if t is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return _arg(t, name, dtype)
+
+
+def peek_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = PEEK_ROTARY_PLAIN, factor: float = 1.0,
+                            trained: float = 0.0, low: float = 1.0, high: float = 4.0) -> np.ndarray:
+    """Radians a token of every pair, float64[rot_dim / 2], on the host: base ** (-2 i / rot_dim), scaled for contexts
+    `factor` times as long as trained (PEEK_ROTARY_LINEAR, _BASE, _TURNS, _RAMP)."""
+    out = np.empty(max(0, int(rot_dim)) // 2, dtype=np.float64)
+    _check(_lib.peek_rotary_frequencies(int(rot_dim), base, int(scaling), factor, trained, low, high,
+                                        out.ctypes.data_as(ctypes.POINTER(ctypes.c_double))))
+    return out
+
+
+def peek_rotate_append(q, k, v, offsets, context, freq, q_out, k_out=None, pool: KVPool | None = None,
+                       block_table=None, interleaved: bool = False, magnitude: float = 1.0, q_norm=None, k_norm=None,
+                       eps: float = 1e-6, stream=None):
+    """Norms and rotates every head of q and k by its token's position, and appends K and V to the pool. q, q_out
+    [tokens, q_heads, head_dim] (both None: only K and V), k, v, k_out [tokens, kv_heads, head_dim] (any token and head
+    strides; an output may be its own input), offsets int64[n+1], context int32[n] (tokens before), freq float64
+    [rot_dim / 2] or None, q_norm, k_norm [head_dim] of the rows' type or None. Without a pool (v and block_table None)
+    only q_out and k_out are written."""
+    n = _queue_n(offsets)
+    kind, dtype = _row_type(k, "k"), k.dtype
+    if k.dim() != 3:
+        raise ValueError("k must be [tokens, heads, head_dim]")
+    tokens, kv_heads, dim = k.shape
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out must be given together")
+    if (pool is None) != (v is None) or (pool is None) != (block_table is None):
+        raise ValueError("pool, v and block_table must be given together")
+    if pool is None and k_out is None:
+        raise ValueError("k needs a pool or k_out")
+    q_heads = 0 if q is None else q.shape[1] if q.dim() == 3 else -1
+    none = (None, 0, 0)
+    rows_q = none if q is None else _rows(q, "q", dtype, None, dim, tokens)
+    rows_q_out = none if q is None else _rows(q_out, "q_out", dtype, q_heads, dim, tokens)
+    rows_k = _rows(k, "k", dtype)
+    rows_v = none if v is None else _rows(v, "v", dtype, kv_heads, dim, tokens)
+    rows_k_out = none if k_out is None else _rows(k_out, "k_out", dtype, kv_heads, dim, tokens)
+    for out, rows_out, of, rows in ((q_out, rows_q_out, q, rows_q), (k_out, rows_k_out, k, rows_k)):
+        if out is not None and rows_out[0] == rows[0] and out.stride() != of.stride():
+            raise ValueError("an output in place of its input must have its strides")
+    rot = 0 if freq is None else 2 * freq.numel()
+    rotary = _RotaryStruct(_arg(freq, "freq", torch.float64), rot, int(bool(interleaved)), magnitude, eps,
+                           _exact_arg(q_norm, "q_norm", dtype, dim), _exact_arg(k_norm, "k_norm", dtype, dim))
+    table = none if block_table is None else _table(block_table, n)
+    at, ctx = _arg(offsets, "offsets"), _arg(context, "context", torch.int32, n)
+    _here(q, k, v, offsets, context, freq, q_out, k_out, block_table, q_norm, k_norm, pool and pool.pages)
+    _check(_lib.peek_rotate_append(None if pool is None else pool._ref, n, tokens, kind, q_heads, kv_heads, dim,
+                                   ctypes.addressof(rotary), *rows_q, *rows_k, *rows_v, at, ctx, *table, *rows_q_out,
+                                   *rows_k_out, _stream(stream)))
+
+
+def peek_kv_read(pool: KVPool, offsets, first, block_table, k_out, v_out, stream=None):
+    """Tokens of the cache as rows: k_out, v_out [tokens, kv_heads, head_dim] (bfloat16 or float16, any token and head
+    strides) receive, in rows offsets[r] .. offsets[r+1] (int64[n+1]), sequence r's tokens from first[r] on (int32[n])."""
+    n = _queue_n(offsets)
+    kind = _row_type(k_out, "k_out")
+    table = _table(block_table, n)
+    rows_k = _rows(k_out, "k_out", k_out.dtype, pool.kv_heads, pool.head_dim)
+    rows_v = _rows(v_out, "v_out", k_out.dtype, pool.kv_heads, pool.head_dim, k_out.shape[0])
+    at, begin = _arg(offsets, "offsets"), _arg(first, "first", torch.int32, n)
+    _here(pool.pages, offsets, first, block_table, k_out, v_out)
+    _check(_lib.peek_kv_read(pool._ref, n, k_out.shape[0], kind, at, begin, *table, *rows_k, *rows_v, _stream(stream)))
+
+
+def peek_shared_decode_attention_workspace(pool: KVPool, n: int, q_heads: int, max_blocks: int, groups: int) -> int:
+    return int(_lib.peek_shared_decode_attention_workspace(pool._ref, int(n), int(q_heads), int(max_blocks),
+                                                           int(groups)))
+
+
+def peek_shared_decode_attention(pool: KVPool, q, context, block_table, group_offsets, shared, out, workspace,
+                                 members=None, scale: float | None = None, lse=None, stream=None):
+    """peek_decode_attention where groups of sequences have their first tokens in common, which are read once a group.
+    Group g: the sequences members[group_offsets[g]] up to members[group_offsets[g + 1]] (members int32[n], None: in
+    order; group_offsets int32[groups + 1]), which share their first shared[g] tokens (int32[groups]), read from the
+    pages of the group's first."""
+    n = q.shape[0]
+    kind = _row_type(q, "q")
+    q_heads = q.shape[1] if q.dim() == 3 else 0
+    if group_offsets.dim() != 1 or group_offsets.numel() < 1:
+        raise ValueError("group_offsets must be 1-D, of groups + 1 entries")
+    groups, i32 = group_offsets.shape[0] - 1, torch.int32
+    table = _table(block_table, n)
+    _here(pool.pages, q, context, block_table, group_offsets, shared, out, workspace, members, lse)
+    _check(_lib.peek_shared_decode_attention(
+        pool._ref, n, kind, q_heads, *_rows(q, "q", q.dtype, None, pool.head_dim), _arg(context, "context", i32, n),
+        *table, groups, _arg(members, "members", i32, n), _arg(group_offsets, "group_offsets", i32),
+        _arg(shared, "shared", i32, groups), pool.head_dim ** -0.5 if scale is None else scale,
+        *_rows(out, "out", q.dtype, q_heads, pool.head_dim, n), _row_arg(lse, "lse", torch.float32, n, q_heads),
+        *_ws(workspace), _stream(stream)))
+
+
+def peek_kv_bounds(pool: KVPool, first, context, block_table, bounds, stream=None):
+    """The largest and smallest key code of every block that holds one of sequence r's tokens first[r] .. context[r] - 1
+    (first None: from 0 on), into bounds int8[num_pages, kv_heads, 2, head_dim]."""
+    n = context.shape[0]
+    table = _table(block_table, n)
+    at = _exact_arg(bounds, "bounds", torch.int8, pool.num_pages, pool.kv_heads, 2, pool.head_dim)
+    begin, ctx = _arg(first, "first", torch.int32, n), _arg(context, "context", torch.int32, n)
+    _here(pool.pages, first, context, block_table, bounds)
+    _check(_lib.peek_kv_bounds(pool._ref, n, begin, ctx, *table, at, _stream(stream)))
+
+
+def peek_block_select_workspace(pool: KVPool, n: int, max_blocks: int) -> int:
+    return int(_lib.peek_block_select_workspace(pool._ref, int(n), int(max_blocks)))
+
+
+def peek_block_select(pool: KVPool, bounds, q, context, block_table, sink: int, recent: int, context_out,
+                      block_table_out, workspace, stream=None):
+    """The blocks whose bounds promise the largest logits to each sequence's queries, for every kv head: block_table_out
+    int32[n, kv_heads, keep] receives keep entries of block_table in order (the first `sink`, the last `recent`, and
+    the best of the others), context_out int32[n, kv_heads] the tokens in them. q [n, q_heads, head_dim]."""
+    n = q.shape[0]
+    kind = _row_type(q, "q")
+    q_heads = q.shape[1] if q.dim() == 3 else 0
+    table = _table(block_table, n)
+    if block_table_out.dim() != 3:
+        raise ValueError("block_table_out must be [n, kv_heads, keep]")
+    keep, i32 = block_table_out.shape[2], torch.int32
+    at = _exact_arg(bounds, "bounds", torch.int8, pool.num_pages, pool.kv_heads, 2, pool.head_dim)
+    _here(pool.pages, bounds, q, context, block_table, context_out, block_table_out, workspace)
+    _check(_lib.peek_block_select(
+        pool._ref, at, n, kind, q_heads, *_rows(q, "q", q.dtype, None, pool.head_dim), _arg(context, "context", i32, n),
+        *table, keep, int(sink), int(recent), _exact_arg(context_out, "context_out", i32, n, pool.kv_heads),
+        _exact_arg(block_table_out, "block_table_out", i32, n, pool.kv_heads, keep), *_ws(workspace), _stream(stream)))
+
+
+def peek_sparse_decode_attention_workspace(pool: KVPool, n: int, q_heads: int, keep: int) -> int:
+    return int(_lib.peek_sparse_decode_attention_workspace(pool._ref, int(n), int(q_heads), int(keep)))
+
+
+def peek_sparse_decode_attention(pool: KVPool, q, context, block_table, out, workspace, scale: float | None = None,
+                                 lse=None, stream=None):
+    """peek_decode_attention with a table and a length for every kv head, as peek_block_select leaves them: block_table
+    int32[n, kv_heads, keep], context int32[n, kv_heads]."""
+    n = q.shape[0]
+    kind = _row_type(q, "q")
+    q_heads = q.shape[1] if q.dim() == 3 else 0
+    if block_table.dim() != 3:
+        raise ValueError("block_table must be [n, kv_heads, keep]")
+    keep, i32 = block_table.shape[2], torch.int32
+    _here(pool.pages, q, context, block_table, out, workspace, lse)
+    _check(_lib.peek_sparse_decode_attention(
+        pool._ref, n, kind, q_heads, *_rows(q, "q", q.dtype, None, pool.head_dim),
+        _exact_arg(context, "context", i32, n, pool.kv_heads),
+        _exact_arg(block_table, "block_table", i32, n, pool.kv_heads, keep), keep,
+        pool.head_dim ** -0.5 if scale is None else scale, *_rows(out, "out", q.dtype, q_heads, pool.head_dim, n),
+        _row_arg(lse, "lse", torch.float32, n, q_heads), *_ws(workspace), _stream(stream)))

@@ -21,7 +21,8 @@ FORCED = ["-DPEEK_SAMPLE_SEED=0", "-DPEEK_WAIT_SPINS=0"]
 BUILD_DIR = os.path.join(HERE, "_build")
 
 # Nothing of these depends on FORCED: compiled once, linked into both libraries
-UNFORCED = ["peek_kv.hip", "peek_kv_evict.hip", "peek_prefill.hip", "peek_decode.hip"]
+UNFORCED = ["peek_kv.hip", "peek_kv_evict.hip", "peek_prefill.hip", "peek_decode.hip", "peek_rotate.hip",
+            "peek_select.hip", "peek_shared.hip"]
 SOURCES = ["peek_host.hip", "peek_walk.hip", "peek_signals.hip", "peek_evict.hip", "peek_blocks.hip",
            "peek_noalloc.hip", *UNFORCED]
 
@@ -64,7 +65,7 @@ def build(verbose: bool = False) -> str:
             if made is forced and src in UNFORCED:
                 continue
             jobs.append([HIPCC, *FLAGS, *defines, "-c", os.path.join(CSRC, src), "-o", obj])
-    with ThreadPoolExecutor(4) as pool:
+    with ThreadPoolExecutor(8) as pool:
         list(pool.map(lambda cmd: _run(cmd, verbose), jobs))
     _link(LIB, objs, verbose)
     _link(FORCED_LIB, forced, verbose)

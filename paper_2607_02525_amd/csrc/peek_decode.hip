@@ -56,8 +56,9 @@ constexpr int kMaxChunk = 4096;                  // tokens of a workgroup, at mo
 struct Decode {
   Pool pool;
   Rows q;
-  const int32_t* context;
-  Table table;
+  const int32_t* context;      // of sequence r and kv head h at r * context_row + h * context_head
+  Table table;                 // kv head h's row `table_head` entries after the one before
+  int64_t context_row, context_head, table_head;
   uint16_t* out;
   int64_t out_token, out_head;
   float* lse;
@@ -80,32 +81,9 @@ struct alignas(16) Block {
   uint32_t page;
 };
 
-// Over the lanes that hold the same row: l, l ^ 16, l ^ 32, l ^ 48.
-__device__ __forceinline__ float swap16_max(float x) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
-}
-__device__ __forceinline__ float swap16_sum(float x) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
-}
-
 // Chunks of a sequence (lengths up to 2^31 - 1).
 __device__ __forceinline__ int32_t parts_of(int32_t tokens, int32_t chunk) {
   return tokens > 0 ? (tokens - 1) / chunk + 1 : 0;
-}
-
-// Four tokens of four bytes each -> four bytes' worth of four tokens.
-__device__ __forceinline__ void turn4(const uint32_t a, const uint32_t b, const uint32_t c, const uint32_t d,
-                                      uint32_t* r) {
-  const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602);
-  const uint32_t cd0 = __builtin_amdgcn_perm(d, c, 0x05010400), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602);
-  r[0] = __builtin_amdgcn_perm(cd0, ab0, 0x05040100);
-  r[1] = __builtin_amdgcn_perm(cd0, ab0, 0x07060302);
-  r[2] = __builtin_amdgcn_perm(cd1, ab1, 0x05040100);
-  r[3] = __builtin_amdgcn_perm(cd1, ab1, 0x07060302);
 }
 
 // WIDE: blocks of 16 tokens or more. Sixteen tokens that start at a multiple
@@ -130,7 +108,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
   unit /= a.row_tiles;
   const int32_t split = unit % a.splits, r = unit / a.splits;
   const int32_t q_heads = a.group * a.pool.heads, lb = a.pool.log_block;
-  const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb);
+  const int32_t held = kv::clip_tokens(a.context[r * a.context_row + head * a.context_head], a.table.width, lb);
   const int32_t from = split * a.chunk, to = from + min(a.chunk, held - from);   // (no sum passes `held`, nor 2^31)
   const int32_t row = row_tile * kRows + (lane & 15), rows = min(kRows, a.group - row_tile * kRows);
   if (from >= to) {
@@ -144,10 +122,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
   }
 
   const int32_t block0 = from >> lb;
+  const int32_t* const row_ids = a.table.ids + r * a.table.stride + head * a.table_head;
   if constexpr (!WIDE) {
     const int32_t blocks = ((to - 1) >> lb) - block0 + 1;
     for (int32_t i = tid; i < blocks; i += kThreads) {
-      const uint32_t page = kv::page_of(a.table, a.pool, r, block0 + i);
+      const uint32_t id = (uint32_t)row_ids[block0 + i], page = id < a.pool.num_pages ? id : 0u;
       const int64_t at = (int64_t)page * 2 * a.pool.heads + head;
       const float k = a.pool.scales[at], v = kv::value_scale(a.pool.scales[at + a.pool.heads]);
       s_block[i] = Block{k * a.scale, log2_fast(v), __builtin_amdgcn_rcpf(v), page};
@@ -178,7 +157,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
   // Where the 16 tokens from t on (WIDE), or this lane's token t, begin.
   typedef const __attribute__((address_space(4))) int32_t* const_ints;
   typedef const __attribute__((address_space(4))) float* const_floats;
-  const const_ints ids = (const_ints)(a.table.ids + (int64_t)r * a.table.stride);
+  const const_ints ids = (const_ints)row_ids;
   const const_floats scales = (const_floats)a.pool.scales;
   const uint8_t* base[2];           // WIDE: of the next tile's halves
   int32_t limit[2];                 // and the last of their 16 tokens that there is
@@ -381,7 +360,8 @@ __global__ __launch_bounds__(THREADS) void k_decode_join(Decode a, uint32_t outs
     const int64_t at = (int64_t)blockIdx.x * (kWaves / WAVES) + wave / WAVES;
     if (at >= (int64_t)a.n * q_heads) return;
     const int32_t r = (int32_t)(at / q_heads), q_head = (int32_t)(at % q_heads);
-    const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb), parts = parts_of(held, a.chunk);
+    const int32_t tokens = a.context[r * a.context_row + q_head / a.group * a.context_head];
+    const int32_t held = kv::clip_tokens(tokens, a.table.width, lb), parts = parts_of(held, a.chunk);
     if (parts < 2) return;
     float l2;
     join_parts<TYPE, D, WAVES>(a.part_out + at * a.splits * D, a.part_lse + at * a.splits, parts, wave % WAVES, lane,
@@ -458,6 +438,78 @@ Plan plan_for(const peek_kv_pool& pool, int32_t n, int32_t q_heads, int32_t max_
   return p;
 }
 
+// Both entry points, once their tables and lengths are where the kernels look for them.
+peek_status decode(Decode& a, const peek_kv_pool* pool, int32_t n, int32_t type, int32_t q_heads, const void* d_q,
+                   int64_t q_token_stride, int64_t q_head_stride, float scale, void* d_out, int64_t out_token_stride,
+                   int64_t out_head_stride, float* d_lse, void* d_workspace, size_t workspace_bytes, hipStream_t st) {
+  peek_status s = check_pool(pool, &a.pool);
+  if (s != PEEK_OK) return s;
+  if (n < 0) return fail(PEEK_ERR_INVALID_ARGUMENT, "n must be >= 0 (got %d)", n);
+  s = check_heads(type, q_heads, a.pool.heads, scale);
+  if (s != PEEK_OK) return s;
+  const int32_t max_blocks = a.table.width;
+  s = check_table(a.table.ids, max_blocks, a.table.stride, pool->block_size);
+  if (s != PEEK_OK) return s;
+  if (a.mass_in && !a.mass) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_mass_in needs d_mass");
+  if (n == 0) return PEEK_OK;
+  if ((s = check_rows("d_q", d_q, q_token_stride, q_head_stride)) != PEEK_OK) return s;
+  s = check_out_rows("d_out", d_out, out_token_stride, out_head_stride, n, q_heads, pool->head_dim);
+  if (s != PEEK_OK) return s;
+  if (!a.context) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_context must not be NULL");
+  const Plan p = plan_for(*pool, n, q_heads, max_blocks, a.mass != nullptr);
+  s = check_workspace(d_workspace, workspace_bytes, p.bytes);
+  if (s != PEEK_OK) return s;
+  a.n = n;
+  a.group = q_heads / a.pool.heads;
+  a.row_tiles = (a.group + kRows - 1) / kRows;
+  const int64_t groups = (int64_t)n * a.pool.heads * a.row_tiles * p.splits;
+  const bool many = p.splits >= kManyParts;
+  const int32_t threads = many ? 1024 : kThreads, rows = many ? 1 : kWaves;      // of a joining workgroup
+  const int64_t outs = p.splits > 1 ? ((int64_t)n * q_heads + rows - 1) / rows : 0;
+  const int64_t masses = a.mass ? (int64_t)n * a.pool.heads * ((max_blocks + threads - 1) / threads) : 0;
+  if (groups >= (1 << 24) || outs + masses >= (1 << 24))
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
+  // (with a table for every head, these are sequences of their own)
+  const bool by_head = a.context_head != 0;
+  s = validate_kv(by_head ? n * a.pool.heads : n, nullptr, 0, a.context, false, a.table.ids, max_blocks,
+                  by_head ? a.table_head : a.table.stride, pool->block_size, &a.pool, st);
+  if (s != PEEK_OK) return s;
+  char* ws = (char*)d_workspace;
+  a.q = Rows{d_q, q_token_stride, q_head_stride};
+  a.out = (uint16_t*)d_out;
+  a.out_token = out_token_stride;
+  a.out_head = out_head_stride;
+  a.lse = d_lse;
+  a.part_out = (float*)(ws + p.part_out);
+  a.part_lse = (float*)(ws + p.part_lse);
+  a.weights = (float*)(ws + p.weights);
+  a.grains = p.grains;
+  a.log_grain = p.log_grain;
+  a.chunk = p.chunk;
+  a.splits = p.splits;
+  set_scale(scale, &a.scale, &a.q_flip, &a.q_mask);
+  with_types(type, pool->type, pool->head_dim, [&](auto t, auto m, auto d) {
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kThreads), 0, st, a); };
+    if (a.pool.log_block >= 4) {
+      a.mass ? go(k_decode<t(), m(), d(), true, true>) : go(k_decode<t(), m(), d(), false, true>);
+    } else {
+      a.mass ? go(k_decode<t(), m(), d(), true, false>) : go(k_decode<t(), m(), d(), false, false>);
+    }
+  });
+  hipError_t err = hipGetLastError();
+  if (err == hipSuccess && outs + masses > 0) {
+    with_types(type, PEEK_TYPE_I8, pool->head_dim, [&](auto t, auto, auto d) {
+      auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(outs + masses)), dim3(threads), 0, st, a, (uint32_t)outs);
+      };
+      many ? go(k_decode_join<t(), d(), 1024, 16>) : go(k_decode_join<t(), d(), kThreads, 1>);
+    });
+    err = hipGetLastError();
+  }
+  if (err != hipSuccess) return fail(PEEK_ERR_DEVICE, "decode launch failed: %s", hipGetErrorString(err));
+  return PEEK_OK;
+}
+
 }  // namespace
 }  // namespace peek
 
@@ -481,74 +533,36 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
   return guarded([&]() -> peek_status {
     clear_error();
     Decode a{};
-    peek_status s = check_pool(pool, &a.pool);
-    if (s != PEEK_OK) return s;
-    if (n < 0) return fail(PEEK_ERR_INVALID_ARGUMENT, "n must be >= 0 (got %d)", n);
-    s = check_heads(type, q_heads, a.pool.heads, scale);
-    if (s != PEEK_OK) return s;
-    s = check_table(d_block_table, max_blocks, table_stride, pool->block_size);
-    if (s != PEEK_OK) return s;
-    if (d_mass_in && !d_mass) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_mass_in needs d_mass");
-    if (n == 0) return PEEK_OK;
-    if ((s = check_rows("d_q", d_q, q_token_stride, q_head_stride)) != PEEK_OK) return s;
-    s = check_out_rows("d_out", d_out, out_token_stride, out_head_stride, n, q_heads, pool->head_dim);
-    if (s != PEEK_OK) return s;
-    if (!d_context) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_context must not be NULL");
-    const Plan p = plan_for(*pool, n, q_heads, max_blocks, d_mass != nullptr);
-    s = check_workspace(d_workspace, workspace_bytes, p.bytes);
-    if (s != PEEK_OK) return s;
-    a.n = n;
-    a.group = q_heads / a.pool.heads;
-    a.row_tiles = (a.group + kRows - 1) / kRows;
-    const int64_t groups = (int64_t)n * a.pool.heads * a.row_tiles * p.splits;
-    const bool many = p.splits >= kManyParts;
-    const int32_t threads = many ? 1024 : kThreads, rows = many ? 1 : kWaves;      // of a joining workgroup
-    const int64_t outs = p.splits > 1 ? ((int64_t)n * q_heads + rows - 1) / rows : 0;
-    const int64_t masses = d_mass ? (int64_t)n * a.pool.heads * ((max_blocks + threads - 1) / threads) : 0;
-    if (groups >= (1 << 24) || outs + masses >= (1 << 24))
-      return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
-    hipStream_t st = (hipStream_t)stream;
-    s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, pool->block_size,
-                    &a.pool, st);
-    if (s != PEEK_OK) return s;
-    char* ws = (char*)d_workspace;
-    a.q = Rows{d_q, q_token_stride, q_head_stride};
     a.context = d_context;
+    a.context_row = 1;
     a.table = Table{d_block_table, table_stride, max_blocks};
-    a.out = (uint16_t*)d_out;
-    a.out_token = out_token_stride;
-    a.out_head = out_head_stride;
-    a.lse = d_lse;
     a.mass_in = d_mass_in;
     a.mass = d_mass;
-    a.part_out = (float*)(ws + p.part_out);
-    a.part_lse = (float*)(ws + p.part_lse);
-    a.weights = (float*)(ws + p.weights);
-    a.grains = p.grains;
-    a.log_grain = p.log_grain;
-    a.chunk = p.chunk;
-    a.splits = p.splits;
-    set_scale(scale, &a.scale, &a.q_flip, &a.q_mask);
-    with_types(type, pool->type, pool->head_dim, [&](auto t, auto m, auto d) {
-      auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kThreads), 0, st, a); };
-      if (a.pool.log_block >= 4) {
-        d_mass ? go(k_decode<t(), m(), d(), true, true>) : go(k_decode<t(), m(), d(), false, true>);
-      } else {
-        d_mass ? go(k_decode<t(), m(), d(), true, false>) : go(k_decode<t(), m(), d(), false, false>);
-      }
-    });
-    hipError_t err = hipGetLastError();
-    if (err == hipSuccess && outs + masses > 0) {
-      with_types(type, PEEK_TYPE_I8, pool->head_dim, [&](auto t, auto, auto d) {
-        auto go = [&](auto kernel) {
-          hipLaunchKernelGGL(kernel, dim3((unsigned)(outs + masses)), dim3(threads), 0, st, a, (uint32_t)outs);
-        };
-        many ? go(k_decode_join<t(), d(), 1024, 16>) : go(k_decode_join<t(), d(), kThreads, 1>);
-      });
-      err = hipGetLastError();
-    }
-    if (err != hipSuccess) return fail(PEEK_ERR_DEVICE, "decode launch failed: %s", hipGetErrorString(err));
-    return PEEK_OK;
+    return decode(a, pool, n, type, q_heads, d_q, q_token_stride, q_head_stride, scale, d_out, out_token_stride,
+                  out_head_stride, d_lse, d_workspace, workspace_bytes, (hipStream_t)stream);
+  });
+}
+
+size_t peek_sparse_decode_attention_workspace(const peek_kv_pool* pool, int32_t n, int32_t q_heads, int32_t keep) {
+  return peek_decode_attention_workspace(pool, n, q_heads, keep, 0);
+}
+
+peek_status peek_sparse_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t type, int32_t q_heads,
+                                         const void* d_q, int64_t q_token_stride, int64_t q_head_stride,
+                                         const int32_t* d_context, const int32_t* d_block_table, int32_t keep,
+                                         float scale, void* d_out, int64_t out_token_stride, int64_t out_head_stride,
+                                         float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream) {
+  return guarded([&]() -> peek_status {
+    clear_error();
+    Decode a{};
+    const int64_t heads = pool ? pool->kv_heads : 0;
+    a.context = d_context;
+    a.context_row = heads;
+    a.context_head = 1;
+    a.table = Table{d_block_table, keep * heads, keep};
+    a.table_head = keep;
+    return decode(a, pool, n, type, q_heads, d_q, q_token_stride, q_head_stride, scale, d_out, out_token_stride,
+                  out_head_stride, d_lse, d_workspace, workspace_bytes, (hipStream_t)stream);
   });
 }
 

@@ -2,6 +2,7 @@
 // the checks that the calls on pages share.
 #include "peek_internal.h"
 #include "peek_kv.h"
+#include "peek_quant.h"
 #include "peek_validate.h"
 
 namespace peek {
@@ -9,6 +10,7 @@ namespace peek {
 using kv::Pool;
 using kv::Rows;
 using kv::Table;
+using namespace quant;
 
 namespace {
 
@@ -29,70 +31,6 @@ constexpr int kWave = 64;
 // reaches 4.95); of 32 87 us (104 with four a lane), of 64 99 (116), of 256 137 (158);
 // blocks of 16 with eight a lane 107. 64 single tokens 5.3 us: the waits for
 // offsets, page id, old scale and codes, one after the other.
-
-__device__ __forceinline__ float wave_max(float x) {
-  for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
-  return x;
-}
-
-// The scale of a block whose largest finite magnitude is `most`.
-template <int FMT>
-__device__ __forceinline__ float scale_of(float most) {
-  if constexpr (FMT == PEEK_TYPE_F8E4M3) {
-    // most = m * 2^e with m in [1, 2); 448 = 1.75 * 2^8
-    const uint32_t bits = __builtin_bit_cast(uint32_t, most);
-    int32_t e = (int32_t)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
-    e = max(-60, min(60, e));
-    return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
-  } else {
-    return fminf(fmaxf(most * (1.0f / 127.0f), kv::kScaleMin), kv::kScaleMax);
-  }
-}
-
-// x / scale, correctly rounded where it is below 512 (beyond, any value there
-// is as good): the product with the rounded reciprocal is at most two units off,
-// its remainder is exact, and the quotient corrected by that is the nearest.
-__device__ __forceinline__ float quotient(float x, float scale, float inv) {
-  const float y = x * inv;
-  return fabsf(y) < 512.0f ? fmaf(fmaf(-y, scale, x), inv, y) : y;
-}
-
-// Four values' codes. `plain`: none is NaN or above the largest code.
-template <int FMT>
-__device__ __forceinline__ uint32_t codes_of(const float* x, float scale, float inv, bool plain) {
-  float y[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[i] = quotient(x[i], scale, inv);
-    if (!plain) {
-      if constexpr (FMT == PEEK_TYPE_F8E4M3) y[i] = y[i] < -448.0f ? -448.0f : y[i] > 448.0f ? 448.0f : y[i];
-      else y[i] = y[i] != y[i] ? 0.0f : y[i] < -127.0f ? -127.0f : y[i] > 127.0f ? 127.0f : y[i];
-    }
-  }
-  if constexpr (FMT == PEEK_TYPE_F8E4M3) {
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
-  } else {
-    // 1.5 * 2^23 + y has y, rounded to nearest even, in its low byte
-    uint32_t u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = __builtin_bit_cast(uint32_t, y[i] + 12582912.0f);
-    return __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400) | __builtin_amdgcn_perm(u[3], u[2], 0x04000c0c);
-  }
-}
-
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-
-template <int TYPE>
-__device__ __forceinline__ void spread8(const u4 w, float* x) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t u = w[i];
-    x[2 * i] = kv::to_float<TYPE>((uint16_t)u);
-    x[2 * i + 1] = kv::to_float<TYPE>((uint16_t)(u >> 16));
-  }
-}
 
 template <int TYPE, int FMT, int D, int HELD>
 __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, int32_t n, int64_t num_tokens,
@@ -152,21 +90,7 @@ __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, in
   plain = __all(plain) && scale < kv::kScaleMax;
   if (old > 0 && !(scale > held)) scale = held;
   const float inv = 1.0f / scale;
-  if (old > 0 && scale > held) {
-    // older values are at most the largest code times a smaller scale; NaN codes stay NaN
-    for (int32_t p = lane; p < old * kPieces; p += kWave) {
-      u2 c = *(const u2*)(codes + p * 8);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float y[4];
-        const uint32_t word = c[h];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = kv::code_value<FMT>((uint8_t)(word >> (8 * e))) * held;
-        c[h] = codes_of<FMT>(y, scale, inv, false);
-      }
-      *(u2*)(codes + p * 8) = c;
-    }
-  }
+  if (old > 0 && scale > held) rescale<FMT>(codes, old * D, held, scale, inv, lane);
   for (int32_t p0 = 0; p0 < pieces; p0 += HELD * kWave) {
     if (pieces > HELD * kWave) load(p0);
 #pragma unroll

@@ -85,6 +85,29 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
 }
 
+// Over the lanes that hold the same row: l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float swap16_max(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float swap16_sum(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+// Four tokens of four bytes each -> four bytes' worth of four tokens.
+__device__ __forceinline__ void turn4(const uint32_t a, const uint32_t b, const uint32_t c, const uint32_t d,
+                                      uint32_t* r) {
+  const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602);
+  const uint32_t cd0 = __builtin_amdgcn_perm(d, c, 0x05010400), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602);
+  r[0] = __builtin_amdgcn_perm(cd0, ab0, 0x05040100);
+  r[1] = __builtin_amdgcn_perm(cd0, ab0, 0x07060302);
+  r[2] = __builtin_amdgcn_perm(cd1, ab1, 0x05040100);
+  r[3] = __builtin_amdgcn_perm(cd1, ab1, 0x07060302);
+}
+
 // ------------------------------------------- running softmax, parts of a row
 // A row's weights are 2^(x - top), of 16 bits where they meet the values. Where a
 // tile's largest x lies too far from `top`, top moves and what the row has

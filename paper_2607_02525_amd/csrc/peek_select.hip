@@ -1,0 +1,478 @@
+// Which blocks of a long context a query should look at, on gfx950: the largest
+// and the smallest key of every block, element by element, and from these the
+// blocks that promise the largest logits.
+//
+// With hi and lo a block's bounds, no key of it has a product with q above
+//   sum_d max(q_d hi_d, q_d lo_d) = max(q, 0) . hi + min(q, 0) . lo,
+// one product of 2 D elements a (query, block). Bounds are 8-bit whole numbers:
+// int8 codes as they are, float8 values in steps of 4 (448 / 4 = 112), rounded outwards; the
+// block's scale goes with them. Queries are rounded to 8 bits by a power of two.
+// Products and sums are then whole numbers below 2^22, so scores are the same
+// in any order of summation, and so is the choice.
+#include <algorithm>
+
+#include "peek_internal.h"
+#include "peek_kv.h"
+#include "peek_mfma.h"
+#include "peek_validate.h"
+
+namespace peek {
+
+using kv::Pool;
+using kv::Rows;
+using kv::Table;
+using namespace mm;
+
+namespace {
+
+constexpr int kWave = 64;
+constexpr int kWaves = 4;
+constexpr int kThreads = kWave * kWaves;
+
+// ------------------------------------------------------------------ bounds
+// A wavefront takes every splits-th block of a sequence for one head.
+
+struct Bounds {
+  Pool pool;
+  const int32_t* first;       // null: from the first token on
+  const int32_t* context;
+  Table table;
+  int8_t* out;                // [num_pages][kv_heads][2][D]
+  int32_t n, splits;
+};
+
+// float8 codes (sign and magnitude) to bytes in the order of their values, and back.
+template <int FMT>
+__device__ __forceinline__ uint32_t ordered4(uint32_t w) {
+  if constexpr (FMT == PEEK_TYPE_F8E4M3) return w ^ ((w >> 7) & 0x01010101u) * 0x7fu;
+  return w;
+}
+
+typedef short p2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(p2, a), __builtin_bit_cast(p2, b)));
+}
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(p2, a), __builtin_bit_cast(p2, b)));
+}
+
+// An ordered byte's bound: in units of the scale (int8), or of four of it, upwards or downwards.
+template <int FMT>
+__device__ __forceinline__ int32_t bound_of(uint8_t o, bool up) {
+  if constexpr (FMT == PEEK_TYPE_F8E4M3) {
+    const uint8_t c = o & 0x80 ? o ^ 0x7f : o;
+    if ((c & 0x7f) == 0x7f) return c & 0x80 ? -127 : 127;        // NaN: beyond every number of its sign
+    const float x = kv::code_value<FMT>(c) * 0.25f;
+    return (int32_t)(up ? ceilf(x) : floorf(x));
+  } else {
+    return max(-127, (int32_t)(int8_t)o);
+  }
+}
+
+template <int FMT, int D>
+__global__ __launch_bounds__(kThreads) void k_kv_bounds(Bounds a) {
+  constexpr int kLanes = D / 16;              // of a token
+  constexpr int kStep = kWave / kLanes;       // tokens a load
+  const int lane = threadIdx.x & (kWave - 1);
+  int64_t unit = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int32_t heads = a.pool.heads, lb = a.pool.log_block;
+  const int32_t head = (int32_t)(unit % heads);
+  unit /= heads;
+  const int32_t split = (int32_t)(unit % a.splits);
+  const int32_t r = (int32_t)(unit / a.splits);
+  if (r >= a.n) return;
+  const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb);
+  const int32_t first = a.first ? max(0, a.first[r]) : 0;
+  const int32_t blocks = (int32_t)(((int64_t)held + (1 << lb) - 1) >> lb);
+  const int32_t at = lane % kLanes, sub = lane / kLanes;
+  if (first >= held) return;
+  for (int64_t b = (first >> lb) + split; b < blocks; b += a.splits) {
+    const uint32_t page = kv::page_of(a.table, a.pool, r, (int32_t)b);
+    const int32_t tokens = min(1 << lb, held - ((int32_t)b << lb));
+    const uint8_t* codes = a.pool.pages + (((int64_t)page * 2 * heads + head) << lb) * D + at * 16;
+    uint32_t hi[8], lo[8];        // bytes 1, 3 of every word in the upper halves of 16 bits, then bytes 0, 2
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      hi[e] = 0x80008000u;
+      lo[e] = 0x7fff7fffu;
+    }
+    for (int32_t t0 = 0; t0 < tokens; t0 += 2 * kStep) {
+      u4 w[2];                    // tokens past the end: the last again
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[i] = *(const u4*)(codes + min(t0 + i * kStep + sub, tokens - 1) * D);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t o = ordered4<FMT>(w[i][e]), odd = o & 0xff00ff00u, even = (o << 8) & 0xff00ff00u;
+          hi[2 * e] = max2(hi[2 * e], odd);
+          lo[2 * e] = min2(lo[2 * e], odd);
+          hi[2 * e + 1] = max2(hi[2 * e + 1], even);
+          lo[2 * e + 1] = min2(lo[2 * e + 1], even);
+        }
+    }
+#pragma unroll
+    for (int d = kLanes; d < kWave; d <<= 1)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        hi[e] = max2(hi[e], __shfl_xor(hi[e], d));
+        lo[e] = min2(lo[e], __shfl_xor(lo[e], d));
+      }
+    const bool turned = a.pool.scales[(int64_t)page * 2 * heads + head] < 0.0f;
+    if (sub < 2) {                // the first kLanes lanes write hi, the next lo
+      const bool up = sub == 0;
+      u4 out;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool from_hi = up != turned;
+        const uint32_t odd = from_hi ? hi[2 * e] : lo[2 * e], even = from_hi ? hi[2 * e + 1] : lo[2 * e + 1];
+        const uint32_t o = (odd & 0xff00ff00u) | ((even >> 8) & 0x00ff00ffu);
+        uint32_t word = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int32_t x = bound_of<FMT>((uint8_t)(o >> (8 * i)), from_hi);
+          word |= (uint32_t)(uint8_t)(turned ? -x : x) << (8 * i);
+        }
+        out[e] = word;
+      }
+      *(u4*)(a.out + (((int64_t)page * heads + head) * 2 + sub) * D + at * 16) = out;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ scores
+// A wavefront takes 64 blocks of one (sequence, kv head): queries times bounds,
+// 16 queries by 16 blocks by 64 elements a matrix instruction.
+
+struct Select {
+  Pool pool;
+  Rows q;
+  const int8_t* bounds;
+  const int32_t* context;
+  Table table;
+  float* scores;              // [n][kv_heads][width]
+  int32_t* context_out;       // [n][kv_heads]
+  int32_t* table_out;         // [n][kv_heads][keep]
+  int32_t n, group, keep, sink, recent;
+};
+
+constexpr int kSpan = 64;     // blocks of a wavefront
+
+typedef int32_t i4 __attribute__((ext_vector_type(4)));
+
+template <int TYPE, int FMT, int D>
+__global__ __launch_bounds__(kThreads) void k_block_scores(Select a, int32_t spans) {
+  constexpr int kSteps = D / 64;
+  const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
+  int64_t unit = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int32_t heads = a.pool.heads, lb = a.pool.log_block;
+  const int32_t head = (int32_t)(unit % heads);
+  unit /= heads;
+  const int32_t span = (int32_t)(unit % spans), r = (int32_t)(unit / spans);
+  if (r >= a.n) return;
+  const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb);
+  const int32_t blocks = (int32_t)(((int64_t)held + (1 << lb) - 1) >> lb), b0 = span * kSpan;
+  if (b0 >= blocks || blocks <= a.keep) return;        // (all of them are kept)
+
+  const int32_t mine = min(b0 + lane, blocks - 1);
+  const uint32_t page = kv::page_of(a.table, a.pool, r, mine);
+  const float step = fabsf(a.pool.scales[(int64_t)page * 2 * heads + head]) * (FMT == PEEK_TYPE_F8E4M3 ? 4.0f : 1.0f);
+  u4 bounds[4][2 * kSteps];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t p = __shfl(page, 16 * i + col);
+    const int8_t* from = a.bounds + ((int64_t)p * heads + head) * 2 * D + grp * 16;
+#pragma unroll
+    for (int s = 0; s < 2 * kSteps; ++s) bounds[i][s] = *(const u4*)(from + s * 64);
+  }
+  float best[4] = {-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
+  for (int32_t row0 = 0; row0 < a.group; row0 += 16) {
+    // lane l: row row0 + l % 16 (past the last: the last again), elements 16 (l / 16) .. + 15 of every 64
+    const uint16_t* q = (const uint16_t*)a.q.data + (int64_t)r * a.q.token +
+        (int64_t)(head * a.group + min(row0 + col, a.group - 1)) * a.q.head + grp * 16;
+    float x[kSteps][16];
+    float most = 0.0f;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const uint32_t w = (*(const u4*)(q + s * 64 + (e >> 3) * 8))[(e >> 1) & 3];
+        x[s][e] = kv::to_float<TYPE>((uint16_t)(w >> (16 * (e & 1))));
+        const float m = fabsf(x[s][e]);
+        most = fmaxf(most, m < __builtin_inff() ? m : 0.0f);
+      }
+    most = max_halves(swap16_max(most));
+    const int32_t e = __builtin_amdgcn_frexp_expf(most) - 7;
+    u4 up[kSteps], down[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t u = 0, v = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float y = __builtin_ldexpf(x[s][4 * w + i], -e);
+          const int32_t c = y != y ? 0 : (int32_t)__builtin_rintf(fminf(fmaxf(y, -127.0f), 127.0f));
+          u |= (uint32_t)(uint8_t)max(c, 0) << (8 * i);
+          v |= (uint32_t)(uint8_t)min(c, 0) << (8 * i);
+        }
+        up[s][w] = u;
+        down[s][w] = v;
+      }
+    int32_t of_row[4];          // exponents of the rows that this lane's products belong to
+#pragma unroll
+    for (int v = 0; v < 4; ++v) of_row[v] = __shfl(e, 4 * grp + v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      i4 dot = {};
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4, up[s]), __builtin_bit_cast(i4, bounds[i][s]),
+                                                    dot, 0, 0, 0);
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4, down[s]),
+                                                    __builtin_bit_cast(i4, bounds[i][kSteps + s]), dot, 0, 0, 0);
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) best[i] = fmaxf(best[i], __builtin_ldexpf((float)dot[v], of_row[v]));
+    }
+  }
+  // block 16 i + col of every i, for all rows; lane l keeps that of block l
+  float score = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float top = max_halves(swap16_max(best[i]));
+    score = grp == i ? top : score;
+  }
+  if (b0 + lane < blocks)
+    a.scores[((int64_t)r * heads + head) * a.table.width + b0 + lane] = score * step + 0.0f;      // (no -0)
+}
+
+// ------------------------------------------------------------------ choice
+// A workgroup takes one (sequence, kv head). The candidates' scores, as whole
+// numbers in their order, are counted by digits of 8 bits from the top: after
+// four passes the least score to stay and how many of that score are known.
+
+__device__ __forceinline__ uint32_t rank_of(float x) {       // NaN above all
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  return x != x ? 0xffffffffu : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_block_select(Select a) {
+  constexpr int kWaves = THREADS / kWave;
+  __shared__ uint32_t s_count[kWaves][256];
+  __shared__ uint32_t s_digit, s_left;
+  __shared__ uint32_t s_more[kWaves], s_equal[kWaves];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int32_t heads = a.pool.heads, lb = a.pool.log_block;
+  const int32_t head = blockIdx.x % heads, r = blockIdx.x / heads;
+  const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb);
+  const int32_t blocks = (int32_t)(((int64_t)held + (1 << lb) - 1) >> lb);
+  const int64_t unit = (int64_t)r * heads + head;
+  const int32_t* ids = a.table.ids + (int64_t)r * a.table.stride;
+  int32_t* out = a.table_out + unit * a.keep;
+  const int32_t kept = min(blocks, a.keep);
+  // the last block stays, so only that one can be part full
+  if (tid == 0) a.context_out[unit] = held - ((blocks - kept) << lb);
+  for (int32_t i = kept + tid; i < a.keep; i += THREADS) out[i] = -1;
+  if (blocks <= a.keep) {
+    for (int32_t i = tid; i < blocks; i += THREADS) out[i] = ids[i];
+    return;
+  }
+  const float* scores = a.scores + unit * a.table.width;
+  const int32_t lo = a.sink, hi = blocks - a.recent;          // candidates (blocks > keep >= sink + recent)
+  uint32_t prefix = 0, left = (uint32_t)(a.keep - a.sink - a.recent);      // so many of the candidates stay
+  for (int shift = 24; shift >= 0 && left > 0; shift -= 8) {
+    for (int32_t i = tid; i < kWaves * 256; i += THREADS) (&s_count[0][0])[i] = 0;
+    __syncthreads();
+    for (int32_t b = lo + tid; b < hi; b += THREADS) {
+      const uint32_t x = rank_of(scores[b]);
+      if (shift == 24 || (x ^ prefix) >> (shift + 8) == 0) atomicAdd(&s_count[wave][(x >> shift) & 255], 1u);
+    }
+    __syncthreads();
+    if (wave == 0) {            // lane l: digits 255 - 4 l .. 252 - 4 l
+      uint32_t c[4], sum = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        c[e] = 0;
+        for (int w = 0; w < kWaves; ++w) c[e] += s_count[w][255 - 4 * lane - e];
+        sum += c[e];
+      }
+      uint32_t before = sum;
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) {
+        const uint32_t x = __shfl_up(before, d);
+        if (lane >= d) before += x;
+      }
+      before -= sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (before < left && left <= before + c[e]) {
+          s_digit = 255 - 4 * lane - e;
+          s_left = left - before;
+        }
+        before += c[e];
+      }
+    }
+    __syncthreads();
+    prefix |= s_digit << shift;
+    left = s_left;
+  }
+  // a wavefront's share of the blocks in order: counted, then placed
+  const int32_t share = ((blocks + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
+  const int32_t from = min(wave * share, blocks), to = min(from + share, blocks);
+  const bool any = a.keep > a.sink + a.recent;
+  auto look = [&](int32_t b, bool* more, bool* equal) {
+    const bool must = b < lo || b >= hi, in = b < to;
+    const uint32_t x = in && !must ? rank_of(scores[b]) : 0u;
+    *more = in && (must || (any && x > prefix));
+    *equal = in && !must && any && x == prefix;
+  };
+  uint32_t more = 0, equal = 0;
+  for (int32_t b = from; b < to; b += kWave) {
+    bool m, e;
+    look(b + lane, &m, &e);
+    more += __popcll(__ballot(m));
+    equal += __popcll(__ballot(e));
+  }
+  if (lane == 0) {
+    s_more[wave] = more;
+    s_equal[wave] = equal;
+  }
+  __syncthreads();
+  uint32_t place = 0, ties = 0;        // of what comes before: places taken, and equal ones
+  for (int w = 0; w < wave; ++w) {
+    place += s_more[w];
+    ties += s_equal[w];
+  }
+  place += min(ties, left);
+  const uint64_t below = (1ull << lane) - 1;
+  for (int32_t b = from; b < to; b += kWave) {
+    bool m, e;
+    look(b + lane, &m, &e);
+    const uint64_t equals = __ballot(e);
+    const bool stays = m || (e && ties + (uint32_t)__popcll(equals & below) < left);
+    const uint64_t all = __ballot(stays);
+    if (stays) out[place + __popcll(all & below)] = ids[b + lane];
+    place += __popcll(all);
+    ties += __popcll(equals);
+  }
+}
+
+int64_t score_bytes(int32_t n, int32_t heads, int32_t width) {
+  return ((int64_t)n * heads * width * (int64_t)sizeof(float) + 255) & ~(int64_t)255;
+}
+
+}  // namespace
+}  // namespace peek
+
+using namespace peek;
+
+extern "C" {
+
+peek_status peek_kv_bounds(const peek_kv_pool* pool, int32_t n, const int32_t* d_first, const int32_t* d_context,
+                           const int32_t* d_block_table, int32_t max_blocks, int64_t table_stride, int8_t* d_bounds,
+                           void* stream) {
+  return guarded([&]() -> peek_status {
+    clear_error();
+    Bounds a{};
+    peek_status s = check_pool(pool, &a.pool);
+    if (s != PEEK_OK) return s;
+    if (n < 0) return fail(PEEK_ERR_INVALID_ARGUMENT, "n must be >= 0 (got %d)", n);
+    if ((s = check_table(d_block_table, max_blocks, table_stride, pool->block_size)) != PEEK_OK) return s;
+    if (n == 0 || max_blocks == 0) return PEEK_OK;
+    if (!d_context || !d_bounds) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_context and d_bounds must not be NULL");
+    if ((reinterpret_cast<uintptr_t>(d_bounds) & 15) != 0)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "d_bounds must be 16-byte aligned");
+    const int64_t units = (int64_t)n * a.pool.heads;
+    a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(max_blocks, 16384 / units));
+    const int64_t groups = (units * a.splits + kWaves - 1) / kWaves;
+    if (groups >= (1 << 24)) return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
+    hipStream_t st = (hipStream_t)stream;
+    s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, pool->block_size, &a.pool,
+                    st);
+    if (s != PEEK_OK) return s;
+    a.first = d_first;
+    a.context = d_context;
+    a.table = Table{d_block_table, table_stride, max_blocks};
+    a.out = d_bounds;
+    a.n = n;
+    with_types(PEEK_TYPE_BF16, pool->type, pool->head_dim, [&](auto, auto f, auto d) {
+      hipLaunchKernelGGL((k_kv_bounds<f(), d()>), dim3((unsigned)groups), dim3(kThreads), 0, st, a);
+    });
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "bounds launch failed: %s", hipGetErrorString(e));
+    return PEEK_OK;
+  });
+}
+
+size_t peek_block_select_workspace(const peek_kv_pool* pool, int32_t n, int32_t max_blocks) {
+  Pool p;
+  if (n < 0 || max_blocks < 0 || check_pool(pool, &p) != PEEK_OK) return 0;
+  return (size_t)score_bytes(n, p.heads, max_blocks);
+}
+
+peek_status peek_block_select(const peek_kv_pool* pool, const int8_t* d_bounds, int32_t n, int32_t type,
+                              int32_t q_heads, const void* d_q, int64_t q_token_stride, int64_t q_head_stride,
+                              const int32_t* d_context, const int32_t* d_block_table, int32_t max_blocks,
+                              int64_t table_stride, int32_t keep, int32_t sink, int32_t recent, int32_t* d_context_out,
+                              int32_t* d_table_out, void* d_workspace, size_t workspace_bytes, void* stream) {
+  return guarded([&]() -> peek_status {
+    clear_error();
+    Select a{};
+    peek_status s = check_pool(pool, &a.pool);
+    if (s != PEEK_OK) return s;
+    if (n < 0) return fail(PEEK_ERR_INVALID_ARGUMENT, "n must be >= 0 (got %d)", n);
+    if ((s = check_heads(type, q_heads, a.pool.heads, 1.0f)) != PEEK_OK) return s;
+    if ((s = check_table(d_block_table, max_blocks, table_stride, pool->block_size)) != PEEK_OK) return s;
+    if (sink < 0 || recent < 1 || keep < 1 || (int64_t)sink + recent > keep)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "sink >= 0, recent >= 1 and sink + recent <= keep (got %d, %d, %d)", sink,
+                  recent, keep);
+    if ((int64_t)keep * pool->block_size > INT32_MAX)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "keep * block_size must be below 2^31 (got %d * %d)", keep,
+                  pool->block_size);
+    if (n == 0) return PEEK_OK;
+    if ((s = check_rows("d_q", d_q, q_token_stride, q_head_stride)) != PEEK_OK) return s;
+    if (!d_bounds || !d_context || !d_context_out || !d_table_out)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "d_bounds, d_context, d_context_out and d_table_out must not be NULL");
+    if ((reinterpret_cast<uintptr_t>(d_bounds) & 15) != 0)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "d_bounds must be 16-byte aligned");
+    s = check_workspace(d_workspace, workspace_bytes, (size_t)score_bytes(n, a.pool.heads, max_blocks));
+    if (s != PEEK_OK) return s;
+    const int64_t units = (int64_t)n * a.pool.heads;
+    const int32_t spans = (max_blocks + kSpan - 1) / kSpan;
+    const int64_t groups = (units * spans + kWaves - 1) / kWaves;
+    if (groups >= (1 << 24) || units >= (1 << 24))
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
+    hipStream_t st = (hipStream_t)stream;
+    s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, pool->block_size, &a.pool,
+                    st);
+    if (s != PEEK_OK) return s;
+    a.q = Rows{d_q, q_token_stride, q_head_stride};
+    a.bounds = d_bounds;
+    a.context = d_context;
+    a.table = Table{d_block_table, table_stride, max_blocks};
+    a.scores = (float*)d_workspace;
+    a.context_out = d_context_out;
+    a.table_out = d_table_out;
+    a.n = n;
+    a.group = q_heads / a.pool.heads;
+    a.keep = keep;
+    a.sink = sink;
+    a.recent = recent;
+    if (max_blocks > keep) {        // (otherwise all blocks are kept)
+      with_types(type, pool->type, pool->head_dim, [&](auto t, auto f, auto d) {
+        hipLaunchKernelGGL((k_block_scores<t(), f(), d()>), dim3((unsigned)groups), dim3(kThreads), 0, st, a, spans);
+      });
+    }
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess) {
+      hipLaunchKernelGGL((k_block_select<1024>), dim3((unsigned)units), dim3(1024), 0, st, a);
+      e = hipGetLastError();
+    }
+    if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "selection launch failed: %s", hipGetErrorString(e));
+    return PEEK_OK;
+  });
+}
+
+}  // extern "C"
