@@ -652,8 +652,8 @@ peek_status peek_shared_decode_attention(const peek_kv_pool* pool, int32_t n, in
  * the largest logits, chosen for every sequence and kv head.
  *
  * peek_kv_bounds: d_bounds int8[num_pages][kv_heads][2][head_dim], 16-byte
- * aligned, receives for every block of sequence r that holds one of its tokens
- * d_first[r] .. d_context[r] - 1 (d_first NULL or negative: from 0 on) the
+ * aligned, receives for every block of sequence r that holds tokens, from that
+ * of token d_first[r] on (d_first NULL or negative: from the first on), the
  * largest (at 0) and the smallest (at 1) of the codes of its keys up to
  * d_context[r], element by element: of int8 codes themselves, of float8 values v
  * the next whole number above, and below, v / 4 (a NaN is the largest of its sign); within

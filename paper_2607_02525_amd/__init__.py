@@ -736,8 +736,8 @@ def peek_shared_decode_attention(pool: KVPool, q, context, block_table, group_of
 
 
 def peek_kv_bounds(pool: KVPool, first, context, block_table, bounds, stream=None):
-    """The largest and smallest key code of every block that holds one of sequence r's tokens first[r] .. context[r] - 1
-    (first None: from 0 on), into bounds int8[num_pages, kv_heads, 2, head_dim]."""
+    """The largest and smallest key code of sequence r's blocks, from that of token first[r] on (None: from the first on)
+    up to context[r] tokens, into bounds int8[num_pages, kv_heads, 2, head_dim]."""
     n = context.shape[0]
     table = _table(block_table, n)
     at = _exact_arg(bounds, "bounds", torch.int8, pool.num_pages, pool.kv_heads, 2, pool.head_dim)

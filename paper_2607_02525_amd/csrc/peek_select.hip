@@ -85,7 +85,6 @@ __global__ __launch_bounds__(kThreads) void k_kv_bounds(Bounds a) {
   const int32_t first = a.first ? max(0, a.first[r]) : 0;
   const int32_t blocks = (int32_t)(((int64_t)held + (1 << lb) - 1) >> lb);
   const int32_t at = lane % kLanes, sub = lane / kLanes;
-  if (first >= held) return;
   for (int64_t b = (first >> lb) + split; b < blocks; b += a.splits) {
     const uint32_t page = kv::page_of(a.table, a.pool, r, (int32_t)b);
     const int32_t tokens = min(1 << lb, held - ((int32_t)b << lb));
