@@ -630,12 +630,20 @@ class _RotaryStruct(ctypes.Structure):
                 ("eps", ctypes.c_float), ("d_q_norm", _vp), ("d_k_norm", _vp)]
 
 
-def _here(*tensors):
-    """Refuses tensors of a device other than the current one, where the call's kernels run."""
-    now = torch.cuda.current_device()
+# The current device's number without the check that torch is initialised, where this torch has that.
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _place(stream, *tensors):
+    """The stream's handle, after refusing tensors of a device other than the current one, where the kernels run."""
+    fast = _raw_device is not None and _raw_stream is not None and torch.cuda.is_initialized()
+    now = _raw_device() if fast else torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device.index != now:
+        if t is not None and t.get_device() != now:
             raise ValueError(f"tensors must be on the current device (cuda:{now}), got one on {t.device}")
+    if stream is None:
+        return _raw_stream(now) if fast else torch.cuda.current_stream().cuda_stream
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def _exact_arg(t, name: str, dtype, *shape: int):
@@ -689,10 +697,11 @@ def peek_rotate_append(q, k, v, offsets, context, freq, q_out, k_out=None, pool:
                            _exact_arg(q_norm, "q_norm", dtype, dim), _exact_arg(k_norm, "k_norm", dtype, dim))
     table = none if block_table is None else _table(block_table, n)
     at, ctx = _arg(offsets, "offsets"), _arg(context, "context", torch.int32, n)
-    _here(q, k, v, offsets, context, freq, q_out, k_out, block_table, q_norm, k_norm, pool and pool.pages)
+    on = _place(stream, q, k, v, offsets, context, freq, q_out, k_out, block_table, q_norm, k_norm,
+                None if pool is None else pool._pages)
     _check(_lib.peek_rotate_append(None if pool is None else pool._ref, n, tokens, kind, q_heads, kv_heads, dim,
                                    ctypes.addressof(rotary), *rows_q, *rows_k, *rows_v, at, ctx, *table, *rows_q_out,
-                                   *rows_k_out, _stream(stream)))
+                                   *rows_k_out, on))
 
 
 def peek_kv_read(pool: KVPool, offsets, first, block_table, k_out, v_out, stream=None):
@@ -704,8 +713,8 @@ def peek_kv_read(pool: KVPool, offsets, first, block_table, k_out, v_out, stream
     rows_k = _rows(k_out, "k_out", k_out.dtype, pool.kv_heads, pool.head_dim)
     rows_v = _rows(v_out, "v_out", k_out.dtype, pool.kv_heads, pool.head_dim, k_out.shape[0])
     at, begin = _arg(offsets, "offsets"), _arg(first, "first", torch.int32, n)
-    _here(pool.pages, offsets, first, block_table, k_out, v_out)
-    _check(_lib.peek_kv_read(pool._ref, n, k_out.shape[0], kind, at, begin, *table, *rows_k, *rows_v, _stream(stream)))
+    on = _place(stream, pool._pages, offsets, first, block_table, k_out, v_out)
+    _check(_lib.peek_kv_read(pool._ref, n, k_out.shape[0], kind, at, begin, *table, *rows_k, *rows_v, on))
 
 
 def peek_shared_decode_attention_workspace(pool: KVPool, n: int, q_heads: int, max_blocks: int, groups: int) -> int:
@@ -726,13 +735,13 @@ def peek_shared_decode_attention(pool: KVPool, q, context, block_table, group_of
         raise ValueError("group_offsets must be 1-D, of groups + 1 entries")
     groups, i32 = group_offsets.shape[0] - 1, torch.int32
     table = _table(block_table, n)
-    _here(pool.pages, q, context, block_table, group_offsets, shared, out, workspace, members, lse)
+    on = _place(stream, pool._pages, q, context, block_table, group_offsets, shared, out, workspace, members, lse)
     _check(_lib.peek_shared_decode_attention(
         pool._ref, n, kind, q_heads, *_rows(q, "q", q.dtype, None, pool.head_dim), _arg(context, "context", i32, n),
         *table, groups, _arg(members, "members", i32, n), _arg(group_offsets, "group_offsets", i32),
         _arg(shared, "shared", i32, groups), pool.head_dim ** -0.5 if scale is None else scale,
         *_rows(out, "out", q.dtype, q_heads, pool.head_dim, n), _row_arg(lse, "lse", torch.float32, n, q_heads),
-        *_ws(workspace), _stream(stream)))
+        *_ws(workspace), on))
 
 
 def peek_kv_bounds(pool: KVPool, first, context, block_table, bounds, stream=None):
@@ -742,8 +751,8 @@ def peek_kv_bounds(pool: KVPool, first, context, block_table, bounds, stream=Non
     table = _table(block_table, n)
     at = _exact_arg(bounds, "bounds", torch.int8, pool.num_pages, pool.kv_heads, 2, pool.head_dim)
     begin, ctx = _arg(first, "first", torch.int32, n), _arg(context, "context", torch.int32, n)
-    _here(pool.pages, first, context, block_table, bounds)
-    _check(_lib.peek_kv_bounds(pool._ref, n, begin, ctx, *table, at, _stream(stream)))
+    on = _place(stream, pool._pages, first, context, block_table, bounds)
+    _check(_lib.peek_kv_bounds(pool._ref, n, begin, ctx, *table, at, on))
 
 
 def peek_block_select_workspace(pool: KVPool, n: int, max_blocks: int) -> int:
@@ -763,11 +772,11 @@ def peek_block_select(pool: KVPool, bounds, q, context, block_table, sink: int, 
         raise ValueError("block_table_out must be [n, kv_heads, keep]")
     keep, i32 = block_table_out.shape[2], torch.int32
     at = _exact_arg(bounds, "bounds", torch.int8, pool.num_pages, pool.kv_heads, 2, pool.head_dim)
-    _here(pool.pages, bounds, q, context, block_table, context_out, block_table_out, workspace)
+    on = _place(stream, pool._pages, bounds, q, context, block_table, context_out, block_table_out, workspace)
     _check(_lib.peek_block_select(
         pool._ref, at, n, kind, q_heads, *_rows(q, "q", q.dtype, None, pool.head_dim), _arg(context, "context", i32, n),
         *table, keep, int(sink), int(recent), _exact_arg(context_out, "context_out", i32, n, pool.kv_heads),
-        _exact_arg(block_table_out, "block_table_out", i32, n, pool.kv_heads, keep), *_ws(workspace), _stream(stream)))
+        _exact_arg(block_table_out, "block_table_out", i32, n, pool.kv_heads, keep), *_ws(workspace), on))
 
 
 def peek_sparse_decode_attention_workspace(pool: KVPool, n: int, q_heads: int, keep: int) -> int:
@@ -784,10 +793,10 @@ def peek_sparse_decode_attention(pool: KVPool, q, context, block_table, out, wor
     if block_table.dim() != 3:
         raise ValueError("block_table must be [n, kv_heads, keep]")
     keep, i32 = block_table.shape[2], torch.int32
-    _here(pool.pages, q, context, block_table, out, workspace, lse)
+    on = _place(stream, pool._pages, q, context, block_table, out, workspace, lse)
     _check(_lib.peek_sparse_decode_attention(
         pool._ref, n, kind, q_heads, *_rows(q, "q", q.dtype, None, pool.head_dim),
         _exact_arg(context, "context", i32, n, pool.kv_heads),
         _exact_arg(block_table, "block_table", i32, n, pool.kv_heads, keep), keep,
         pool.head_dim ** -0.5 if scale is None else scale, *_rows(out, "out", q.dtype, q_heads, pool.head_dim, n),
-        _row_arg(lse, "lse", torch.float32, n, q_heads), *_ws(workspace), _stream(stream)))
+        _row_arg(lse, "lse", torch.float32, n, q_heads), *_ws(workspace), on))

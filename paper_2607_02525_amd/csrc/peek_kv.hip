@@ -70,24 +70,26 @@ __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, in
       w[i] = p < pieces ? *(const u4*)(x + (int64_t)(p / kPieces) * src.token + p % kPieces * 8) : (u4){};
     }
   };
-  float most = 0.0f;
-  bool plain = true;
+  uint32_t bits = 0;
   for (int32_t p0 = 0; p0 < pieces; p0 += HELD * kWave) {
     load(p0);
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-      float y[8];
-      spread8<TYPE>(w[i], y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float m = fabsf(y[e]);
-        plain = plain && m < __builtin_inff();
-        most = fmaxf(most, m < __builtin_inff() ? m : 0.0f);
-      }
-    }
+    for (int i = 0; i < HELD; ++i) bits = largest8(w[i], bits);
   }
-  float scale = scale_of<FMT>(wave_max(most));
-  plain = __all(plain) && scale < kv::kScaleMax;
+  bits = wave_largest(bits);
+  float most = kv::to_float<TYPE>((uint16_t)bits);
+  bool plain = bits < kInfinity<TYPE>;
+  if (!plain) {
+    most = 0.0f;
+    for (int32_t p0 = 0; p0 < pieces; p0 += HELD * kWave) {
+      if (pieces > HELD * kWave) load(p0);
+#pragma unroll
+      for (int i = 0; i < HELD; ++i) most = finite8<TYPE>(w[i], most);
+    }
+    most = wave_max(most);
+  }
+  float scale = scale_of<FMT>(most);
+  plain = plain && scale < kv::kScaleMax;
   if (old > 0 && !(scale > held)) scale = held;
   const float inv = 1.0f / scale;
   if (old > 0 && scale > held) rescale<FMT>(codes, old * D, held, scale, inv, lane);

@@ -36,14 +36,21 @@ __device__ __forceinline__ float quotient(float x, float scale, float inv) {
   return fabsf(y) < 512.0f ? fmaf(fmaf(-y, scale, x), inv, y) : y;
 }
 
-// Four values' codes. `plain`: none is NaN or above the largest code.
+// Four values' codes. `plain`: all are finite and below a code beyond the largest, which is so of what the scale was
+// made from: then a power of two needs no correction, and another scale no look at the quotient's size.
 template <int FMT>
 __device__ __forceinline__ uint32_t codes_of(const float* x, float scale, float inv, bool plain) {
   float y[4];
+  if (plain) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[i] = quotient(x[i], scale, inv);
-    if (!plain) {
+    for (int i = 0; i < 4; ++i) {
+      y[i] = x[i] * inv;
+      if constexpr (FMT == PEEK_TYPE_I8) y[i] = fmaf(fmaf(-y[i], scale, x[i]), inv, y[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[i] = quotient(x[i], scale, inv);
       if constexpr (FMT == PEEK_TYPE_F8E4M3) y[i] = y[i] < -448.0f ? -448.0f : y[i] > 448.0f ? 448.0f : y[i];
       else y[i] = y[i] != y[i] ? 0.0f : y[i] < -127.0f ? -127.0f : y[i] > 127.0f ? 127.0f : y[i];
     }
@@ -62,6 +69,7 @@ __device__ __forceinline__ uint32_t codes_of(const float* x, float scale, float 
 
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef unsigned short p2u __attribute__((ext_vector_type(2)));
 
 template <int TYPE>
 __device__ __forceinline__ void spread8(const u4 w, float* x) {
@@ -71,6 +79,37 @@ __device__ __forceinline__ void spread8(const u4 w, float* x) {
     x[2 * i] = kv::to_float<TYPE>((uint16_t)u);
     x[2 * i + 1] = kv::to_float<TYPE>((uint16_t)(u >> 16));
   }
+}
+
+// Magnitudes of 16-bit elements are in the order of their bits without the sign: the largest of eight and of those in
+// `most`, two side by side. (Infinities and NaN are above every number: kInfinity and more.)
+template <int TYPE>
+constexpr uint32_t kInfinity = TYPE == PEEK_TYPE_BF16 ? 0x7f80u : 0x7c00u;
+__device__ __forceinline__ uint32_t largest8(const u4 w, uint32_t most) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(p2u, most),
+                                                                  __builtin_bit_cast(p2u, w[i] & 0x7fff7fffu)));
+  return most;
+}
+// Of a wavefront.
+__device__ __forceinline__ uint32_t wave_largest(uint32_t most) {
+  most = max(most & 0xffffu, most >> 16);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) most = max(most, (uint32_t)__shfl_xor(most, d));
+  return __builtin_amdgcn_readfirstlane(most);
+}
+// The largest finite magnitude of eight elements and of `most`.
+template <int TYPE>
+__device__ __forceinline__ float finite8(const u4 w, float most) {
+  float x[8];
+  spread8<TYPE>(w, x);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float m = fabsf(x[e]);
+    most = fmaxf(most, m < __builtin_inff() ? m : 0.0f);
+  }
+  return most;
 }
 
 // `count` codes (a multiple of 8) of a scale rounded again to a larger one, by a wavefront. Values are at most the

@@ -35,6 +35,8 @@ constexpr int kWave = 64;
 constexpr int kWaves = 4;
 constexpr int kThreads = kWave * kWaves;
 constexpr int kTokens = 16;        // whose angles a workgroup holds at a time
+constexpr int kRowTokens = 4;      // of a workgroup over rows, where there are many
+constexpr int64_t kManyBlocks = 1024;
 
 struct OutRows {
   uint16_t* data;
@@ -55,6 +57,7 @@ struct Rotate {
   int64_t num_tokens, slots;
   uint32_t page_groups;            // workgroups of blocks, before those of rows
   int32_t n, q_heads, kv_heads, rot, inter, row_tokens;
+  int32_t share;                   // heads of a workgroup of blocks
   float eps, magnitude;
 };
 
@@ -63,21 +66,41 @@ struct Turns {
   float c[kTokens][64], s[kTokens][64];
 };
 
+// The angle as a fraction of a turn, from a product in 64 bits; its nearest quarter and what is left of it, x, of
+// pi / 4 at most, whose sine and cosine are their series up to x^9 and x^10 (what is left out is below 2^-28).
 __device__ __forceinline__ void turn(const Rotate& a, int64_t position, int pair, float* c, float* s) {
   constexpr double kTurn = 0.15915494309189533577;        // 1 / (2 pi)
   const double angle = (double)position * a.freq[pair] * kTurn;
-  const float part = (float)(angle - __builtin_rint(angle));
-  float sn, cs;
-  sincospif(2.0f * part, &sn, &cs);
-  *c = cs * a.magnitude;
-  *s = sn * a.magnitude;
+  const float part = (float)(angle - __builtin_rint(angle)), quarter = __builtin_rintf(4.0f * part);
+  const float x = fmaf(quarter, -0.25f, part) * 6.28318530717958648f, y = x * x;
+  float sn = fmaf(y, 1.0f / 362880, -1.0f / 5040);
+  sn = fmaf(y, sn, 1.0f / 120);
+  sn = fmaf(y, sn, -1.0f / 6);
+  sn = fmaf(x * y, sn, x);
+  float cs = fmaf(y, -1.0f / 3628800, 1.0f / 40320);
+  cs = fmaf(y, cs, -1.0f / 720);
+  cs = fmaf(y, cs, 1.0f / 24);
+  cs = fmaf(y, cs, -0.5f);
+  cs = fmaf(y, cs, 1.0f);
+  // cos, sin of x + q pi / 2: q = 0 (c, s), 1 (-s, c), 2 (-c, -s), 3 (s, -c)
+  const int q = (int)quarter & 3;
+  const float c0 = q & 1 ? sn : cs, s0 = q & 1 ? cs : sn;
+  *c = (q == 1 || q == 2 ? -c0 : c0) * a.magnitude;
+  *s = (q >= 2 ? -s0 : s0) * a.magnitude;
 }
 
-// The two pieces (of eight elements) of a head that are item j of D / 16.
+// The two pieces (of eight elements) of a head that are item j of D / 16: both halves of eight pairs, or, where there
+// are none of these (interleaved pairs lie in one piece), pieces of either half of the head.
+template <int D>
 __device__ __forceinline__ void pieces_of(const Rotate& a, int rot, int j, int* p0, int* p1) {
-  const bool halves = !a.inter && j < rot / 16;
-  *p0 = halves ? j : 2 * j;
-  *p1 = halves ? j + rot / 16 : 2 * j + 1;
+  const bool halves = j < rot / 16;
+  if (a.inter || rot == 0) {
+    *p0 = j;
+    *p1 = j + D / 16;
+  } else {
+    *p0 = halves ? j : 2 * j;
+    *p1 = halves ? j + rot / 16 : 2 * j + 1;
+  }
 }
 
 template <int TYPE>
@@ -109,37 +132,75 @@ __device__ __forceinline__ void rotate_item(const Rotate& a, const uint16_t* nor
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = x[e] * by * w[e];
   }
-  if (j < rot / 16) {
-    if (a.inter) {
+  if (a.inter) {
+    // (the pieces of an item are eight or more apart: a part of the head may end between them)
+    const bool turns[2] = {p0 < rot / 8, p1 < rot / 8};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float u = x[2 * e], w = x[2 * e + 1], cs = c[8 * j + e], sn = s[8 * j + e];
-        x[2 * e] = fmaf(u, cs, -w * sn);
-        x[2 * e + 1] = fmaf(w, cs, u * sn);
-      }
-    } else {
+    for (int h = 0; h < 2; ++h) {
+      if (!turns[h]) continue;
+      const int pair = 4 * (h == 0 ? p0 : p1);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float u = x[e], w = x[e + 8], cs = c[8 * j + e], sn = s[8 * j + e];
-        x[e] = fmaf(u, cs, -w * sn);
-        x[e + 8] = fmaf(w, cs, u * sn);
+      for (int e = 0; e < 4; ++e) {
+        const float u = x[8 * h + 2 * e], w = x[8 * h + 2 * e + 1], cs = c[pair + e], sn = s[pair + e];
+        x[8 * h + 2 * e] = fmaf(u, cs, -w * sn);
+        x[8 * h + 2 * e + 1] = fmaf(w, cs, u * sn);
       }
     }
+  } else if (j < rot / 16) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float u = x[e], w = x[e + 8], cs = c[8 * j + e], sn = s[8 * j + e];
+      x[e] = fmaf(u, cs, -w * sn);
+      x[e + 8] = fmaf(w, cs, u * sn);
+    }
   }
-  if (norm != nullptr || j < rot / 16) {       // (what passes keeps its bits)
+  if (norm != nullptr || rot > 0) {       // (what passes is rounded to what it was)
     *lo = pack8<TYPE>(x);
     *hi = pack8<TYPE>(x + 8);
   }
 }
 
 // ------------------------------------------------------------------- rows
-// Rows of q, and of k where there is no cache: row_tokens tokens' heads a workgroup.
-template <int TYPE, int D>
+// Rows of q, and of k where there is no cache: TOKENS tokens' heads a workgroup.
+// A thread has four items on their way at a time, the first of them before the
+// positions are known (of rows that are in no sequence they are not stored).
+constexpr int kBatch = 4;
+
+template <int TYPE, int D, int TOKENS>
 __device__ __forceinline__ void rotate_rows(const Rotate& a, uint32_t group, Turns& turns, int64_t* s_at) {
   constexpr int kItems = D / 16;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int64_t t0 = (int64_t)group * a.row_tokens;
-  for (int32_t i = wave; i < a.row_tokens; i += kWaves) {
+  const int64_t t0 = (int64_t)group * TOKENS;
+  const int32_t heads = a.q_heads + (a.pool.pages == nullptr && a.k_out.data != nullptr ? a.kv_heads : 0);
+  const uint32_t each = (uint32_t)heads * kItems, all = each * (uint32_t)min((int64_t)TOKENS, a.num_tokens - t0);
+  u4 lo[kBatch], hi[kBatch];
+  // an item's token, head and place in it
+  auto item = [&](uint32_t u, int* i, int32_t* h, int* j) {
+    *i = 0;
+#pragma unroll
+    for (int t = 1; t < TOKENS; ++t) *i += u >= t * each;
+    const uint32_t rest = u - *i * each;
+    *h = rest / kItems;
+    *j = rest % kItems;
+  };
+  auto load = [&](uint32_t u0) {
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const uint32_t u = u0 + b * kThreads;
+      if (u >= all) continue;
+      int i, j, p0, p1;
+      int32_t h;
+      item(u, &i, &h, &j);
+      pieces_of<D>(a, a.rot, j, &p0, &p1);
+      const bool is_q = h < a.q_heads;
+      const Rows& from = is_q ? a.q : a.k;
+      const uint16_t* x = (const uint16_t*)from.data + (t0 + i) * from.token + (is_q ? h : h - a.q_heads) * from.head;
+      lo[b] = *(const u4*)(x + 8 * p0);
+      hi[b] = *(const u4*)(x + 8 * p1);
+    }
+  };
+  load(tid);
+  for (int32_t i = wave; i < TOKENS; i += kWaves) {
     const int64_t t = t0 + i;
     int64_t position = -1;
     if (t < a.num_tokens) {
@@ -151,39 +212,41 @@ __device__ __forceinline__ void rotate_rows(const Rotate& a, uint32_t group, Tur
     if (position >= 0 && lane < a.rot / 2) turn(a, position, lane, &turns.c[i][lane], &turns.s[i][lane]);
   }
   __syncthreads();
-  const int32_t heads = a.q_heads + (a.pool.pages == nullptr && a.k_out.data != nullptr ? a.kv_heads : 0);
-  const uint32_t each = (uint32_t)heads * kItems, all = each * a.row_tokens;
-  for (uint32_t u = tid; u < all; u += kThreads) {
-    const uint32_t i = u / each, rest = u - i * each;
-    const int32_t h = rest / kItems, j = rest % kItems;
-    if (s_at[i] < 0) continue;
-    const bool is_q = h < a.q_heads;
-    const int32_t head = is_q ? h : h - a.q_heads;
-    const Rows& from = is_q ? a.q : a.k;
-    const OutRows& to = is_q ? a.q_out : a.k_out;
-    int p0, p1;
-    pieces_of(a, a.rot, j, &p0, &p1);
-    const uint16_t* x = (const uint16_t*)from.data + (t0 + i) * from.token + head * from.head;
-    u4 lo = *(const u4*)(x + 8 * p0), hi = *(const u4*)(x + 8 * p1);
-    rotate_item<TYPE, D>(a, is_q ? a.q_norm : a.k_norm, a.rot, j, p0, p1, turns.c[i], turns.s[i], &lo, &hi);
-    uint16_t* y = to.data + (t0 + i) * to.token + head * to.head;
-    *(u4*)(y + 8 * p0) = lo;
-    *(u4*)(y + 8 * p1) = hi;
+  for (uint32_t u0 = tid; u0 < all; u0 += kBatch * kThreads) {
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const uint32_t u = u0 + b * kThreads;
+      if (u >= all) continue;
+      int i, j, p0, p1;
+      int32_t h;
+      item(u, &i, &h, &j);
+      if (s_at[i] < 0) continue;
+      pieces_of<D>(a, a.rot, j, &p0, &p1);
+      const bool is_q = h < a.q_heads;
+      const OutRows& to = is_q ? a.q_out : a.k_out;
+      rotate_item<TYPE, D>(a, is_q ? a.q_norm : a.k_norm, a.rot, j, p0, p1, turns.c[i], turns.s[i], &lo[b], &hi[b]);
+      uint16_t* y = to.data + (t0 + i) * to.token + (is_q ? h : h - a.q_heads) * to.head;
+      *(u4*)(y + 8 * p0) = lo[b];
+      *(u4*)(y + 8 * p1) = hi[b];
+    }
+    load(u0 + kBatch * kThreads);
   }
 }
 
 // ------------------------------------------------------------------ blocks
-// A workgroup takes K or V of one block for four heads, a wavefront to a head;
-// blocks are found as an append finds them. HELD chunks of 16 tokens stay in
+// A workgroup takes K or V of one block, a wavefront to every fourth head of its
+// share of them (all, where there are blocks enough: their angles are computed
+// once); blocks are found as an append finds them. HELD chunks of 16 tokens stay in
 // registers from the maximum to the rounding; those of larger blocks are taken again.
 template <int TYPE, int FMT, int D, int HELD>
 __device__ __forceinline__ void rotate_block(const Rotate& a, uint32_t group, Turns& turns) {
   constexpr int kItems = D / 16;
   constexpr int kEach = kTokens * kItems / kWave;        // items of a chunk and lane: 2 (D = 128) or 1
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int32_t quads = (a.pool.heads + kWaves - 1) / kWaves;
-  const int64_t slot = group / (2 * quads);
-  const int32_t part = group % (2 * quads), is_v = part / quads, head = part % quads * kWaves + wave;
+  const int32_t shares = (a.pool.heads + a.share - 1) / a.share;
+  const int64_t slot = group / (2 * shares);
+  const int32_t part = group % (2 * shares), is_v = part / shares;
+  const int32_t head0 = part % shares * a.share, heads = min(a.share, a.pool.heads - head0);
   const int32_t lb = a.pool.log_block;
   const int32_t r = kv::last_at_most(a.n, slot, lane, [&](int32_t i) { return (a.offsets[i] >> lb) + 2 * (int64_t)i; });
   const int64_t start = a.offsets[r], first = max((int64_t)0, start), end = min(a.num_tokens, a.offsets[r + 1]);
@@ -199,112 +262,121 @@ __device__ __forceinline__ void rotate_block(const Rotate& a, uint32_t group, Tu
   }
   uint16_t* const k_out = is_v ? nullptr : a.k_out.data;
   if (!stored && k_out == nullptr) return;
-  const bool active = head < a.pool.heads;        // (the others stay for the barriers)
   const int32_t old = (int32_t)(from - (b << lb)), tokens = (int32_t)(to - from);
   const int32_t rot = is_v ? 0 : a.rot;
   const uint16_t* const norm = is_v ? nullptr : a.k_norm;
 
   const Rows src = is_v ? a.v : a.k;
   const int64_t row0 = first + from - ctx;
-  const uint16_t* x = (const uint16_t*)src.data + row0 * src.token + head * src.head;
-  uint16_t* y = k_out != nullptr ? k_out + row0 * a.k_out.token + head * a.k_out.head : nullptr;
-  const int64_t at = ((int64_t)page * 2 + is_v) * a.pool.heads + head;
-  uint8_t* codes = a.pool.pages + (at << lb) * D;
-  const float held = active && stored && old > 0 ? a.pool.scales[at] : 0.0f;
+  for (int32_t of = 0; of < heads; of += kWaves) {
+    const int32_t head = head0 + of + wave;
+    const bool active = of + wave < heads;        // (the others stay for the barriers)
+    const uint16_t* x = (const uint16_t*)src.data + row0 * src.token + head * src.head;
+    uint16_t* y = k_out != nullptr ? k_out + row0 * a.k_out.token + head * a.k_out.head : nullptr;
+    const int64_t at = ((int64_t)page * 2 + is_v) * a.pool.heads + head;
+    uint8_t* codes = a.pool.pages + (at << lb) * D;
+    const float held = active && stored && old > 0 ? a.pool.scales[at] : 0.0f;
 
-  u4 w[HELD][kEach][2];
-  // chunk c's rows as they go into the cache; `again`: those in k_out are ready
-  auto load = [&](int32_t c, u4 (*z)[2], bool again) {
-    if (rot > 0 && !again) {
-      __syncthreads();
-      const int32_t pairs = rot / 2;
-      for (int32_t i = tid; i < kTokens * pairs; i += kThreads) {
-        const int32_t t = i / pairs, p = i - t * pairs;
-        if (c * kTokens + t < tokens) turn(a, from + c * kTokens + t, p, &turns.c[t][p], &turns.s[t][p]);
+    u4 w[HELD][kEach][2];
+    // chunk c's rows as they go into the cache; `again`: those in k_out are ready
+    auto load = [&](int32_t c, u4 (*z)[2], bool again) {
+      if (rot > 0 && !again && (of == 0 || tokens > kTokens)) {      // (else they are there)
+        __syncthreads();
+        const int32_t pairs = rot / 2;
+        for (int32_t i = tid; i < kTokens * pairs; i += kThreads) {
+          const int32_t t = i / pairs, p = i - t * pairs;
+          if (c * kTokens + t < tokens) turn(a, from + c * kTokens + t, p, &turns.c[t][p], &turns.s[t][p]);
+        }
+        __syncthreads();
       }
-      __syncthreads();
-    }
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int32_t u = i * kWave + lane, t = c * kTokens + u / kItems, j = u % kItems;
-      z[i][0] = z[i][1] = (u4){};
-      if (!active || t >= tokens) continue;
-      int p0, p1;
-      pieces_of(a, rot, j, &p0, &p1);
-      const uint16_t* p = again ? y + t * a.k_out.token : x + t * src.token;
-      z[i][0] = *(const u4*)(p + 8 * p0);
-      z[i][1] = *(const u4*)(p + 8 * p1);
-      if (again) continue;
-      rotate_item<TYPE, D>(a, norm, rot, j, p0, p1, turns.c[u / kItems], turns.s[u / kItems], &z[i][0], &z[i][1]);
-      if (y != nullptr) {
-        *(u4*)(y + t * a.k_out.token + 8 * p0) = z[i][0];
-        *(u4*)(y + t * a.k_out.token + 8 * p1) = z[i][1];
+      for (int i = 0; i < kEach; ++i) {
+        const int32_t u = i * kWave + lane, t = c * kTokens + u / kItems, j = u % kItems;
+        z[i][0] = z[i][1] = (u4){};
+        if (!active || t >= tokens) continue;
+        int p0, p1;
+        pieces_of<D>(a, rot, j, &p0, &p1);
+        const uint16_t* p = again ? y + t * a.k_out.token : x + t * src.token;
+        z[i][0] = *(const u4*)(p + 8 * p0);
+        z[i][1] = *(const u4*)(p + 8 * p1);
+        if (again) continue;
+        rotate_item<TYPE, D>(a, norm, rot, j, p0, p1, turns.c[u / kItems], turns.s[u / kItems], &z[i][0], &z[i][1]);
+        if (y != nullptr) {
+          *(u4*)(y + t * a.k_out.token + 8 * p0) = z[i][0];
+          *(u4*)(y + t * a.k_out.token + 8 * p1) = z[i][1];
+        }
       }
-    }
-  };
-  float most = 0.0f;
-  bool plain = true;
-  auto look = [&](const u4 (*z)[2]) {
+    };
+    const int32_t chunks = (tokens + kTokens - 1) / kTokens;
+    const bool kept = chunks <= HELD;
+    uint32_t bits = 0;
+    float most = 0.0f;                // finite magnitudes of chunks that are not held
 #pragma unroll
-    for (int i = 0; i < 2 * kEach; ++i) {
-      float f[8];
-      spread8<TYPE>(z[i / 2][i % 2], f);
+    for (int c = 0; c < HELD; ++c) {
+      if (c < chunks) {
+        load(c, w[c], false);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float m = fabsf(f[e]);
-        plain = plain && m < __builtin_inff();
-        most = fmaxf(most, m < __builtin_inff() ? m : 0.0f);
+        for (int i = 0; i < 2 * kEach; ++i) bits = largest8(w[c][i / 2][i % 2], bits);
       }
     }
-  };
-  const int32_t chunks = (tokens + kTokens - 1) / kTokens;
-  const bool kept = chunks <= HELD;
-#pragma unroll
-  for (int c = 0; c < HELD; ++c) {
-    if (c < chunks) {
-      load(c, w[c], false);
-      look(w[c]);
-    }
-  }
-  for (int32_t c = HELD; c < chunks; ++c) {
-    u4 z[kEach][2];
-    load(c, z, false);
-    look(z);
-  }
-  if (!stored) return;
-  float scale = scale_of<FMT>(wave_max(most));
-  plain = __all(plain) && scale < kv::kScaleMax;
-  if (old > 0 && !(scale > held)) scale = held;
-  const float inv = 1.0f / scale;
-  if (active && old > 0 && scale > held) rescale<FMT>(codes, old * D, held, scale, inv, lane);
-  auto store = [&](int32_t c, const u4 (*z)[2]) {
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int32_t u = i * kWave + lane, t = c * kTokens + u / kItems, j = u % kItems;
-      if (!active || t >= tokens) continue;
-      int p[2];
-      pieces_of(a, rot, j, &p[0], &p[1]);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float f[8];
-        spread8<TYPE>(z[i][h], f);
-        *(u2*)(codes + (old + t) * D + p[h] * 8) =
-            (u2){codes_of<FMT>(f, scale, inv, plain), codes_of<FMT>(f + 4, scale, inv, plain)};
-      }
-    }
-  };
-  if (kept) {
-#pragma unroll
-    for (int c = 0; c < HELD; ++c)
-      if (c < chunks) store(c, w[c]);
-  } else {
-    for (int32_t c = 0; c < chunks; ++c) {
+    for (int32_t c = HELD; c < chunks; ++c) {
       u4 z[kEach][2];
-      load(c, z, y != nullptr);
-      store(c, z);
+      load(c, z, false);
+#pragma unroll
+      for (int i = 0; i < 2 * kEach; ++i) {
+        bits = largest8(z[i / 2][i % 2], bits);
+        most = finite8<TYPE>(z[i / 2][i % 2], most);
+      }
     }
+    if (!stored) continue;
+    bits = wave_largest(bits);
+    bool plain = bits < kInfinity<TYPE>;
+    if (plain) {
+      most = kv::to_float<TYPE>((uint16_t)bits);
+    } else {
+#pragma unroll
+      for (int c = 0; c < HELD; ++c) {
+        if (c < chunks) {
+#pragma unroll
+          for (int i = 0; i < 2 * kEach; ++i) most = finite8<TYPE>(w[c][i / 2][i % 2], most);
+        }
+      }
+      most = wave_max(most);
+    }
+    float scale = scale_of<FMT>(most);
+    plain = plain && scale < kv::kScaleMax;
+    if (old > 0 && !(scale > held)) scale = held;
+    const float inv = 1.0f / scale;
+    if (active && old > 0 && scale > held) rescale<FMT>(codes, old * D, held, scale, inv, lane);
+    auto store = [&](int32_t c, const u4 (*z)[2]) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int32_t u = i * kWave + lane, t = c * kTokens + u / kItems, j = u % kItems;
+        if (!active || t >= tokens) continue;
+        int p[2];
+        pieces_of<D>(a, rot, j, &p[0], &p[1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float f[8];
+          spread8<TYPE>(z[i][h], f);
+          *(u2*)(codes + (old + t) * D + p[h] * 8) =
+              (u2){codes_of<FMT>(f, scale, inv, plain), codes_of<FMT>(f + 4, scale, inv, plain)};
+        }
+      }
+    };
+    if (kept) {
+#pragma unroll
+      for (int c = 0; c < HELD; ++c)
+        if (c < chunks) store(c, w[c]);
+    } else {
+      for (int32_t c = 0; c < chunks; ++c) {
+        u4 z[kEach][2];
+        load(c, z, y != nullptr);
+        store(c, z);
+      }
+    }
+    if (active && lane == 0) a.pool.scales[at] = scale;
   }
-  if (active && lane == 0) a.pool.scales[at] = scale;
 }
 
 template <int TYPE, int FMT, int D, int HELD>
@@ -312,7 +384,8 @@ __global__ __launch_bounds__(kThreads) void k_rotate_append(Rotate a) {
   __shared__ Turns s_turns;
   __shared__ int64_t s_at[kTokens];
   if (blockIdx.x < a.page_groups) rotate_block<TYPE, FMT, D, HELD>(a, blockIdx.x, s_turns);
-  else rotate_rows<TYPE, D>(a, blockIdx.x - a.page_groups, s_turns, s_at);
+  else if (a.row_tokens == 1) rotate_rows<TYPE, D, 1>(a, blockIdx.x - a.page_groups, s_turns, s_at);
+  else rotate_rows<TYPE, D, kRowTokens>(a, blockIdx.x - a.page_groups, s_turns, s_at);
 }
 
 // -------------------------------------------------------------------- read
@@ -466,9 +539,10 @@ peek_status peek_rotate_append(const peek_kv_pool* pool, int32_t n, int64_t num_
     if (!d_offsets || !d_context)
       return fail(PEEK_ERR_INVALID_ARGUMENT, "d_offsets and d_context must not be NULL");
     a.slots = pool ? (num_tokens >> a.pool.log_block) + 2 * (int64_t)n : 0;
-    const int64_t pages = a.slots * 2 * ((kv_heads + kWaves - 1) / kWaves);
+    a.share = a.slots >= kManyBlocks ? kv_heads : kWaves;
+    const int64_t pages = a.slots * 2 * ((kv_heads + a.share - 1) / a.share);
     const int32_t row_heads = q_heads + (!pool && d_k_out ? kv_heads : 0);
-    a.row_tokens = num_tokens >= 4096 ? 4 : 1;
+    a.row_tokens = num_tokens >= 4096 ? kRowTokens : 1;
     const int64_t rows = row_heads > 0 ? (num_tokens + a.row_tokens - 1) / a.row_tokens : 0;
     if (pages >= (1 << 24) || rows >= (1 << 24))
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many tokens for one call (%lld)", (long long)num_tokens);

@@ -32,6 +32,8 @@ constexpr int kThreads = kWave * kWaves;
 // ------------------------------------------------------------------ bounds
 // A wavefront takes every splits-th block of a sequence for one head.
 
+constexpr int64_t kBoundsWaves = 8192;      // wavefronts of a call, where the sequences are fewer
+
 struct Bounds {
   Pool pool;
   const int32_t* first;       // null: from the first token on
@@ -69,27 +71,45 @@ __device__ __forceinline__ int32_t bound_of(uint8_t o, bool up) {
   }
 }
 
+// What the lane 4, or 8, places round the 16 has.
+__device__ __forceinline__ uint32_t round4(uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, true); }
+__device__ __forceinline__ uint32_t round8(uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, true); }
+
+// Two words of every lane to one: joined over the lanes 32 (or 16) apart, the first word in the lower of them and the
+// second in the upper.
+template <typename F>
+__device__ __forceinline__ uint32_t fold32(uint32_t a, uint32_t b, F&& join) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  return join((uint32_t)r[0], (uint32_t)r[1]);
+}
+template <typename F>
+__device__ __forceinline__ uint32_t fold16(uint32_t a, uint32_t b, F&& join) {
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  return join((uint32_t)r[0], (uint32_t)r[1]);
+}
+
 template <int FMT, int D>
 __global__ __launch_bounds__(kThreads) void k_kv_bounds(Bounds a) {
-  constexpr int kLanes = D / 16;              // of a token
+  constexpr int kLanes = D / 16;              // of a token, 16 codes to a lane
   constexpr int kStep = kWave / kLanes;       // tokens a load
   const int lane = threadIdx.x & (kWave - 1);
-  int64_t unit = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  uint32_t unit = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int32_t heads = a.pool.heads, lb = a.pool.log_block;
-  const int32_t head = (int32_t)(unit % heads);
+  const int32_t head = unit % heads;
   unit /= heads;
-  const int32_t split = (int32_t)(unit % a.splits);
-  const int32_t r = (int32_t)(unit / a.splits);
+  const int32_t split = unit % a.splits, r = unit / a.splits;
   if (r >= a.n) return;
   const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb);
   const int32_t first = a.first ? max(0, a.first[r]) : 0;
   const int32_t blocks = (int32_t)(((int64_t)held + (1 << lb) - 1) >> lb);
   const int32_t at = lane % kLanes, sub = lane / kLanes;
+  const bool upper32 = lane >= 32, upper16 = lane & 16, upper8 = lane & 8;
   for (int64_t b = (first >> lb) + split; b < blocks; b += a.splits) {
     const uint32_t page = kv::page_of(a.table, a.pool, r, (int32_t)b);
     const int32_t tokens = min(1 << lb, held - ((int32_t)b << lb));
     const uint8_t* codes = a.pool.pages + (((int64_t)page * 2 * heads + head) << lb) * D + at * 16;
-    uint32_t hi[8], lo[8];        // bytes 1, 3 of every word in the upper halves of 16 bits, then bytes 0, 2
+    const bool turned = a.pool.scales[(int64_t)page * 2 * heads + head] < 0.0f;
+    uint32_t hi[8], lo[8];        // of word e bytes 1 and 3, in the upper halves of 16 bits, at 2 e; bytes 0 and 2 after it
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       hi[e] = 0x80008000u;
@@ -110,38 +130,46 @@ __global__ __launch_bounds__(kThreads) void k_kv_bounds(Bounds a) {
           lo[2 * e + 1] = min2(lo[2 * e + 1], even);
         }
     }
+    // Over the lanes of the same codes, half of the words going with each step: a lane ends with one of
+    // the eight, of word 2 upper8 + upper16 the bytes 1 and 3 (or 0 and 2, upper32).
+    auto over_lanes = [&](const uint32_t* x, auto join) {
+      uint32_t y[4], z[2];
 #pragma unroll
-    for (int d = kLanes; d < kWave; d <<= 1)
+      for (int e = 0; e < 4; ++e) y[e] = fold32(x[2 * e], x[2 * e + 1], join);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        hi[e] = max2(hi[e], __shfl_xor(hi[e], d));
-        lo[e] = min2(lo[e], __shfl_xor(lo[e], d));
+      for (int e = 0; e < 2; ++e) {
+        z[e] = fold16(y[2 * e], y[2 * e + 1], join);
+        if constexpr (kLanes == 4) z[e] = join(z[e], round4(z[e]));
       }
-    const bool turned = a.pool.scales[(int64_t)page * 2 * heads + head] < 0.0f;
-    if (sub < 2) {                // the first kLanes lanes write hi, the next lo
-      const bool up = sub == 0;
-      u4 out;
+      return join(upper8 ? z[1] : z[0], round8(upper8 ? z[0] : z[1]));
+    };
+    const uint32_t top = over_lanes(hi, [](uint32_t x, uint32_t y) { return max2(x, y); });
+    const uint32_t bottom = over_lanes(lo, [](uint32_t x, uint32_t y) { return min2(x, y); });
+    int32_t up[2], down[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool from_hi = up != turned;
-        const uint32_t odd = from_hi ? hi[2 * e] : lo[2 * e], even = from_hi ? hi[2 * e + 1] : lo[2 * e + 1];
-        const uint32_t o = (odd & 0xff00ff00u) | ((even >> 8) & 0x00ff00ffu);
-        uint32_t word = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int32_t x = bound_of<FMT>((uint8_t)(o >> (8 * i)), from_hi);
-          word |= (uint32_t)(uint8_t)(turned ? -x : x) << (8 * i);
-        }
-        out[e] = word;
+    for (int i = 0; i < 2; ++i) {
+      up[i] = bound_of<FMT>((uint8_t)(top >> (16 * i + 8)), true);
+      down[i] = bound_of<FMT>((uint8_t)(bottom >> (16 * i + 8)), false);
+      if (turned) {
+        const int32_t x = up[i];
+        up[i] = -down[i];
+        down[i] = -x;
       }
-      *(u4*)(a.out + (((int64_t)page * heads + head) * 2 + sub) * D + at * 16) = out;
     }
+    auto word = [&](const int32_t* x) {        // bytes 0 and 2, or 1 and 3
+      const uint32_t w = (uint32_t)(uint8_t)x[0] | (uint32_t)(uint8_t)x[1] << 16;
+      return upper32 ? w : w << 8;
+    };
+    // the lower lanes write the largest, the upper ones the smallest
+    const uint32_t out = fold32(word(up), word(down), [](uint32_t x, uint32_t y) { return x | y; });
+    const int32_t e = 2 * upper8 + upper16;
+    *(uint32_t*)(a.out + (((int64_t)page * heads + head) * 2 + upper32) * D + at * 16 + e * 4) = out;
   }
 }
 
 // ------------------------------------------------------------------ scores
-// A wavefront takes 64 blocks of one (sequence, kv head): queries times bounds,
-// 16 queries by 16 blocks by 64 elements a matrix instruction.
+// A wavefront takes 64 blocks at a time of one (sequence, kv head): queries times
+// bounds, 16 queries by 16 blocks by 64 elements a matrix instruction.
 
 struct Select {
   Pool pool;
@@ -159,50 +187,32 @@ constexpr int kSpan = 64;     // blocks of a wavefront
 
 typedef int32_t i4 __attribute__((ext_vector_type(4)));
 
-template <int TYPE, int FMT, int D>
-__global__ __launch_bounds__(kThreads) void k_block_scores(Select a, int32_t spans) {
-  constexpr int kSteps = D / 64;
-  const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
-  int64_t unit = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int32_t heads = a.pool.heads, lb = a.pool.log_block;
-  const int32_t head = (int32_t)(unit % heads);
-  unit /= heads;
-  const int32_t span = (int32_t)(unit % spans), r = (int32_t)(unit / spans);
-  if (r >= a.n) return;
-  const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb);
-  const int32_t blocks = (int32_t)(((int64_t)held + (1 << lb) - 1) >> lb), b0 = span * kSpan;
-  if (b0 >= blocks || blocks <= a.keep) return;        // (all of them are kept)
+constexpr int64_t kScoreWaves = 4096;      // wavefronts of a call, where these have 64 blocks each or more
 
-  const int32_t mine = min(b0 + lane, blocks - 1);
-  const uint32_t page = kv::page_of(a.table, a.pool, r, mine);
-  const float step = fabsf(a.pool.scales[(int64_t)page * 2 * heads + head]) * (FMT == PEEK_TYPE_F8E4M3 ? 4.0f : 1.0f);
-  u4 bounds[4][2 * kSteps];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t p = __shfl(page, 16 * i + col);
-    const int8_t* from = a.bounds + ((int64_t)p * heads + head) * 2 * D + grp * 16;
-#pragma unroll
-    for (int s = 0; s < 2 * kSteps; ++s) bounds[i][s] = *(const u4*)(from + s * 64);
-  }
-  float best[4] = {-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
-  for (int32_t row0 = 0; row0 < a.group; row0 += 16) {
-    // lane l: row row0 + l % 16 (past the last: the last again), elements 16 (l / 16) .. + 15 of every 64
-    const uint16_t* q = (const uint16_t*)a.q.data + (int64_t)r * a.q.token +
-        (int64_t)(head * a.group + min(row0 + col, a.group - 1)) * a.q.head + grp * 16;
+// Queries as whole numbers: lane l has row row0 + l % 16 (past the last: the last again), elements 16 (l / 16) .. + 15
+// of every 64; positive ones in `up`, negative ones in `down`.
+template <int TYPE, int D>
+struct Query {
+  static constexpr int kSteps = D / 64;
+  u4 up[kSteps], down[kSteps];
+  float of_row[4];            // the units of the rows that this lane's products belong to
+
+  __device__ __forceinline__ void take(const uint16_t* q, int lane) {
     float x[kSteps][16];
     float most = 0.0f;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s)
+    for (int s = 0; s < kSteps; ++s) {
+      const u4 w[2] = {*(const u4*)(q + s * 64), *(const u4*)(q + s * 64 + 8)};
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const uint32_t w = (*(const u4*)(q + s * 64 + (e >> 3) * 8))[(e >> 1) & 3];
-        x[s][e] = kv::to_float<TYPE>((uint16_t)(w >> (16 * (e & 1))));
+        const uint32_t u = w[e >> 3][(e >> 1) & 3];
+        x[s][e] = kv::to_float<TYPE>((uint16_t)(u >> (16 * (e & 1))));
         const float m = fabsf(x[s][e]);
         most = fmaxf(most, m < __builtin_inff() ? m : 0.0f);
       }
+    }
     most = max_halves(swap16_max(most));
     const int32_t e = __builtin_amdgcn_frexp_expf(most) - 7;
-    u4 up[kSteps], down[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
 #pragma unroll
@@ -218,49 +228,104 @@ __global__ __launch_bounds__(kThreads) void k_block_scores(Select a, int32_t spa
         up[s][w] = u;
         down[s][w] = v;
       }
-    int32_t of_row[4];          // exponents of the rows that this lane's products belong to
+    const float unit = __builtin_ldexpf(1.0f, e);       // 2^-139 to 2^121
 #pragma unroll
-    for (int v = 0; v < 4; ++v) of_row[v] = __shfl(e, 4 * grp + v);
+    for (int v = 0; v < 4; ++v) of_row[v] = __shfl(unit, 4 * (lane >> 4) + v);
+  }
+};
+
+template <int TYPE, int FMT, int D>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) void k_block_scores(Select a, int32_t waves) {
+  constexpr int kSteps = D / 64;
+  const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
+  uint32_t unit = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int32_t heads = a.pool.heads, lb = a.pool.log_block;
+  const int32_t head = unit % heads;
+  unit /= heads;
+  const int32_t wave = unit % waves, r = unit / waves;
+  if (r >= a.n) return;
+  const uint16_t* q = (const uint16_t*)a.q.data + (int64_t)r * a.q.token + grp * 16;
+  auto q_row = [&](int32_t row0) { return q + (int64_t)(head * a.group + min(row0 + col, a.group - 1)) * a.q.head; };
+  const int32_t held = kv::clip_tokens(a.context[r], a.table.width, lb);
+  const int32_t blocks = (int32_t)(((int64_t)held + (1 << lb) - 1) >> lb);
+  if (blocks <= a.keep) return;        // (all of them are kept)
+  Query<TYPE, D> query;
+  int32_t row_at = -1;                 // whose rows `query` has
+  auto entry = [&](int64_t b0) { return a.table.ids[(int64_t)r * a.table.stride + min(b0 + lane, (int64_t)blocks - 1)]; };
+  uint32_t next = (uint32_t)entry((int64_t)wave * kSpan);
+  for (int64_t b0 = (int64_t)wave * kSpan; b0 < blocks; b0 += (int64_t)waves * kSpan) {
+    const uint32_t page = next < a.pool.num_pages ? next : 0u;
+    next = (uint32_t)entry(b0 + (int64_t)waves * kSpan);
+    u4 bounds[4][2 * kSteps];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      i4 dot = {};
+      const uint32_t p = __shfl(page, 16 * i + col);
+      const int8_t* from = a.bounds + ((int64_t)p * heads + head) * 2 * D + grp * 16;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4, up[s]), __builtin_bit_cast(i4, bounds[i][s]),
-                                                    dot, 0, 0, 0);
-        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4, down[s]),
-                                                    __builtin_bit_cast(i4, bounds[i][kSteps + s]), dot, 0, 0, 0);
+      for (int s = 0; s < 2 * kSteps; ++s) bounds[i][s] = *(const u4*)(from + s * 64);
+    }
+    const float step = fabsf(a.pool.scales[(int64_t)page * 2 * heads + head]) * (FMT == PEEK_TYPE_F8E4M3 ? 4.0f : 1.0f);
+    float best[4] = {-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
+    for (int32_t row0 = 0; row0 < a.group; row0 += 16) {
+      if (row_at != row0) {
+        query.take(q_row(row0), lane);
+        row_at = row0;
       }
 #pragma unroll
-      for (int v = 0; v < 4; ++v) best[i] = fmaxf(best[i], __builtin_ldexpf((float)dot[v], of_row[v]));
-    }
-  }
-  // block 16 i + col of every i, for all rows; lane l keeps that of block l
-  float score = 0.0f;
+      for (int i = 0; i < 4; ++i) {
+        i4 dot = {};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float top = max_halves(swap16_max(best[i]));
-    score = grp == i ? top : score;
+        for (int s = 0; s < kSteps; ++s) {
+          dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4, query.up[s]),
+                                                      __builtin_bit_cast(i4, bounds[i][s]), dot, 0, 0, 0);
+          dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4, query.down[s]),
+                                                      __builtin_bit_cast(i4, bounds[i][kSteps + s]), dot, 0, 0, 0);
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v) best[i] = fmaxf(best[i], (float)dot[v] * query.of_row[v]);
+      }
+    }
+    // block 16 i + col of every i, for all rows; lane l keeps that of block l
+    float score = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float top = max_halves(swap16_max(best[i]));
+      score = grp == i ? top : score;
+    }
+    if (b0 + lane < blocks)
+      a.scores[((int64_t)r * heads + head) * a.table.width + b0 + lane] = score * step + 0.0f;      // (no -0)
   }
-  if (b0 + lane < blocks)
-    a.scores[((int64_t)r * heads + head) * a.table.width + b0 + lane] = score * step + 0.0f;      // (no -0)
 }
 
 // ------------------------------------------------------------------ choice
 // A workgroup takes one (sequence, kv head). The candidates' scores, as whole
 // numbers in their order, are counted by digits of 8 bits from the top: after
-// four passes the least score to stay and how many of that score are known.
+// four passes the least score to stay and how many of that score are known. One barrier a
+// pass: every wavefront sums the counts for itself, and clears the other
+// pass's while this one's are made.
 
 __device__ __forceinline__ uint32_t rank_of(float x) {       // NaN above all
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
   return x != x ? 0xffffffffu : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// The sum of the lanes up to this one.
+__device__ __forceinline__ uint32_t sum_to(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // within 16 lanes: from 1, 2, 4, 8 lanes below
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // lane 15 to the next 16, 47 too
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // lane 31 to the upper 32
+  return x;
+}
+
+constexpr int kHeld = 8;      // scores of a thread that stay in registers; where there are more, they are read again
+
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_block_select(Select a) {
   constexpr int kWaves = THREADS / kWave;
-  __shared__ uint32_t s_count[kWaves][256];
-  __shared__ uint32_t s_digit, s_left;
+  __shared__ uint32_t s_count[2][kWaves][256];
   __shared__ uint32_t s_more[kWaves], s_equal[kWaves];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int32_t heads = a.pool.heads, lb = a.pool.log_block;
@@ -280,60 +345,80 @@ __global__ __launch_bounds__(THREADS) void k_block_select(Select a) {
   }
   const float* scores = a.scores + unit * a.table.width;
   const int32_t lo = a.sink, hi = blocks - a.recent;          // candidates (blocks > keep >= sink + recent)
-  uint32_t prefix = 0, left = (uint32_t)(a.keep - a.sink - a.recent);      // so many of the candidates stay
-  for (int shift = 24; shift >= 0 && left > 0; shift -= 8) {
-    for (int32_t i = tid; i < kWaves * 256; i += THREADS) (&s_count[0][0])[i] = 0;
-    __syncthreads();
-    for (int32_t b = lo + tid; b < hi; b += THREADS) {
-      const uint32_t x = rank_of(scores[b]);
-      if (shift == 24 || (x ^ prefix) >> (shift + 8) == 0) atomicAdd(&s_count[wave][(x >> shift) & 255], 1u);
+  // A wavefront has blocks in order, 64 after 64; block b is a candidate's rank, or must stay.
+  const int32_t share = (int32_t)(((int64_t)blocks + THREADS - 1) / THREADS) * kWave;
+  const int32_t from = (int32_t)min((int64_t)wave * share, (int64_t)blocks), to = min(blocks - from, share) + from;
+  const bool fits = share <= kHeld * kWave;
+  auto read = [&](int32_t b) { return b < to && b >= lo && b < hi ? rank_of(scores[b]) : 0u; };
+  uint32_t x[kHeld];
+  if (fits) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) x[i] = read(from + i * kWave + lane);
+  }
+  auto each = [&](auto f) {          // f(block, rank) of this lane's blocks, up to the end of the share and beyond
+    if (fits) {
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (from + i * kWave < to) f(from + i * kWave + lane, x[i]);
+    } else {
+      for (int32_t b = from; b < to; b += kWave) f(b + lane, read(b + lane));
     }
-    __syncthreads();
-    if (wave == 0) {            // lane l: digits 255 - 4 l .. 252 - 4 l
-      uint32_t c[4], sum = 0;
+  };
+  uint32_t prefix = 0, left = (uint32_t)(a.keep - a.sink - a.recent);      // so many of the candidates stay
+  const bool any = left > 0;
+  if (any) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        c[e] = 0;
-        for (int w = 0; w < kWaves; ++w) c[e] += s_count[w][255 - 4 * lane - e];
-        sum += c[e];
-      }
-      uint32_t before = sum;
+    for (int e = 0; e < 4; ++e) s_count[0][wave][4 * lane + e] = 0;
+    __builtin_amdgcn_wave_barrier();
+    for (int pass = 0; pass < 4; ++pass) {
+      const int shift = 24 - 8 * pass;
+      uint32_t(*count)[256] = s_count[pass & 1];
+      // (lanes of one digit counted as one, by ballots, took 1.5 to 2.5 us more than these)
+      each([&](int32_t b, uint32_t rank) {
+        if (b < to && b >= lo && b < hi && (pass == 0 || (rank ^ prefix) >> (shift + 8) == 0))
+          atomicAdd(&count[wave][(rank >> shift) & 255], 1u);
+      });
+      __syncthreads();
+      // (a wavefront clears its own counts for the next pass: they were last read before this barrier)
 #pragma unroll
-      for (int d = 1; d < kWave; d <<= 1) {
-        const uint32_t x = __shfl_up(before, d);
-        if (lane >= d) before += x;
+      for (int e = 0; e < 4; ++e) s_count[(pass + 1) & 1][wave][4 * lane + e] = 0;
+      uint32_t c[4] = {}, sum = 0;      // lane l: digits 255 - 4 l .. 252 - 4 l
+      for (int w = 0; w < kWaves; ++w) {
+        const u4 v = *(const u4*)&count[w][252 - 4 * lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] += v[3 - e];
       }
-      before -= sum;
+      sum = c[0] + c[1] + c[2] + c[3];
+      uint32_t before = sum_to(sum) - sum;
+      uint32_t digit = 0, rest = 0;
+      bool here = false;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (before < left && left <= before + c[e]) {
-          s_digit = 255 - 4 * lane - e;
-          s_left = left - before;
+          digit = 255 - 4 * lane - e;
+          rest = left - before;
+          here = true;
         }
         before += c[e];
       }
+      const int from_lane = __builtin_ctzll(__ballot(here) | 1ull << 63);
+      prefix |= (uint32_t)__builtin_amdgcn_readlane(digit, from_lane) << shift;
+      left = __builtin_amdgcn_readlane(rest, from_lane);
     }
-    __syncthreads();
-    prefix |= s_digit << shift;
-    left = s_left;
   }
-  // a wavefront's share of the blocks in order: counted, then placed
-  const int32_t share = ((blocks + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
-  const int32_t from = min(wave * share, blocks), to = min(from + share, blocks);
-  const bool any = a.keep > a.sink + a.recent;
-  auto look = [&](int32_t b, bool* more, bool* equal) {
-    const bool must = b < lo || b >= hi, in = b < to;
-    const uint32_t x = in && !must ? rank_of(scores[b]) : 0u;
-    *more = in && (must || (any && x > prefix));
-    *equal = in && !must && any && x == prefix;
+  // counted, then placed
+  auto look = [&](int32_t b, uint32_t rank, bool* more, bool* equal) {
+    const bool in = b < to, must = b < lo || b >= hi;
+    *more = in && (must || (any && rank > prefix));
+    *equal = in && !must && any && rank == prefix;
   };
   uint32_t more = 0, equal = 0;
-  for (int32_t b = from; b < to; b += kWave) {
+  each([&](int32_t b, uint32_t rank) {
     bool m, e;
-    look(b + lane, &m, &e);
+    look(b, rank, &m, &e);
     more += __popcll(__ballot(m));
     equal += __popcll(__ballot(e));
-  }
+  });
   if (lane == 0) {
     s_more[wave] = more;
     s_equal[wave] = equal;
@@ -346,16 +431,16 @@ __global__ __launch_bounds__(THREADS) void k_block_select(Select a) {
   }
   place += min(ties, left);
   const uint64_t below = (1ull << lane) - 1;
-  for (int32_t b = from; b < to; b += kWave) {
+  each([&](int32_t b, uint32_t rank) {
     bool m, e;
-    look(b + lane, &m, &e);
+    look(b, rank, &m, &e);
     const uint64_t equals = __ballot(e);
     const bool stays = m || (e && ties + (uint32_t)__popcll(equals & below) < left);
     const uint64_t all = __ballot(stays);
-    if (stays) out[place + __popcll(all & below)] = ids[b + lane];
+    if (stays) out[place + __popcll(all & below)] = ids[b];
     place += __popcll(all);
     ties += __popcll(equals);
-  }
+  });
 }
 
 int64_t score_bytes(int32_t n, int32_t heads, int32_t width) {
@@ -384,7 +469,7 @@ peek_status peek_kv_bounds(const peek_kv_pool* pool, int32_t n, const int32_t* d
     if ((reinterpret_cast<uintptr_t>(d_bounds) & 15) != 0)
       return fail(PEEK_ERR_INVALID_ARGUMENT, "d_bounds must be 16-byte aligned");
     const int64_t units = (int64_t)n * a.pool.heads;
-    a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(max_blocks, 16384 / units));
+    a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(max_blocks, kBoundsWaves / units));
     const int64_t groups = (units * a.splits + kWaves - 1) / kWaves;
     if (groups >= (1 << 24)) return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
     hipStream_t st = (hipStream_t)stream;
@@ -440,7 +525,8 @@ peek_status peek_block_select(const peek_kv_pool* pool, const int8_t* d_bounds, 
     if (s != PEEK_OK) return s;
     const int64_t units = (int64_t)n * a.pool.heads;
     const int32_t spans = (max_blocks + kSpan - 1) / kSpan;
-    const int64_t groups = (units * spans + kWaves - 1) / kWaves;
+    const int32_t waves = (int32_t)std::max<int64_t>(1, std::min<int64_t>(spans, kScoreWaves / units));
+    const int64_t groups = (units * waves + kWaves - 1) / kWaves;
     if (groups >= (1 << 24) || units >= (1 << 24))
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
     hipStream_t st = (hipStream_t)stream;
@@ -461,12 +547,16 @@ peek_status peek_block_select(const peek_kv_pool* pool, const int8_t* d_bounds, 
     a.recent = recent;
     if (max_blocks > keep) {        // (otherwise all blocks are kept)
       with_types(type, pool->type, pool->head_dim, [&](auto t, auto f, auto d) {
-        hipLaunchKernelGGL((k_block_scores<t(), f(), d()>), dim3((unsigned)groups), dim3(kThreads), 0, st, a, spans);
+        hipLaunchKernelGGL((k_block_scores<t(), f(), d()>), dim3((unsigned)groups), dim3(kThreads), 0, st, a, waves);
       });
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess) {
-      hipLaunchKernelGGL((k_block_select<1024>), dim3((unsigned)units), dim3(1024), 0, st, a);
+      auto go = [&](auto kernel, int threads) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3((unsigned)threads), 0, st, a);
+      };
+      if (max_blocks <= kHeld * 256) go(k_block_select<256>, 256);
+      else go(k_block_select<1024>, 1024);
       e = hipGetLastError();
     }
     if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "selection launch failed: %s", hipGetErrorString(e));
