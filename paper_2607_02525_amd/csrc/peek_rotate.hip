@@ -278,9 +278,22 @@ __device__ __forceinline__ void rotate_block(const Rotate& a, uint32_t group, Tu
     const float held = active && stored && old > 0 ? a.pool.scales[at] : 0.0f;
 
     u4 w[HELD][kEach][2];
-    // chunk c's rows as they go into the cache; `again`: those in k_out are ready
+    // chunk c's rows as they go into the cache; `again`: those in k_out are ready. The rows are on their way while
+    // the angles are computed.
     auto load = [&](int32_t c, u4 (*z)[2], bool again) {
-      if (rot > 0 && !again && (of == 0 || tokens > kTokens)) {      // (else they are there)
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int32_t u = i * kWave + lane, t = c * kTokens + u / kItems, j = u % kItems;
+        z[i][0] = z[i][1] = (u4){};
+        if (!active || t >= tokens) continue;
+        int p0, p1;
+        pieces_of<D>(a, rot, j, &p0, &p1);
+        const uint16_t* p = again ? y + t * a.k_out.token : x + t * src.token;
+        z[i][0] = *(const u4*)(p + 8 * p0);
+        z[i][1] = *(const u4*)(p + 8 * p1);
+      }
+      if (again) return;
+      if (rot > 0 && (of == 0 || tokens > kTokens)) {      // (else they are there)
         __syncthreads();
         const int32_t pairs = rot / 2;
         for (int32_t i = tid; i < kTokens * pairs; i += kThreads) {
@@ -292,14 +305,9 @@ __device__ __forceinline__ void rotate_block(const Rotate& a, uint32_t group, Tu
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         const int32_t u = i * kWave + lane, t = c * kTokens + u / kItems, j = u % kItems;
-        z[i][0] = z[i][1] = (u4){};
         if (!active || t >= tokens) continue;
         int p0, p1;
         pieces_of<D>(a, rot, j, &p0, &p1);
-        const uint16_t* p = again ? y + t * a.k_out.token : x + t * src.token;
-        z[i][0] = *(const u4*)(p + 8 * p0);
-        z[i][1] = *(const u4*)(p + 8 * p1);
-        if (again) continue;
         rotate_item<TYPE, D>(a, norm, rot, j, p0, p1, turns.c[u / kItems], turns.s[u / kItems], &z[i][0], &z[i][1]);
         if (y != nullptr) {
           *(u4*)(y + t * a.k_out.token + 8 * p0) = z[i][0];

@@ -187,7 +187,7 @@ constexpr int kSpan = 64;     // blocks of a wavefront
 
 typedef int32_t i4 __attribute__((ext_vector_type(4)));
 
-constexpr int64_t kScoreWaves = 4096;      // wavefronts of a call, where these have 64 blocks each or more
+constexpr int64_t kScoreWaves = 16384;      // wavefronts of a call, where these have 64 blocks each or more
 
 // Queries as whole numbers: lane l has row row0 + l % 16 (past the last: the last again), elements 16 (l / 16) .. + 15
 // of every 64; positive ones in `up`, negative ones in `down`.
@@ -299,10 +299,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) v
 
 // ------------------------------------------------------------------ choice
 // A workgroup takes one (sequence, kv head). The candidates' scores, as whole
-// numbers in their order, are counted by digits of 8 bits from the top: after
-// four passes the least score to stay and how many of that score are known. One barrier a
-// pass: every wavefront sums the counts for itself, and clears the other
-// pass's while this one's are made.
+// numbers in their order, are counted by digits of 8 bits from the first bit in
+// which they differ: after three or four passes the least score to stay and how
+// many of that score are known. One barrier a pass: every wavefront sums the
+// counts for itself, and clears the other pass's while this one's are made.
+//
+// Bound by its waits: 9 us for 8 rows of 1472 blocks, 10 us for 512 of up to 1500, 12 us
+// for 128 of up to 4063. In one kernel with the scores, which then come at the rate
+// of a compute unit: 22 us, 45, 46 where the two take 15, 45, 36.
 
 __device__ __forceinline__ uint32_t rank_of(float x) {       // NaN above all
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
@@ -351,32 +355,49 @@ __global__ __launch_bounds__(THREADS) void k_block_select(Select a) {
   const bool fits = share <= kHeld * kWave;
   auto read = [&](int32_t b) { return b < to && b >= lo && b < hi ? rank_of(scores[b]) : 0u; };
   uint32_t x[kHeld];
+  int32_t entry[kHeld];
   if (fits) {
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) x[i] = read(from + i * kWave + lane);
+    for (int i = 0; i < kHeld; ++i) {
+      const int32_t b = from + i * kWave + lane;
+      x[i] = read(b);
+      entry[i] = b < to ? ids[b] : 0;
+    }
   }
-  auto each = [&](auto f) {          // f(block, rank) of this lane's blocks, up to the end of the share and beyond
+  auto each = [&](auto f) {          // f(block, rank, held entry) of this lane's blocks, up to the end of the share and beyond
     if (fits) {
 #pragma unroll
       for (int i = 0; i < kHeld; ++i)
-        if (from + i * kWave < to) f(from + i * kWave + lane, x[i]);
+        if (from + i * kWave < to) f(from + i * kWave + lane, x[i], entry[i]);
     } else {
-      for (int32_t b = from; b < to; b += kWave) f(b + lane, read(b + lane));
+      for (int32_t b = from; b < to; b += kWave) f(b + lane, read(b + lane), 0);
     }
   };
   uint32_t prefix = 0, left = (uint32_t)(a.keep - a.sink - a.recent);      // so many of the candidates stay
   const bool any = left > 0;
   if (any) {
+    // the bits in which candidates differ: scores of one call begin alike
+    const uint32_t alike = rank_of(scores[lo]);
+    uint32_t differ = 0;
+    each([&](int32_t b, uint32_t rank, int32_t) { differ |= b < to && b >= lo && b < hi ? rank ^ alike : 0u; });
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) differ |= __shfl_xor(differ, d);
+    if (lane == 0) s_more[wave] = differ;
 #pragma unroll
     for (int e = 0; e < 4; ++e) s_count[0][wave][4 * lane + e] = 0;
-    __builtin_amdgcn_wave_barrier();
-    for (int pass = 0; pass < 4; ++pass) {
-      const int shift = 24 - 8 * pass;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) differ |= s_more[w];
+    differ = __builtin_amdgcn_readfirstlane(differ);
+    int open = differ != 0 ? 32 - __builtin_clz(differ) : 0;      // low bits of the least rank to stay that are not known
+    prefix = open == 32 ? 0u : alike >> open << open;
+    for (int pass = 0; open > 0; ++pass) {
+      const int shift = max(0, open - 8);
+      const uint32_t digits = (1u << (open - shift)) - 1;
       uint32_t(*count)[256] = s_count[pass & 1];
       // (lanes of one digit counted as one, by ballots, took 1.5 to 2.5 us more than these)
-      each([&](int32_t b, uint32_t rank) {
-        if (b < to && b >= lo && b < hi && (pass == 0 || (rank ^ prefix) >> (shift + 8) == 0))
-          atomicAdd(&count[wave][(rank >> shift) & 255], 1u);
+      each([&](int32_t b, uint32_t rank, int32_t) {
+        if (b < to && b >= lo && b < hi && (pass == 0 || (rank ^ prefix) >> open == 0))
+          atomicAdd(&count[wave][(rank >> shift) & digits], 1u);
       });
       __syncthreads();
       // (a wavefront clears its own counts for the next pass: they were last read before this barrier)
@@ -404,7 +425,9 @@ __global__ __launch_bounds__(THREADS) void k_block_select(Select a) {
       const int from_lane = __builtin_ctzll(__ballot(here) | 1ull << 63);
       prefix |= (uint32_t)__builtin_amdgcn_readlane(digit, from_lane) << shift;
       left = __builtin_amdgcn_readlane(rest, from_lane);
+      open = shift;
     }
+    __syncthreads();        // (s_more is written again)
   }
   // counted, then placed
   auto look = [&](int32_t b, uint32_t rank, bool* more, bool* equal) {
@@ -413,7 +436,7 @@ __global__ __launch_bounds__(THREADS) void k_block_select(Select a) {
     *equal = in && !must && any && rank == prefix;
   };
   uint32_t more = 0, equal = 0;
-  each([&](int32_t b, uint32_t rank) {
+  each([&](int32_t b, uint32_t rank, int32_t) {
     bool m, e;
     look(b, rank, &m, &e);
     more += __popcll(__ballot(m));
@@ -431,13 +454,13 @@ __global__ __launch_bounds__(THREADS) void k_block_select(Select a) {
   }
   place += min(ties, left);
   const uint64_t below = (1ull << lane) - 1;
-  each([&](int32_t b, uint32_t rank) {
+  each([&](int32_t b, uint32_t rank, int32_t held_entry) {
     bool m, e;
     look(b, rank, &m, &e);
     const uint64_t equals = __ballot(e);
     const bool stays = m || (e && ties + (uint32_t)__popcll(equals & below) < left);
     const uint64_t all = __ballot(stays);
-    if (stays) out[place + __popcll(all & below)] = ids[b];
+    if (stays) out[place + __popcll(all & below)] = fits ? held_entry : ids[b];
     place += __popcll(all);
     ties += __popcll(equals);
   });
@@ -556,6 +579,7 @@ peek_status peek_block_select(const peek_kv_pool* pool, const int8_t* d_bounds, 
         hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3((unsigned)threads), 0, st, a);
       };
       if (max_blocks <= kHeld * 256) go(k_block_select<256>, 256);
+      else if (max_blocks <= kHeld * 512) go(k_block_select<512>, 512);
       else go(k_block_select<1024>, 1024);
       e = hipGetLastError();
     }
