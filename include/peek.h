@@ -560,7 +560,7 @@ peek_status peek_kv_evict(int32_t n, int32_t kv_heads, int32_t block_size, const
  * Errors: INVALID_ARGUMENT, DEVICE.
  * ---------------------------------------------------------------------- */
 typedef struct peek_rotary {
-  const double* d_freq;  /* [rot_dim / 2], radians a token */
+  const double* d_freq;  /* [rot_dim / 2], radians a token; 8-byte aligned */
   int32_t rot_dim;       /* multiple of 16, 0 (no rotation) to head_dim */
   int32_t interleaved;   /* 0: pairs (i, i + rot_dim / 2); else (2i, 2i + 1) */
   float magnitude;       /* times the rotated numbers; finite */
@@ -629,8 +629,9 @@ peek_status peek_kv_read(const peek_kv_pool* pool, int32_t n, int64_t num_tokens
  * are read from the pages that the table names for the group's first member. A
  * member with fewer tokens than that shares nothing and reads its own pages.
  * Sequences past the last group's end share nothing either. Rows of sequences
- * that d_members does not name are left as they are, and so are the outputs of
- * an id outside 0 .. n - 1. Everything else is as in peek_decode_attention.
+ * that d_members does not name are left as they are; an id outside 0 .. n - 1 is
+ * passed over, or, as a group's first, stands for sequence 0 (PEEK_VALIDATE reports it, and
+ * offsets that are none). Everything else is as in peek_decode_attention; groups < 2^24.
  * Scratch comes only from d_workspace (device, 256-byte aligned, at least
  * peek_shared_decode_attention_workspace bytes). Asynchronous on `stream`.
  * n = 0 is a no-op.
@@ -658,7 +659,8 @@ peek_status peek_shared_decode_attention(const peek_kv_pool* pool, int32_t n, in
  * d_context[r], element by element: of int8 codes themselves, of float8 values v
  * the next whole number above, and below, v / 4 (a NaN is the largest of its sign); within
  * -127 .. 127; where the keys' scale is negative, those of the negated codes. After
- * an append, first = the context before it brings the bounds up to date.
+ * an append, first = the context before it brings the bounds up to date. A block
+ * that several sequences name holds equally many tokens of each.
  * Asynchronous on `stream`; no workspace. n = 0 is a no-op.
  * Errors: INVALID_ARGUMENT, DEVICE.
  *

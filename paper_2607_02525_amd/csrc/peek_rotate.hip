@@ -511,6 +511,8 @@ peek_status peek_rotate_append(const peek_kv_pool* pool, int32_t n, int64_t num_
       return fail(PEEK_ERR_INVALID_ARGUMENT, "rot_dim must be a multiple of 16 in [0, head_dim] (got %d)",
                   rotary->rot_dim);
     if (rotary->rot_dim > 0 && !rotary->d_freq) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_freq must not be NULL");
+    if ((reinterpret_cast<uintptr_t>(rotary->d_freq) & 7) != 0)
+      return fail(PEEK_ERR_INVALID_ARGUMENT, "d_freq must be 8-byte aligned");
     if (!std::isfinite(rotary->magnitude)) return fail(PEEK_ERR_INVALID_ARGUMENT, "magnitude must be finite");
     if (!(rotary->eps >= 0) || !std::isfinite(rotary->eps))
       return fail(PEEK_ERR_INVALID_ARGUMENT, "eps must be 0 or more and finite");

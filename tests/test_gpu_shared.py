@@ -206,6 +206,22 @@ def test_equal_inputs_give_equal_bits_and_graphs_replay():
         ctx.sub_((ctx > 330).to(torch.int32))
 
 
+def test_validation_on_request(monkeypatch):
+    import paper_2607_02525_amd as P
+    args, kw = run_shared(32, [(96, [5, 6, 1])], 2, 4, 16, 64, HF, I8, mixed=False)
+    args[3][1:, :6] = args[3][:1, :6]            # every sequence's table names what it shares
+    monkeypatch.setenv("PEEK_VALIDATE", "1")
+    P.peek_shared_decode_attention(*args, **kw)
+    i32 = torch.int32
+    for offsets, members in (([0, 4], [0, 1, 2]), ([2, 1], [0, 1, 2]), ([-1, 3], [0, 1, 2]), ([0, 3], [0, 3, 2]),
+                             ([0, 3], [0, -1, 2])):
+        bad = list(args)
+        bad[4] = torch.tensor(offsets, dtype=i32).cuda()
+        with pytest.raises(P.PeekError) as e:
+            P.peek_shared_decode_attention(*bad, **{**kw, "members": torch.tensor(members, dtype=i32).cuda()})
+        assert e.value.status == P.PEEK_ERR_INVALID_ARGUMENT
+
+
 def test_shared_on_another_stream():
     side = torch.cuda.Stream()
     run_shared(31, [(96, [5, 6, 1])], 2, 4, 16, 64, HF, I8, stream=side)

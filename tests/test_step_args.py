@@ -71,14 +71,14 @@ REFUSED = [
               dict(d=96), dict(d=64), dict(rot=0), dict(rot=rotary(rot_dim=8)), dict(rot=rotary(rot_dim=-16)),
               dict(rot=rotary(rot_dim=144)), dict(rot=rotary(d_freq=None)), dict(rot=rotary(magnitude=math.inf)),
               dict(rot=rotary(magnitude=math.nan)), dict(rot=rotary(eps=-1.0)), dict(rot=rotary(eps=math.nan)),
-              dict(rot=rotary(d_q_norm=0x10008)), dict(rot=rotary(d_k_norm=0x10002)), dict(q=None), dict(qo=None),
+              dict(rot=rotary(d_freq=0x10004)), dict(rot=rotary(d_q_norm=0x10008)), dict(rot=rotary(d_k_norm=0x10002)), dict(q=None), dict(qo=None),
               dict(qos=(256, 128)), dict(qos=(512, 64)), dict(kos=(128, 128)), dict(ko=ODD), dict(v=None), dict(v=ODD),
               dict(off=None), dict(ctx=None), dict(table=None), dict(stride=3), dict(blocks=-1),
               dict(tokens=1 << 40), *ROWS]),
     (read, [dict(n=-1), dict(tokens=-1), dict(type=3), dict(off=None), dict(first=None), dict(table=None),
             dict(stride=3), dict(v=None), dict(v=ODD), dict(ks=(128, 128)), dict(vs=(256, 64)), dict(tokens=1 << 40),
             *ROWS]),
-    (shared, [dict(n=-1), dict(groups=-1), dict(type=2), dict(hq=3), dict(hq=0), dict(scale=math.nan), dict(q=None),
+    (shared, [dict(n=-1), dict(groups=-1), dict(groups=1 << 24), dict(type=2), dict(hq=3), dict(hq=0), dict(scale=math.nan), dict(q=None),
               dict(qs=(4, 128)), dict(ctx=None), dict(table=None), dict(stride=3), dict(offsets=None),
               dict(tokens=None), dict(out=None), dict(os=(256, 128)), dict(ws=None), dict(ws=ODD), dict(n=1 << 24),
               dict(blocks=1 << 28, stride=1 << 28)]),
@@ -93,7 +93,7 @@ REFUSED = [
 
 
 @pytest.mark.parametrize("call,kw", [(c, kw) for c, all_ in REFUSED for kw in all_],
-                         ids=lambda x: getattr(x, "__name__", None) or str(x)[:60])
+                         ids=[f"{c.__name__} {i} {'+'.join(kw)}" for c, all_ in REFUSED for i, kw in enumerate(all_)])
 def test_refusals(call, kw):
     assert call(pool(), **kw) == BAD
     assert P.peek_last_error()
