@@ -491,11 +491,12 @@ class KVPool:
 
 def _rows(t, name: str, dtype, heads: int | None = None, dim: int | None = None, tokens: int | None = None):
     """Pointer and strides of rows of heads [tokens, heads, dim], whose last dimension is contiguous."""
-    if t.dim() != 3:
+    shape = t.shape
+    if len(shape) != 3:
         raise ValueError(f"{name} must be [tokens, heads, head_dim]")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    n, h, d = t.shape
+    n, h, d = shape
     if (heads is not None and h != heads) or (dim is not None and d != dim) or (tokens is not None and n != tokens):
         raise ValueError(f"{name} must be [{tokens}, {heads}, {dim}], got {list(t.shape)}")
     token, head, one = t.stride()
@@ -632,15 +633,20 @@ class _RotaryStruct(ctypes.Structure):
 
 # The current device's number without the check that torch is initialised, where this torch has that.
 _raw_device = getattr(torch._C, "_cuda_getDevice", None)
+_devices = None     # how many there are, once asked
 
 
 def _place(stream, *tensors):
     """The stream's handle, after refusing tensors of a device other than the current one, where the kernels run."""
+    global _devices
     fast = _raw_device is not None and _raw_stream is not None and torch.cuda.is_initialized()
     now = _raw_device() if fast else torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != now:
-            raise ValueError(f"tensors must be on the current device (cuda:{now}), got one on {t.device}")
+    if _devices is None:
+        _devices = torch.cuda.device_count()
+    if _devices > 1:            # (of a single device, as every tensor's own check has found, they all are)
+        for t in tensors:
+            if t is not None and t.get_device() != now:
+                raise ValueError(f"tensors must be on the current device (cuda:{now}), got one on {t.device}")
     if stream is None:
         return _raw_stream(now) if fast else torch.cuda.current_stream().cuda_stream
     return stream if isinstance(stream, int) else stream.cuda_stream
@@ -648,7 +654,9 @@ def _place(stream, *tensors):
 
 def _exact_arg(t, name: str, dtype, *shape: int):
     """As _arg, of this shape and no other."""
-    if t is not None and tuple(t.shape) != shape:
+    if t is None:
+        return None
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     return _arg(t, name, dtype)
 
@@ -683,19 +691,22 @@ def peek_rotate_append(q, k, v, offsets, context, freq, q_out, k_out=None, pool:
     if pool is None and k_out is None:
         raise ValueError("k needs a pool or k_out")
     q_heads = 0 if q is None else q.shape[1] if q.dim() == 3 else -1
-    none = (None, 0, 0)
-    rows_q = none if q is None else _rows(q, "q", dtype, None, dim, tokens)
-    rows_q_out = none if q is None else _rows(q_out, "q_out", dtype, q_heads, dim, tokens)
+    rows_q = rows_q_out = rows_v = rows_k_out = table = (None, 0, 0)
     rows_k = _rows(k, "k", dtype)
-    rows_v = none if v is None else _rows(v, "v", dtype, kv_heads, dim, tokens)
-    rows_k_out = none if k_out is None else _rows(k_out, "k_out", dtype, kv_heads, dim, tokens)
-    for out, rows_out, of, rows in ((q_out, rows_q_out, q, rows_q), (k_out, rows_k_out, k, rows_k)):
-        if out is not None and rows_out[0] == rows[0] and out.stride() != of.stride():
-            raise ValueError("an output in place of its input must have its strides")
+    if q is not None:
+        rows_q = _rows(q, "q", dtype, None, dim, tokens)
+        rows_q_out = _rows(q_out, "q_out", dtype, q_heads, dim, tokens)
+    if v is not None:
+        rows_v = _rows(v, "v", dtype, kv_heads, dim, tokens)
+        table = _table(block_table, n)
+    if k_out is not None:
+        rows_k_out = _rows(k_out, "k_out", dtype, kv_heads, dim, tokens)
+    if (q is not None and rows_q_out[0] == rows_q[0] and rows_q_out != rows_q) or \
+            (k_out is not None and rows_k_out[0] == rows_k[0] and rows_k_out != rows_k):
+        raise ValueError("an output in place of its input must have its strides")
     rot = 0 if freq is None else 2 * freq.numel()
     rotary = _RotaryStruct(_arg(freq, "freq", torch.float64), rot, int(bool(interleaved)), magnitude, eps,
                            _exact_arg(q_norm, "q_norm", dtype, dim), _exact_arg(k_norm, "k_norm", dtype, dim))
-    table = none if block_table is None else _table(block_table, n)
     at, ctx = _arg(offsets, "offsets"), _arg(context, "context", torch.int32, n)
     on = _place(stream, q, k, v, offsets, context, freq, q_out, k_out, block_table, q_norm, k_norm,
                 None if pool is None else pool._pages)
