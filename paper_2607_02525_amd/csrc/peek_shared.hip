@@ -18,7 +18,8 @@
 //
 // Groups of few rows take tiles of 16 or 32 rows instead, and their keys to the
 // products without LDS between wavefronts: they are bound by reading them. So
-// is a sequence's own span, for which they serve too.
+// is a sequence's own span, for which they serve too, in the same launch: what
+// waits for memory runs beside what waits for the matrix cores.
 #include <algorithm>
 
 #include "peek_internal.h"
@@ -42,7 +43,7 @@ constexpr int kThreads = kWave * kWaves;
 constexpr int kTile = 32;             // own keys of a wavefront's step
 constexpr int kMaxChunk = 4096;       // own keys of a workgroup, at most
 constexpr int64_t kLeastSteps = 2;    // tiles of shared keys of a workgroup
-constexpr int kFewKeys = kWaves * kTile;      // keys of a step of k_shared_few
+constexpr int kFewKeys = kWaves * kTile;      // keys of a step of stream_keys
 
 struct Shared {
   Pool pool;
@@ -143,8 +144,7 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // ------------------------------------------------------------- shared keys
-// A step is a tile of rows (32 to each of WAVES wavefronts) against a tile of
-// keys.
+// A step is a tile of rows (32 to a wavefront) against a tile of keys.
 
 // The sum of the lanes up to this one.
 __device__ __forceinline__ int64_t sum_to(int64_t x) {
@@ -245,22 +245,27 @@ struct Line {
   }
 };
 
-template <int TYPE, int FMT, int D, int WAVES>
-__global__ __launch_bounds__(kWave * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_shared_prefix(Shared a) {
-  using T = Tile<TYPE, FMT, D, WAVES>;
-  constexpr int kRows = 32 * WAVES, kThreads = kWave * WAVES;
+// LDS of a workgroup of either kind: two buffers of K and V tiles and their scales, or the wavefronts' rings and their
+// references and sums.
+template <int D>
+constexpr int kMemory = 4 * kKeys * D * 2 + 512;
+
+template <int TYPE, int FMT, int D>
+__device__ __forceinline__ void shared_tiles(const Shared& a, uint32_t block, uint8_t* memory) {
+  using T = Tile<TYPE, FMT, D, kWaves>;
+  constexpr int kRows = 32 * kWaves;
   constexpr int kEach = T::kUnitsEach;                        // 16-code units of a tile and thread
-  constexpr int kMine = kEach > 1 ? kEach / 2 : 1;            // keys that they are of
+  constexpr int kMine = kEach / 2;                            // keys that they are of, K and V of each
   constexpr int kStride = kThreads / (D / 16);                // from one of these to the next
-  __shared__ __attribute__((aligned(1024))) uint8_t s_k[2][T::kBytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t s_v[2][T::kBytes];
-  __shared__ f4 s_scale[2][kKeys / 4];
+  uint8_t(*const s_k)[T::kBytes] = (uint8_t(*)[T::kBytes])memory;
+  uint8_t(*const s_v)[T::kBytes] = s_k + 2;
+  f4(*const s_scale)[kKeys / 4] = (f4(*)[kKeys / 4])(s_v + 2);
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   // kv heads side by side: each on XCDs of its own where there are eight
-  const int32_t head = blockIdx.x % a.pool.heads, piece = blockIdx.x / a.pool.heads, lb = a.pool.log_block;
+  const int32_t head = block % a.pool.heads, piece = block / a.pool.heads, lb = a.pool.log_block;
   Line<kRows, kKeys> line;
-  line.count(a, kLeastSteps, lane, blockIdx.x == 0 && wave == 0);
+  line.count(a, kLeastSteps, lane, block == 0 && wave == 0);
   const int64_t end = min(line.all, (piece + 1) * line.each);
 
   const int col = lane & 31, half = lane >> 5;
@@ -268,8 +273,7 @@ __global__ __launch_bounds__(kWave * WAVES) __attribute__((amdgpu_waves_per_eu(2
   const uint32_t half_bytes = ((uint32_t)a.pool.heads << lb) * D;         // a page's keys, or values
   const uint8_t* head_pages = a.pool.pages + ((int64_t)head << lb) * D;
   const int32_t unit_key = tid / (D / 16) % kKeys, unit_at = tid % (D / 16);
-  const bool upper = kEach == 1 && tid >= kThreads / 2;       // has values only
-  const bool leads = unit_at == 0 && (unit_key & 3) == 0 && !upper;       // fetches four keys' scales
+  const bool leads = unit_at == 0 && (unit_key & 3) == 0;       // fetches four keys' scales
 
   for (int64_t at = piece * line.each; at < end;) {
     const Run run = line.find(a, piece, at, end, lane);
@@ -314,12 +318,8 @@ __global__ __launch_bounds__(kWave * WAVES) __attribute__((amdgpu_waves_per_eu(2
         const uint32_t id = (uint32_t)page[k] < a.pool.num_pages ? (uint32_t)page[k] : 0u;
         const uint32_t in_block = key_of(j, k) & ((1 << lb) - 1);
         const uint8_t* p = head_pages + (uint64_t)id * (2 * half_bytes) + in_block * D + unit_at * 16;
-        if constexpr (kEach > 1) {
-          codes[k] = *(const u4*)p;
-          codes[kMine + k] = *(const u4*)(p + half_bytes);
-        } else {
-          codes[0] = *(const u4*)(p + (upper ? half_bytes : 0u));
-        }
+        codes[k] = *(const u4*)p;
+        codes[kMine + k] = *(const u4*)(p + half_bytes);
         if (leads) {
           const float* x = a.pool.scales + head + (uint64_t)id * (uint32_t)(2 * a.pool.heads);
           scale_k[k] = x[0];
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(kWave * WAVES) __attribute__((amdgpu_waves_per_eu(2
     auto store = [&](int buf) {
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const bool is_v = kEach > 1 ? i >= kMine : upper;
+        const bool is_v = i >= kMine;
         const int32_t key = unit_key + i % kMine * kStride;
         const u2 x0 = widen4<TYPE, FMT>(codes[i][0]), x1 = widen4<TYPE, FMT>(codes[i][1]);
         const u2 x2 = widen4<TYPE, FMT>(codes[i][2]), x3 = widen4<TYPE, FMT>(codes[i][3]);
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(kWave * WAVES) __attribute__((amdgpu_waves_per_eu(2
 // keys of the documents, tiles of 64 rows 83: more vector instructions to a
 // wavefront, whose keys still come at the rate of memory.
 template <int TYPE, int FMT, int D, int ROWS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_shared_few(Shared a, uint32_t shared_groups) {
+__device__ __forceinline__ void stream_keys(const Shared& a, uint32_t block, uint32_t shared_groups, uint8_t* memory) {
   constexpr int kSteps = D / 32, kParts = D / 16;
   constexpr int kRows = 16 * ROWS;
   constexpr int kLoads = D / 16;                  // of a tile: 1 KB each, keys and then values
@@ -413,12 +413,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   constexpr int kTurn = kWaves * kTile;
   constexpr int kJoin = kWaves * 16 * (D + 4) * (int)sizeof(float);
   constexpr int kRing = kWaves * 2 * kSlot;
-  __shared__ __attribute__((aligned(1024))) uint8_t s_ring[kRing > kJoin ? kRing : kJoin];
-  __shared__ float s_top[kWaves][16], s_sum[kWaves][16];
+  static_assert(kRing + 512 <= kMemory<D> && kJoin + 512 <= kMemory<D>, "the rings and what is joined fit");
+  uint8_t* const s_ring = memory;
+  float(*const s_top)[16] = (float(*)[16])(memory + kMemory<D> - 512);
+  float(*const s_sum)[16] = s_top + kWaves;
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const bool own = blockIdx.x >= shared_groups;
-  const uint32_t unit = own ? blockIdx.x - shared_groups : blockIdx.x;
+  const bool own = block >= shared_groups;
+  const uint32_t unit = own ? block - shared_groups : block;
   const int32_t head = unit % a.pool.heads, lb = a.pool.log_block, q_heads = a.group * a.pool.heads;
   const int32_t piece = unit / a.pool.heads;
   Line<kRows, kFewKeys> line;
@@ -444,7 +446,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     from = begin + split * a.own_chunk;
     whole = begin == 0 && held <= a.own_chunk;      // the only part: this is the answer
   } else {
-    line.count(a, 1, lane, blockIdx.x == 0 && wave == 0);
+    line.count(a, 1, lane, block == 0 && wave == 0);
     at = piece * line.each;
     end = min(line.all, at + line.each);
   }
@@ -695,6 +697,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 }
 
 // ---------------------------------------------------------------- own keys
+template <int TYPE, int FMT, int D>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_shared_tiles(Shared a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t s_memory[kMemory<D>];
+  shared_tiles<TYPE, FMT, D>(a, blockIdx.x, s_memory);
+}
+template <int TYPE, int FMT, int D, int ROWS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_shared_stream(Shared a, uint32_t shared_groups) {
+  __shared__ __attribute__((aligned(1024))) uint8_t s_memory[kMemory<D>];
+  stream_keys<TYPE, FMT, D, ROWS>(a, blockIdx.x, shared_groups, s_memory);
+}
+// Workgroups below `shared_groups` take tiles of 128 rows over shared keys, the others own keys, beside them.
+template <int TYPE, int FMT, int D, int ROWS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_shared_both(Shared a, uint32_t shared_groups) {
+  __shared__ __attribute__((aligned(1024))) uint8_t s_memory[kMemory<D>];
+  if (blockIdx.x < shared_groups) shared_tiles<TYPE, FMT, D>(a, blockIdx.x, s_memory);
+  else stream_keys<TYPE, FMT, D, ROWS>(a, blockIdx.x - shared_groups, 0, s_memory);
+}
+
 // In blocks of 4 or 8 tokens: 16 rows of one sequence over a chunk of its own keys, as
 // in the decode of single sequences. Blocks are looked up in LDS.
 template <int TYPE, int FMT, int D>
@@ -1028,9 +1048,8 @@ peek_status validate_groups(int32_t n, int32_t groups, const int32_t* members, c
 
 // -------------------------------------------------------------------- plan
 struct Plan {
-  bool few;                           // shared keys by k_shared_few
+  bool few;                           // shared keys by stream_keys
   int32_t own_rows;                   // of a tile of own keys
-  int32_t waves;                      // of a workgroup of k_shared_prefix
   int32_t tile_rows;
   int32_t pieces, slots, slot_rows;
   int32_t own_chunk, own_splits;
@@ -1042,6 +1061,10 @@ constexpr int64_t kOwnGroups = 2048;
 // tokens 43 us either way, 32 to each 32 instead of 39 by tiles of 128, 128 to each 62 instead of 56.
 constexpr int64_t kFewRows = 64;
 constexpr int32_t kMostGroups = 1 << 24;
+// Workgroups over shared keys beside those over own ones, of the 512 that the device holds at once: 192 agents with 500 to
+// 8000 own tokens 452, 460, 461, 478 us with 256, 320, 384, 512 of them (492 one after the other, tiles of 256 rows first);
+// 256 sequences in 4 groups with 16 own tokens 95, 99, 90, 87 (103).
+constexpr int64_t kBothGroups = 384;
 constexpr int32_t kManyParts = 32;
 constexpr int64_t kFewJoins = 512;
 
@@ -1052,11 +1075,10 @@ Plan plan_for(const peek_kv_pool& pool, int32_t n, int32_t q_heads, int32_t max_
   const int64_t all_rows = (int64_t)n * group;                              // of a kv head
   const int64_t rows_each = groups > 0 ? all_rows / groups : 0;
   p.few = groups > 0 && pool.block_size >= 16 && rows_each <= kFewRows;
-  p.waves = rows_each > 128 ? 8 : 4;
   p.own_rows = pool.block_size >= 16 && ((p.few && rows_each > 8) || group > 16) ? 32 : 16;
-  p.tile_rows = p.few ? p.own_rows : 32 * p.waves;
+  p.tile_rows = p.few ? p.own_rows : 32 * kWaves;
   const int64_t tiles = all_rows / p.tile_rows + groups;                    // no more than these
-  p.pieces = (int32_t)std::max<int64_t>(1, (p.few || p.waves == 4 ? 512 : 256) / pool.kv_heads);
+  p.pieces = (int32_t)std::max<int64_t>(1, (!p.few && pool.block_size >= 16 ? kBothGroups : 512) / pool.kv_heads);
   p.slots = (int32_t)(p.pieces + tiles);
   p.slot_rows = (int32_t)std::min<int64_t>(p.tile_rows, all_rows);
   int64_t chunk = 256;
@@ -1167,20 +1189,18 @@ peek_status peek_shared_decode_attention(const peek_kv_pool* pool, int32_t n, in
     a.step_keys = p.few ? kFewKeys : kKeys;
     set_scale(scale, &a.scale, &a.q_flip, &a.q_mask);
     with_types(type, pool->type, pool->head_dim, [&](auto t, auto m, auto d) {
-      if (prefix_groups > 0 && !p.few) {
-        auto go = [&](auto kernel) {
-          hipLaunchKernelGGL(kernel, dim3((unsigned)prefix_groups), dim3(kWave * p.waves), 0, st, a);
-        };
-        if (p.waves == 8) go(k_shared_prefix<t(), m(), d(), 8>);
-        else go(k_shared_prefix<t(), m(), d(), 4>);
-      }
-      const uint32_t first = p.few ? (uint32_t)prefix_groups : 0u;
+      const bool both = prefix_groups > 0 && !p.few && a.pool.log_block >= 4;
+      if (prefix_groups > 0 && !p.few && !both)
+        hipLaunchKernelGGL((k_shared_tiles<t(), m(), d()>), dim3((unsigned)prefix_groups), dim3(kThreads), 0, st, a);
+      const uint32_t first = p.few || both ? (uint32_t)prefix_groups : 0u;
       auto go = [&](auto kernel, auto... more) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)own_groups + first), dim3(kThreads), 0, st, a, more...);
       };
       if (a.pool.log_block < 4) go(k_shared_own<t(), m(), d()>);
-      else if (own_rows == 32) go(k_shared_few<t(), m(), d(), 2>, first);
-      else go(k_shared_few<t(), m(), d(), 1>, first);
+      else if (both && own_rows == 32) go(k_shared_both<t(), m(), d(), 2>, first);
+      else if (both) go(k_shared_both<t(), m(), d(), 1>, first);
+      else if (own_rows == 32) go(k_shared_stream<t(), m(), d(), 2>, first);
+      else go(k_shared_stream<t(), m(), d(), 1>, first);
     });
     hipError_t err = hipGetLastError();
     if (err == hipSuccess) {

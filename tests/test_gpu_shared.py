@@ -106,7 +106,7 @@ SHARED = [
     ([(15, [20, 3])], 2, 2, 16, 128, BF, I8),                            # less than a block: nothing
     ([(128, [4] * 33)], 1, 1, 128, 128, HF, I8),
     ([(64, [0, 0, 0])], 2, 4, 16, 64, BF, F8),                           # nothing of their own
-    ([(1600, [3] * 45), (528, [2] * 30)], 1, 4, 16, 128, BF, F8),        # 120 to 180 rows: two tiles of 128 or one of 256
+    ([(1600, [3] * 45), (528, [2] * 30)], 1, 4, 16, 128, BF, F8),        # 120 to 180 rows: one or two tiles of 128
     ([(528, [3] * 45), (1040, [2] * 80)], 2, 4, 16, 64, HF, I8),
     ([(520, [1] * 20), (84, [5, 2])], 1, 16, 4, 128, HF, F8),
     ([(32 + 16 * (g % 3), [1 + g % 5] * (g % 4)) for g in range(150)], 1, 2, 16, 64, BF, I8),      # 150 groups
