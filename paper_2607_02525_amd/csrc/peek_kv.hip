@@ -27,9 +27,11 @@ constexpr int kWave = 64;
 // Bound by memory: 16-byte loads of eight elements, which stay in registers
 // from the maximum to the rounding up to HELD of them a lane, as many as a block has,
 // 16 at most; larger blocks are read again, from L2. Measured, 72000 tokens of 8 heads
-// of 128, 439 MB: 91 to 98 us, 4.5 to 4.8 TB/s, in blocks of 16 tokens (a large copy
-// reaches 4.95); of 32 87 us (104 with four a lane), of 64 99 (116), of 256 137 (158);
-// blocks of 16 with eight a lane 107. 64 single tokens 5.3 us: the waits for
+// of 128, 439 MB: 87 us, 5.0 TB/s, in blocks of 16 tokens (a large copy
+// reaches 4.95); of 32 88 us, of 64 94, of 128 119, of 256 135 (with four pieces a lane
+// blocks of 32, 64 and 256 take a sixth more, with eight blocks of 16). The maximum is taken of
+// 16-bit magnitudes, two at a time, and only blocks with an infinity or NaN look at their elements one by
+// one (94 us with a float maximum of finite elements). 64 single tokens 5.3 us: the waits for
 // offsets, page id, old scale and codes, one after the other.
 
 template <int TYPE, int FMT, int D, int HELD>

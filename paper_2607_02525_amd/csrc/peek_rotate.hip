@@ -15,6 +15,14 @@
 // both halves of eight pairs: no lane needs another's elements to turn its own,
 // and what it overwrites in place is what it has read. Angles are computed once
 // for the heads of a workgroup and shared through LDS.
+//
+// Bound by memory: 72000 tokens of 32 query and 8 kv heads of 128, half of each head
+// turned in pairs, into int8 blocks of 16 and k_out, 1.77 GB: 355 us, 5.0 TB/s (a large copy
+// 4.95); 84000 of 64 and 8 heads, normed, 3.07 GB: 680 us, 4.5 TB/s. Rows alone run at 5.1 to 5.5 TB/s;
+// blocks alone at 2.9 to 3.3, by their vector instructions (19 an element of a
+// plain append before its maximum and quotients were shortened, now 7), beside rows they
+// cost what their bytes do. Blocks of 64 tokens 399 us, of 256 444. 64 single tokens 6.5 us.
+// Fewer registers for more wavefronts spill: limits of 4 and 5 to a SIMD 425 and 660 us instead of 389.
 #include <cmath>
 
 #include "peek_internal.h"
@@ -36,7 +44,8 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWave * kWaves;
 constexpr int kTokens = 16;        // whose angles a workgroup holds at a time
 constexpr int kRowTokens = 4;      // of a workgroup over rows, where there are many
-constexpr int64_t kManyBlocks = 1024;
+constexpr int64_t kManyBlocks = 1024;   // all heads of a block to a workgroup: 4500 blocks 421 us instead of 453; few
+                                        // blocks have more workgroups with four heads each
 
 struct OutRows {
   uint16_t* data;
@@ -161,7 +170,8 @@ __device__ __forceinline__ void rotate_item(const Rotate& a, const uint16_t* nor
 }
 
 // ------------------------------------------------------------------- rows
-// Rows of q, and of k where there is no cache: TOKENS tokens' heads a workgroup.
+// Rows of q, and of k where there is no cache: TOKENS tokens' heads a workgroup, four where there are
+// thousands of them (one search for their sequence each, and four times the angles to a barrier), else one.
 // A thread has four items on their way at a time, the first of them before the
 // positions are known (of rows that are in no sequence they are not stored).
 constexpr int kBatch = 4;
@@ -398,7 +408,8 @@ __global__ __launch_bounds__(kThreads) void k_rotate_append(Rotate a) {
 
 // -------------------------------------------------------------------- read
 // A wavefront takes the tokens of one (block, K or V, head), found as an append
-// finds them.
+// finds them. Bound by memory: 64 sequences of 3200 to 7168 tokens, 2 GB: 394 us, 5.0 TB/s;
+// one of 5117: 9 us, its waits and 31 MB.
 template <int TYPE, int FMT, int D>
 __global__ __launch_bounds__(kThreads) void k_kv_read(Pool pool, OutRows k, OutRows v, int32_t n, int64_t num_tokens,
                                                       const int64_t* __restrict__ offsets,

@@ -30,7 +30,11 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWave * kWaves;
 
 // ------------------------------------------------------------------ bounds
-// A wavefront takes every splits-th block of a sequence for one head.
+// A wavefront takes every splits-th block of a sequence for one head. Maxima and
+// minima are taken of 16-bit halves, two at a time, and joined over the lanes so that
+// every step leaves half of the words (145 us with all words joined over all lanes).
+// Bound by memory: 64 sequences of 3200 to 7168 tokens, 369 MB: 86 us, 4.3 TB/s; the
+// newest block of 64 sequences 5 us, of one 2.7.
 
 constexpr int64_t kBoundsWaves = 8192;      // wavefronts of a call, where the sequences are fewer
 
@@ -169,7 +173,9 @@ __global__ __launch_bounds__(kThreads) void k_kv_bounds(Bounds a) {
 
 // ------------------------------------------------------------------ scores
 // A wavefront takes 64 blocks at a time of one (sequence, kv head): queries times
-// bounds, 16 queries by 16 blocks by 64 elements a matrix instruction.
+// bounds, 16 queries by 16 blocks by 64 elements a matrix instruction. Bound by
+// reading the bounds, 2 D bytes a block and head in pages of any order: 64 sequences of up to
+// 1500 blocks 31 to 35 us, 3.4 TB/s; 16 of up to 4063 22 us, 5.9 TB/s; one of 1472 6 us.
 
 struct Select {
   Pool pool;

@@ -1056,6 +1056,9 @@ struct Plan {
   size_t part_lse, prefix_out, prefix_lse, first_step, first_tile, bytes;
 };
 
+// Own keys are cut into chunks, of 256 to kMaxChunk, that leave no more workgroups than this where tables are full: empty
+// ones wait for a sequence's length and group before they end (with 8192 the 128 document chats take 81 us instead of
+// 77, with 1024 the same).
 constexpr int64_t kOwnGroups = 2048;
 // Rows of a group and kv head, on average, up to which the reading is what bounds it: 64 to each of 4 groups over 8192
 // tokens 43 us either way, 32 to each 32 instead of 39 by tiles of 128, 128 to each 62 instead of 56.
@@ -1065,6 +1068,8 @@ constexpr int32_t kMostGroups = 1 << 24;
 // 8000 own tokens 452, 460, 461, 478 us with 256, 320, 384, 512 of them (492 one after the other, tiles of 256 rows first);
 // 256 sequences in 4 groups with 16 own tokens 95, 99, 90, 87 (103).
 constexpr int64_t kBothGroups = 384;
+// A row is joined by a workgroup of 16 wavefronts where it may have this many parts of its own, or where rows are this few
+// (two sequences of 40 heads, 40 parts to a row: 6.3 us, with a wavefront to a row 8.7), else by one wavefront.
 constexpr int32_t kManyParts = 32;
 constexpr int64_t kFewJoins = 512;
 
@@ -1075,6 +1080,8 @@ Plan plan_for(const peek_kv_pool& pool, int32_t n, int32_t q_heads, int32_t max_
   const int64_t all_rows = (int64_t)n * group;                              // of a kv head
   const int64_t rows_each = groups > 0 ? all_rows / groups : 0;
   p.few = groups > 0 && pool.block_size >= 16 && rows_each <= kFewRows;
+  // (tiles of 16 rows where groups have 8 or fewer on average and are as uneven as queues are, or where only own keys
+  // go this way: two users of 4 heads each 17.9 us instead of 20.9 by tiles of 32)
   p.own_rows = pool.block_size >= 16 && ((p.few && rows_each > 8) || group > 16) ? 32 : 16;
   p.tile_rows = p.few ? p.own_rows : 32 * kWaves;
   const int64_t tiles = all_rows / p.tile_rows + groups;                    // no more than these
