@@ -371,7 +371,7 @@ __device__ __forceinline__ void shared_tiles(const Shared& a, uint32_t block, ui
       __syncthreads();
     }
     // (groups that overlap have more tiles than there is room for)
-    if (active && row0 + wave * 32 + col < rows && slot < a.slots) {
+    if (active && row0 + wave * 32 + col < rows && (uint32_t)slot < (uint32_t)a.slots) {
       const float sum = sum_halves(tile.sum), over = 1.0f / sum;
       const int64_t place = ((int64_t)head * a.slots + slot) * a.slot_rows + wave * 32 + col;
       float* out = a.prefix_out + place * D + half * 4;
@@ -474,7 +474,7 @@ __device__ __forceinline__ void stream_keys(const Shared& a, uint32_t block, uin
     } else {
       run = line.find(a, piece, at, end, lane);
       from = run.first * kFewKeys;
-      count = min(run.tokens - from, (run.last - run.first) * kFewKeys);
+      count = (int32_t)min((int64_t)(run.tokens - from), (int64_t)(run.last - run.first) * kFewKeys);
       at += run.last - run.first;
     }
     const int32_t rows = run.rows, row0 = run.row0, slot = run.slot;
@@ -662,7 +662,7 @@ __device__ __forceinline__ void stream_keys(const Shared& a, uint32_t block, uin
       for (int32_t u = tid; u < 16 * (D / 8); u += kThreads) {
         const int32_t c = u / (D / 8), d = u % (D / 8) * 8;
         // (groups that overlap have more tiles than there is room for)
-        if (row0 + 16 * i + c >= rows || slot >= a.slots) continue;
+        if (row0 + 16 * i + c >= rows || (uint32_t)slot >= (uint32_t)a.slots) continue;
         float highest = s_top[0][c];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) highest = fmaxf(highest, s_top[w][c]);
@@ -747,14 +747,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   }
   const int32_t begin = shares(g, held);
   if ((int64_t)split * a.own_chunk >= held - begin) return;
-  const int32_t from = begin + split * a.own_chunk, to = from + min(a.own_chunk, held - from);
+  // tokens from here on are counted from `from`, a block's first: no sum of them comes near 2^31
+  const int32_t from = begin + split * a.own_chunk, to = min(a.own_chunk, held - from);
   const bool whole = begin == 0 && held <= a.own_chunk;      // the only part: this is the answer
 
-  const int32_t block0 = from >> lb;
-  const int32_t* const row_ids = a.table.ids + r * a.table.stride;
-  const int32_t blocks = ((to - 1) >> lb) - block0 + 1;
+  const int32_t* const row_ids = a.table.ids + r * a.table.stride + (from >> lb);
+  const int32_t blocks = ((to - 1) >> lb) + 1;
   for (int32_t i = tid; i < blocks; i += kThreads) {
-    const uint32_t id = (uint32_t)row_ids[block0 + i], page = id < a.pool.num_pages ? id : 0u;
+    const uint32_t id = (uint32_t)row_ids[i], page = id < a.pool.num_pages ? id : 0u;
     const int64_t at = (int64_t)page * 2 * a.pool.heads + head;
     const float k = a.pool.scales[at], v = kv::value_scale(a.pool.scales[at + a.pool.heads]);
     s_block[i] = Block{k * a.scale, log2_fast(v), __builtin_amdgcn_rcpf(v), page};
@@ -781,7 +781,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   const int64_t half_page = ((int64_t)a.pool.heads << lb) * D;      // bytes from a page's keys to its values
 
   auto row_at = [&](int32_t t) {
-    const uint32_t page = s_block[(t >> lb) - block0].page;
+    const uint32_t page = s_block[t >> lb].page;
     return a.pool.pages + ((((int64_t)page * 2 * a.pool.heads + head) << lb) + (t & ((1 << lb) - 1))) * D;
   };
   auto load_keys = [&](int32_t t0) {
@@ -827,7 +827,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
         const u2 lo = widen4<TYPE, FMT>(kw[h][2 * k]), hi = widen4<TYPE, FMT>(kw[h][2 * k + 1]);
         s[h] = mul16<TYPE>((u4){lo[0], lo[1], hi[0], hi[1]}, q[k], s[h]);
       }
-      const Block c = s_block[(min(t0 + 16 * h + 4 * grp, to - 1) >> lb) - block0];
+      const Block c = s_block[min(t0 + 16 * h + 4 * grp, to - 1) >> lb];
       scale[h] = c.scale;
       log_v[h] = c.log_v;
       inv_v[h] = c.inv_v;
@@ -879,7 +879,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   };
 
   {
-    const int32_t mine = to - from - wave * kTile;      // tokens from this wavefront's first one on
+    const int32_t mine = to - wave * kTile;      // tokens from this wavefront's first one on
     if (mine > 0) {
       load_keys(to - mine);
       load_values(to - mine);
@@ -956,7 +956,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : kWave * WAVES) void k_share
     const int64_t piece = over(from, each);
     shared_parts = (int32_t)(over(from + keys - 1, each) - piece) + 1;
     const int64_t slot = piece + a.first_tile[g.index] + tile;
-    if (slot + shared_parts > a.slots) return;
+    if (slot < 0 || slot + shared_parts > a.slots) return;
     place = ((int64_t)head * a.slots + slot) * stride + in_group - tile * rows;
   }
   const int32_t parts = shared_parts + parts_of(held - begin, a.own_chunk);
