@@ -626,8 +626,9 @@ peek_status peek_kv_read(const peek_kv_pool* pool, int32_t n, int64_t num_tokens
  * d_group_offsets[g+1] (int32[groups + 1], from 0, non-decreasing, to n); d_members
  * int32[n] names every sequence once, NULL stands for 0, 1, ... n - 1. The first
  * d_shared[g] tokens of its members, cut to whole blocks, are the same: they
- * are read from the pages that the table names for the group's first member. A
- * member with fewer tokens than that shares nothing and reads its own pages.
+ * are read from the pages that the table names for the group's first member,
+ * however many tokens that one has. A member with fewer tokens than are
+ * shared shares nothing and reads its own pages.
  * Sequences past the last group's end share nothing either. Rows of sequences
  * that d_members does not name are left as they are; an id outside 0 .. n - 1 is
  * passed over, or, as a group's first, stands for sequence 0 (PEEK_VALIDATE reports it, and

@@ -137,3 +137,33 @@ def test_validation_on_request(monkeypatch):
         rotate(at=torch.tensor([-1, 3]).cuda(), pool=None)
     with pytest.raises(P.PeekError):
         P.peek_kv_bounds(pool, None, torch.tensor([33], dtype=I32).cuda(), table, bounds)
+
+
+@pytest.mark.parametrize("held", [0, 40])
+@pytest.mark.parametrize("n,G,B", [(5, 4, 16), (40, 8, 16), (5, 2, 8)])
+def test_a_first_member_without_tokens(held, n, G, B):
+    """A padded row at a group's head: its pages stand for the others' shared keys, its own answer has none of them."""
+    import paper_2607_02525_amd as P
+    from tests.test_gpu_shared import grouped_pool
+    gen = torch.Generator().manual_seed(held + n)
+    codes, scales, table, contexts = grouped_pool(gen, [(128, [9, 5, 0, 70] + [3] * (n - 4))], B, 2, 64, F8)
+    contexts = [held, *contexts[1:]]
+    q = torch.randn(n, 2 * G, 64, generator=gen).to(BF)
+    pool = P.KVPool(codes.cuda(), scales.cuda())
+    out, lse = torch.full_like(q, math.nan).cuda(), torch.full((n, 2 * G), math.nan).cuda()
+    ws = torch.empty(max(256, P.peek_shared_decode_attention_workspace(pool, n, 2 * G, table.shape[1], 1)),
+                     dtype=torch.uint8).cuda()
+    P.peek_shared_decode_attention(pool, q.cuda(), torch.tensor(contexts, dtype=I32).cuda(), table.cuda(),
+                                   torch.tensor([0, n], dtype=I32).cuda(), torch.tensor([128], dtype=I32).cuda(), out,
+                                   ws, lse=lse)
+    for r, c in enumerate(contexts):
+        if c == 0:
+            assert out[r].abs().max() == 0 and (lse[r] == -math.inf).all()
+            continue
+        row = table[r].clone()
+        if c >= 128:
+            row[:128 // B] = table[0, :128 // B]
+        k, v = R.cached(codes, scales, row, c)
+        want, wl, _, spread, reach = R.attend(q[r:r + 1], k, v, 0.125, c)
+        near(out[r:r + 1], want, R.out_bound(want, spread, reach, BF, c, R.most_of(scales, F8)), f"sequence {r}")
+        near(lse[r:r + 1], wl, R.lse_bound(wl, reach, 64), f"lse of {r}")
