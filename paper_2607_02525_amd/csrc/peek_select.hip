@@ -176,6 +176,8 @@ __global__ __launch_bounds__(kThreads) void k_kv_bounds(Bounds a) {
 // bounds, 16 queries by 16 blocks by 64 elements a matrix instruction. Bound by
 // reading the bounds, 2 D bytes a block and head in pages of any order: 64 sequences of up to
 // 1500 blocks 31 to 35 us, 3.4 TB/s; 16 of up to 4063 22 us, 5.9 TB/s; one of 1472 6 us.
+// With four wavefronts to a SIMD instead of three, and registers for as many, the 64 sequences
+// took 1.5 us more, with six 38 more; bounds of the next blocks fetched before these are used: 1 to 8 more.
 
 struct Select {
   Pool pool;
@@ -241,7 +243,7 @@ struct Query {
 };
 
 template <int TYPE, int FMT, int D>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4))) void k_block_scores(Select a, int32_t waves) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void k_block_scores(Select a, int32_t waves) {
   constexpr int kSteps = D / 64;
   const int lane = threadIdx.x & (kWave - 1), col = lane & 15, grp = lane >> 4;
   uint32_t unit = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
