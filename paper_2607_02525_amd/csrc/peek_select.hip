@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_bounds(Bounds a) {
 // A wavefront takes 64 blocks at a time of one (sequence, kv head): queries times
 // bounds, 16 queries by 16 blocks by 64 elements a matrix instruction. Bound by
 // reading the bounds, 2 D bytes a block and head in pages of any order: 64 sequences of up to
-// 1500 blocks 31 to 35 us, 3.4 TB/s; 16 of up to 4063 22 us, 5.9 TB/s; one of 1472 6 us.
+// 1500 blocks 30 to 34 us, 3.4 TB/s; 16 of up to 4063 22 us, 5.9 TB/s; one of 1472 6 us.
 // With four wavefronts to a SIMD instead of three, and registers for as many, the 64 sequences
 // took 1.5 us more, with six 38 more; bounds of the next blocks fetched before these are used: 1 to 8 more.
 
