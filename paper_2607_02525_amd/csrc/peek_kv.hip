@@ -92,7 +92,10 @@ __global__ __launch_bounds__(256) void k_kv_append(Pool pool, Rows k, Rows v, in
   }
   float scale = scale_of<FMT>(most);
   plain = plain && scale < kv::kScaleMax;
-  if (old > 0 && !(scale > held)) scale = held;
+  if (old > 0 && !(scale > held)) {
+    scale = held;
+    plain = plain && plain_scale<FMT>(held);
+  }
   const float inv = 1.0f / scale;
   if (old > 0 && scale > held) rescale<FMT>(codes, old * D, held, scale, inv, lane);
   for (int32_t p0 = 0; p0 < pieces; p0 += HELD * kWave) {

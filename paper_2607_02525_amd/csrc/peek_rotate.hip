@@ -363,7 +363,10 @@ __device__ __forceinline__ void rotate_block(const Rotate& a, uint32_t group, Tu
     }
     float scale = scale_of<FMT>(most);
     plain = plain && scale < kv::kScaleMax;
-    if (old > 0 && !(scale > held)) scale = held;
+    if (old > 0 && !(scale > held)) {
+      scale = held;
+      plain = plain && plain_scale<FMT>(held);
+    }
     const float inv = 1.0f / scale;
     if (active && old > 0 && scale > held) rescale<FMT>(codes, old * D, held, scale, inv, lane);
     auto store = [&](int32_t c, const u4 (*z)[2]) {
