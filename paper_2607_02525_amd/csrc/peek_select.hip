@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
       score = grp == i ? top : score;
     }
     if (b0 + lane < blocks)
-      a.scores[((int64_t)r * heads + head) * a.table.width + b0 + lane] = score * step + 0.0f;      // (no -0)
+      a.scores[((int64_t)r * heads + head) * a.table.width + b0 + lane] = score * step;
   }
 }
 
@@ -316,8 +316,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 // for 128 of up to 4063. In one kernel with the scores, which then come at the rate
 // of a compute unit: 22 us, 45, 46 where the two take 15, 45, 36.
 
-__device__ __forceinline__ uint32_t rank_of(float x) {       // NaN above all
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+// NaN above all. (-0, of a product too small for 32 bits, becomes 0 by adding 0 here, where that cannot be made one
+// operation with the product, rounded once and -0 again.)
+__device__ __forceinline__ uint32_t rank_of(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);
   return x != x ? 0xffffffffu : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 

@@ -265,3 +265,22 @@ def test_a_step_of_everything_captured_and_replayed():
             for x in (a.shared, a.out if keep == width else a.shared):
                 assert (x.float() - a.dense.float()).abs().max() <= 2 * 3 * 2.0 ** -8 * a.dense.float().abs().max() + 0.05
             ctx += 1
+
+
+@pytest.mark.parametrize("fmt", [F8, I8], ids=["f8", "i8"])
+def test_scores_too_small_for_32_bits_are_equal_whatever_their_sign(fmt):
+    """Queries of 2^-120 and scales of 2^-60: every score is 0, also that of a key against the query."""
+    import paper_2607_02525_amd as P
+    nb, B, D, keep = 12, 4, 64, 5
+    codes = torch.empty(nb, 2, 1, B, D, dtype=torch.uint8)
+    for b in range(nb):
+        codes[b] = torch.tensor([-8.0 if b % 2 == 0 else 8.0]).to(fmt).view(torch.uint8)
+    codes, scales = codes.view(fmt), torch.full((nb, 2, 1), 2.0 ** -60)
+    q, table = torch.full((1, 1, D), 2.0 ** -120, dtype=BF), torch.arange(nb, dtype=torch.int32).view(1, nb)
+    pool = P.KVPool(codes.cuda(), scales.cuda())
+    bounds = torch.empty(nb, 1, 2, D, dtype=torch.int8).cuda()
+    P.peek_kv_bounds(pool, None, ints([nb * B]), table.cuda(), bounds)
+    _, t = select(P, pool, bounds, q.cuda(), [nb * B], table, keep, 0, 1)
+    want, _ = chosen(codes, scales, bounds.cpu(), q, [nb * B], table, keep, 0, 1)
+    assert want.flatten().tolist() == [0, 1, 2, 3, nb - 1]
+    assert torch.equal(t.cpu(), want)
