@@ -384,8 +384,9 @@ peek_status peek_offline_order(int32_t n, const int32_t* d_tokens, const int64_t
  * Tokens of other sequences, slots past a sequence's end and pages it does
  * not name may hold anything, NaN included: they do not reach its outputs.
  * A page id outside the pool is a broken precondition (PEEK_VALIDATE reports
- * it); memory outside the pool is not touched: peek_kv_append leaves such a
- * block out, attention reads page 0 in its place. Lengths beyond the table
+ * it); memory outside the pool is not touched: calls that write a block's
+ * codes, scales or bounds leave such a one out, those that read the cache
+ * read page 0 in its place. Lengths beyond the table
  * (max_blocks * block_size tokens) and negative ones are cut to it.
  * PEEK_VALIDATE checks offsets, lengths, page ids and scales of these calls.
  * ---------------------------------------------------------------------- */

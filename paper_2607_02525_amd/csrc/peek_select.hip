@@ -109,7 +109,7 @@ __global__ __launch_bounds__(kThreads) void k_kv_bounds(Bounds a) {
   const int32_t at = lane % kLanes, sub = lane / kLanes;
   const bool upper32 = lane >= 32, upper16 = lane & 16, upper8 = lane & 8;
   for (int64_t b = (first >> lb) + split; b < blocks; b += a.splits) {
-    const uint32_t page = kv::page_of(a.table, a.pool, r, (int32_t)b);
+    const uint32_t id = (uint32_t)a.table.ids[(int64_t)r * a.table.stride + b], page = id < a.pool.num_pages ? id : 0u;
     const int32_t tokens = min(1 << lb, held - ((int32_t)b << lb));
     const uint8_t* codes = a.pool.pages + (((int64_t)page * 2 * heads + head) << lb) * D + at * 16;
     const bool turned = a.pool.scales[(int64_t)page * 2 * heads + head] < 0.0f;
@@ -167,7 +167,8 @@ __global__ __launch_bounds__(kThreads) void k_kv_bounds(Bounds a) {
     // the lower lanes write the largest, the upper ones the smallest
     const uint32_t out = fold32(word(up), word(down), [](uint32_t x, uint32_t y) { return x | y; });
     const int32_t e = 2 * upper8 + upper16;
-    *(uint32_t*)(a.out + (((int64_t)page * heads + head) * 2 + upper32) * D + at * 16 + e * 4) = out;
+    if (id < a.pool.num_pages)       // (no page, no bounds: page 0 is another block's)
+      *(uint32_t*)(a.out + (((int64_t)page * heads + head) * 2 + upper32) * D + at * 16 + e * 4) = out;
   }
 }
 

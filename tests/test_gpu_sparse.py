@@ -284,3 +284,18 @@ def test_scores_too_small_for_32_bits_are_equal_whatever_their_sign(fmt):
     want, _ = chosen(codes, scales, bounds.cpu(), q, [nb * B], table, keep, 0, 1)
     assert want.flatten().tolist() == [0, 1, 2, 3, nb - 1]
     assert torch.equal(t.cpu(), want)
+
+
+def test_bounds_of_no_page_are_left_out():
+    """A page id outside the pool: page 0 is another sequence's, whose bounds stay."""
+    import paper_2607_02525_amd as P
+    gen = torch.Generator().manual_seed(5)
+    codes, scales, _ = make_pool(gen, [64], 2, 16, 64, I8, spare=0)
+    table = torch.tensor([[1, -1, 3, 4]], dtype=torch.int32)
+    bounds = torch.full((4, 2, 2, 64), 99, dtype=torch.int8).cuda()
+    P.peek_kv_bounds(P.KVPool(codes.cuda(), scales.cuda()), None, ints([64]), table.cuda(), bounds)
+    got = bounds.cpu()
+    assert (got[[0, 2]] == 99).all(), "pages that the sequence does not name"
+    for p in (1, 3):
+        hi, lo = S.bounds(codes, scales, p, 16)
+        assert torch.equal(got[p], torch.from_numpy(np.stack([hi, lo], 1).astype(np.int8)))
