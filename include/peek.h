@@ -632,8 +632,8 @@ peek_status peek_kv_read(const peek_kv_pool* pool, int32_t n, int64_t num_tokens
  * shared shares nothing and reads its own pages.
  * Sequences past the last group's end share nothing either. Rows of sequences
  * that d_members does not name are left as they are; an id outside 0 .. n - 1 is
- * passed over, or, as a group's first, stands for sequence 0 (PEEK_VALIDATE reports it, and
- * offsets that are none). Everything else is as in peek_decode_attention; groups < 2^24.
+ * passed over, or, as a group's first, stands for sequence 0 (PEEK_VALIDATE reports it, a sequence
+ * named twice, and offsets that are none; of the table it looks at the entries that are read). Everything else is as in peek_decode_attention; groups < 2^24.
  * Scratch comes only from d_workspace (device, 256-byte aligned, at least
  * peek_shared_decode_attention_workspace bytes). Asynchronous on `stream`.
  * n = 0 is a no-op.

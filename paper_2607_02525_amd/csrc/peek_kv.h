@@ -87,6 +87,26 @@ __device__ __forceinline__ float code_value(uint8_t c) {
   }
 }
 
+// What PEEK_VALIDATE finds.
+constexpr int32_t kBadOffsets = 1, kBadLength = 2, kBadPage = 4, kBadScale = 8;
+
+// Of block b of sequence r: its page, and where the pool has scales and the block `holds` tokens these (of one that an
+// append adds to: what that asks for).
+__device__ __forceinline__ int32_t block_faults(const Table& table, const Pool& pool, int32_t r, int32_t b, bool holds,
+                                                bool appends) {
+  const int32_t id = table.ids[(int64_t)r * table.stride + b];
+  if (id < 0 || (uint32_t)id >= pool.num_pages) return kBadPage;
+  if (pool.scales == nullptr || !holds) return 0;
+  const float* x = pool.scales + (int64_t)id * 2 * pool.heads;
+  int32_t bad = 0;
+  for (int32_t h = 0; h < pool.heads; ++h) {
+    const bool k_fits = appends ? x[h] >= 0 && x[h] <= kScaleMax : fabsf(x[h]) < __builtin_inff();
+    const float v = x[pool.heads + h];
+    if (!k_fits || !(v >= 0 && v <= kScaleMax)) bad = kBadScale;
+  }
+  return bad;
+}
+
 // The last r in [0, n) with at(r) <= x, for at() that does not decrease (0 if
 // there is none). A wavefront looks at 64 places at a time: one load's
 // wait up to 64 sequences, two up to 4096.
@@ -149,5 +169,7 @@ void with_types(int32_t type, int32_t format, int32_t dim, F&& f) {
 peek_status validate_kv(int32_t n, const int64_t* d_offsets, int64_t num_tokens, const int32_t* d_len, bool appends,
                         const int32_t* d_table, int32_t max_blocks, int64_t table_stride, int32_t block_size,
                         const kv::Pool* pool, hipStream_t st);
+// These faults as a status, with its message.
+peek_status kv_status(int32_t bad);
 
 }  // namespace peek

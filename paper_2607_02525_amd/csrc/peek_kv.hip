@@ -123,29 +123,18 @@ __global__ void k_validate_kv(int32_t n, const int64_t* __restrict__ offsets, in
   int64_t fresh = 0;
   if (offsets != nullptr) {
     const int64_t a = offsets[r], b = offsets[r + 1];
-    if (a < 0 || b < a || b > num_tokens) f |= 1;
+    if (a < 0 || b < a || b > num_tokens) f |= kv::kBadOffsets;
     else fresh = b - a;
   }
   if (len != nullptr) {
     const int64_t held = len[r], all = held + (appends ? fresh : 0);
     if (held < 0 || all > ((int64_t)table.width << log_block)) {
-      f |= 2;
+      f |= kv::kBadLength;
     } else {
       const int32_t from = appends ? (int32_t)(held >> log_block) : 0;
       const int32_t to = (int32_t)((all + (1 << log_block) - 1) >> log_block);
-      for (int32_t b = from + (int32_t)threadIdx.x; b < to; b += (int32_t)blockDim.x) {
-        const int32_t id = table.ids[(int64_t)r * table.stride + b];
-        if (id < 0 || (uint32_t)id >= pool.num_pages) {
-          f |= 4;
-        } else if (pool.scales != nullptr && (int64_t)b << log_block < held) {       // the block holds tokens
-          const float* x = pool.scales + (int64_t)id * 2 * pool.heads;
-          for (int32_t h = 0; h < pool.heads; ++h) {
-            const bool k_fits = appends ? x[h] >= 0 && x[h] <= kv::kScaleMax : fabsf(x[h]) < __builtin_inff();
-            const float v = x[pool.heads + h];
-            if (!k_fits || !(v >= 0 && v <= kv::kScaleMax)) f |= 8;
-          }
-        }
-      }
+      for (int32_t b = from + (int32_t)threadIdx.x; b < to; b += (int32_t)blockDim.x)
+        f |= kv::block_faults(table, pool, r, b, (int64_t)b << log_block < held, appends);
     }
   }
   if (f) atomicOr(bad, f);
@@ -172,11 +161,16 @@ peek_status validate_kv(int32_t n, const int64_t* d_offsets, int64_t num_tokens,
   if (e == hipSuccess) e = hipStreamSynchronize(st);
   (void)hipFree(d_bad);
   if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "input validation failed to run: %s", hipGetErrorString(e));
-  if (bad & 1)
+  return kv_status(bad);
+}
+
+peek_status kv_status(int32_t bad) {
+  if (bad & kv::kBadOffsets)
     return fail(PEEK_ERR_INVALID_ARGUMENT, "d_offsets must be non-decreasing from 0 or more and end within num_tokens");
-  if (bad & 2) return fail(PEEK_ERR_INVALID_ARGUMENT, "a sequence has fewer than 0 tokens or more than its table holds");
-  if (bad & 4) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_block_table names pages outside the pool");
-  if (bad & 8)
+  if (bad & kv::kBadLength)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "a sequence has fewer than 0 tokens or more than its table holds");
+  if (bad & kv::kBadPage) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_block_table names pages outside the pool");
+  if (bad & kv::kBadScale)
     return fail(PEEK_ERR_INVALID_ARGUMENT,
                 "a block's scales are out of range (keys: finite; values, and what an append adds to: 0 to 2^60)");
   return PEEK_OK;

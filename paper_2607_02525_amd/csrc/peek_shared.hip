@@ -1019,31 +1019,73 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : kWave * WAVES) void k_share
 }
 
 // -------------------------------------------------------------- validation
-__global__ void k_validate_groups(int32_t n, int32_t groups, const int32_t* __restrict__ members,
-                                  const int32_t* __restrict__ offsets, int32_t* __restrict__ bad) {
-  const int32_t i = blockIdx.x * blockDim.x + threadIdx.x;
-  if (i < groups && (offsets[i] < 0 || offsets[i + 1] < offsets[i] || offsets[i + 1] > n)) atomicOr(bad, 1);
-  if (i < n && members != nullptr && (members[i] < 0 || members[i] >= n)) atomicOr(bad, 2);
-}
-__global__ void k_no_flag(int32_t* flag) { *flag = 0; }
+// What the call reads: a group's shared blocks in its first member's row (where a member shares them), a member's own
+// ones in its own.
+constexpr int32_t kBadMember = 16, kMemberTwice = 32, kBadGroups = 64, kBadShared = 128;
 
-// With PEEK_VALIDATE: group offsets non-decreasing within 0 .. n, members within the batch. Waits for `st`.
-peek_status validate_groups(int32_t n, int32_t groups, const int32_t* members, const int32_t* offsets, hipStream_t st) {
+__global__ __launch_bounds__(kWave) void k_validate_shared(Shared a, int32_t* __restrict__ bad, int32_t* __restrict__ seen) {
+  const int lane = threadIdx.x, lb = a.pool.log_block;
+  const int64_t most = (int64_t)a.table.width << lb;
+  int32_t f = 0;
+  if ((int32_t)blockIdx.x < a.groups) {
+    const int32_t g = blockIdx.x, from = a.group_offsets[g], to = a.group_offsets[g + 1];
+    if (from < 0 || to < from || to > a.n || (g == 0 && from != 0)) f |= kBadGroups;
+    const Group x = group_at(a, g);
+    if (x.lo < x.hi && (a.shared[g] < 0 || a.shared[g] > most)) f |= kBadShared;
+    bool read = false;
+    for (int32_t i = x.lo + lane; i < x.hi && x.tokens > 0; i += kWave) {
+      const int32_t r = member_at(a, i);
+      read = read || (r >= 0 && shares(x, held_by(a, r)) > 0);
+    }
+    if (__any(read)) {
+      const int32_t r = max(0, member_at(a, x.lo));
+      for (int32_t b = lane; b < x.tokens >> lb; b += kWave) f |= kv::block_faults(a.table, a.pool, r, b, true, false);
+    }
+  } else {
+    const int32_t position = blockIdx.x - a.groups, r = member_at(a, position);
+    const Group g = group_of(a, position, lane);
+    if (r < 0) {
+      f |= kBadMember;
+    } else {
+      if (lane == 0 && atomicAdd(&seen[r], 1) > 0) f |= kMemberTwice;
+      const int32_t held = a.context[r];
+      if (held < 0 || held > most) {
+        f |= kv::kBadLength;
+      } else {
+        const int32_t blocks = (int32_t)(((int64_t)held + (1 << lb) - 1) >> lb);
+        for (int32_t b = (shares(g, held) >> lb) + lane; b < blocks; b += kWave)
+          f |= kv::block_faults(a.table, a.pool, r, b, true, false);
+      }
+    }
+  }
+  if (f) atomicOr(bad, f);
+}
+__global__ void k_clear(int32_t* p, int32_t count) {
+  const int32_t i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < count) p[i] = 0;
+}
+
+// With PEEK_VALIDATE: group offsets from 0, non-decreasing, within 0 .. n, members within the batch and each once,
+// lengths within the table, pages and scales of what is read. Waits for `st`.
+peek_status validate_shared(const Shared& a, hipStream_t st) {
   if (!validation_enabled()) return PEEK_OK;
   int32_t* d_bad = nullptr;
-  PEEK_HIP_TRY(hipMalloc((void**)&d_bad, sizeof(int32_t)));
+  PEEK_HIP_TRY(hipMalloc((void**)&d_bad, ((size_t)a.n + 1) * sizeof(int32_t)));
   int32_t bad = 0;
-  hipLaunchKernelGGL(k_no_flag, dim3(1), dim3(1), 0, st, d_bad);
-  hipLaunchKernelGGL(k_validate_groups, dim3((unsigned)((std::max(n, groups) + 255) / 256)), dim3(256), 0, st, n, groups,
-                     members, offsets, d_bad);
+  hipLaunchKernelGGL(k_clear, dim3((unsigned)(a.n / 256 + 1)), dim3(256), 0, st, d_bad, a.n + 1);
+  hipLaunchKernelGGL(k_validate_shared, dim3((unsigned)(a.groups + a.n)), dim3(kWave), 0, st, a, d_bad, d_bad + 1);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) e = hipMemcpyAsync(&bad, d_bad, sizeof(int32_t), hipMemcpyDeviceToHost, st);
   if (e == hipSuccess) e = hipStreamSynchronize(st);
   (void)hipFree(d_bad);
   if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "input validation failed to run: %s", hipGetErrorString(e));
-  if (bad & 1) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_group_offsets must be non-decreasing within 0 .. n");
-  if (bad & 2) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_members names sequences outside the batch");
-  return PEEK_OK;
+  if (bad & kBadGroups)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "d_group_offsets must be non-decreasing offsets from 0, within 0 .. n");
+  if (bad & kBadMember) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_members names sequences outside the batch");
+  if (bad & kMemberTwice) return fail(PEEK_ERR_INVALID_ARGUMENT, "d_members names a sequence twice");
+  if (bad & kBadShared)
+    return fail(PEEK_ERR_INVALID_ARGUMENT, "a group shares fewer than 0 tokens or more than the table holds");
+  return kv_status(bad);
 }
 
 // -------------------------------------------------------------------- plan
@@ -1166,16 +1208,13 @@ peek_status peek_shared_decode_attention(const peek_kv_pool* pool, int32_t n, in
     if (own_groups >= (1 << 24) || joins >= (1 << 24))
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
     hipStream_t st = (hipStream_t)stream;
-    s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, pool->block_size, &a.pool,
-                    st);
-    if (s == PEEK_OK) s = validate_groups(n, groups, d_members, d_group_offsets, st);
-    if (s != PEEK_OK) return s;
     a.q = Rows{d_q, q_token_stride, q_head_stride};
     a.context = d_context;
     a.table = Table{d_block_table, table_stride, max_blocks};
     a.members = d_members;
     a.group_offsets = d_group_offsets;
     a.shared = d_shared;
+    if ((s = validate_shared(a, st)) != PEEK_OK) return s;
     a.out = (uint16_t*)d_out;
     a.out_token = out_token_stride;
     a.out_head = out_head_stride;

@@ -225,3 +225,83 @@ def test_validation_on_request(monkeypatch):
 def test_shared_on_another_stream():
     side = torch.cuda.Stream()
     run_shared(31, [(96, [5, 6, 1])], 2, 4, 16, 64, HF, I8, stream=side)
+
+
+def checked(P, groups, contexts, table, codes, scales, members=None, offsets=None, shared=None):
+    """The call on these, 4 query heads to each of the pool's; returns its rows."""
+    n, H, D, i32 = len(contexts), codes.shape[2], codes.shape[4], torch.int32
+    gen = torch.Generator().manual_seed(n)
+    q = torch.randn(n, 4 * H, D, generator=gen).to(BF)
+    pool = P.KVPool(codes.cuda(), scales.cuda())
+    sizes = [len(own) for _, own in groups]
+    offsets = [sum(sizes[:g]) for g in range(len(sizes) + 1)] if offsets is None else offsets
+    shared = [s for s, _ in groups] if shared is None else shared
+    out = torch.full_like(q, 7.0).cuda()
+    need = P.peek_shared_decode_attention_workspace(pool, n, 4 * H, table.shape[1], len(shared))
+    ws = torch.empty(max(256, need), dtype=torch.uint8).cuda()
+    P.peek_shared_decode_attention(pool, q.cuda(), torch.tensor(contexts, dtype=i32).cuda(), table.cuda(),
+                                   torch.tensor(offsets, dtype=i32).cuda(), torch.tensor(shared, dtype=i32).cuda(), out,
+                                   ws, members=None if members is None else torch.tensor(members, dtype=i32).cuda())
+    torch.cuda.synchronize()
+    return out.cpu()
+
+
+def refused(P, match, *args, **kw):
+    with pytest.raises(P.PeekError, match=match) as e:
+        checked(P, *args, **kw)
+    assert e.value.status == P.PEEK_ERR_INVALID_ARGUMENT
+
+
+def test_validation_lets_pass_what_is_never_read(monkeypatch):
+    """Members' own entries for what they share, whatever they are, and what the first member of a group names for tokens
+    that none of it shares."""
+    import paper_2607_02525_amd as P
+    monkeypatch.setenv("PEEK_VALIDATE", "1")
+    groups = [(96, [5, 6, 1]), (32, [3, 40]), (0, [9])]
+    for B in (16, 4):
+        gen = torch.Generator().manual_seed(11)
+        codes, scales, table, contexts = grouped_pool(gen, groups, B, 2, 64, F8)      # (others' entries: a page of NaN)
+        with_junk = checked(P, groups, contexts, table, codes, scales)
+        assert with_junk.isfinite().all()
+        for r in (1, 2):
+            table[r, :96 // B] = -1
+        table[4, :32 // B] = 1 << 30
+        assert torch.equal(checked(P, groups, contexts, table, codes, scales), with_junk)
+        # nobody in the group has as many tokens as are shared
+        table, contexts = torch.full((2, 8), -1, dtype=torch.int32), [0, 3]
+        table[1, 0] = 1
+        few = scales.clone()
+        few[1] = 0.5
+        assert checked(P, [(8 * B, [0, 3])], contexts, table, codes, few).shape[0] == 2
+
+
+def test_validation_reports_what_is_read(monkeypatch):
+    """What a group shares is checked where it is read: in its first member's row, however few tokens that one has."""
+    import paper_2607_02525_amd as P
+    monkeypatch.setenv("PEEK_VALIDATE", "1")
+    for B in (16, 4):
+        groups = [(96, [5, 6, 1])]
+        gen = torch.Generator().manual_seed(12)
+        codes, scales, table, contexts = grouped_pool(gen, groups, B, 2, 64, I8)
+        contexts[0] = 0                                        # a row of padding
+        assert checked(P, groups, contexts, table, codes, scales).isfinite().all()
+        for entry in (-1, len(codes), 0):                      # (page 0: scales of NaN)
+            broken = table.clone()
+            broken[0, 1] = entry
+            refused(P, "scales" if entry == 0 else "pages", groups, contexts, broken, codes, scales)
+            broken = table.clone()
+            broken[2, 96 // B] = entry                         # a member's own keys
+            refused(P, "scales" if entry == 0 else "pages", groups, contexts, broken, codes, scales)
+        # a member with fewer tokens than are shared reads its own
+        contexts[1] = 50
+        refused(P, "scales", groups, contexts, table, codes, scales)
+        contexts[1] = table.shape[1] * B + 1
+        refused(P, "tokens", groups, contexts, table, codes, scales)
+        contexts[1] = -1
+        refused(P, "tokens", groups, contexts, table, codes, scales)
+        contexts[1] = 102
+        refused(P, "tokens", groups, contexts, table, codes, scales, shared=[-1])
+        refused(P, "tokens", groups, contexts, table, codes, scales, shared=[table.shape[1] * B + 1])
+        refused(P, "offsets", groups, contexts, table, codes, scales, offsets=[1, 3])
+        refused(P, "twice", groups, contexts, table, codes, scales, members=[0, 1, 1])
+        assert checked(P, groups, contexts, table, codes, scales, members=[0, 2, 1]).isfinite().all()
