@@ -568,7 +568,7 @@ peek_status peek_rotate_append(const peek_kv_pool* pool, int32_t n, int64_t num_
     const int32_t row_heads = q_heads + (!pool && d_k_out ? kv_heads : 0);
     a.row_tokens = num_tokens >= 4096 ? kRowTokens : 1;
     const int64_t rows = row_heads > 0 ? (num_tokens + a.row_tokens - 1) / a.row_tokens : 0;
-    if (pages >= (1 << 24) || rows >= (1 << 24))
+    if (pages + rows >= (1 << 24))        // (a launch has fewer than 2^32 threads)
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many tokens for one call (%lld)", (long long)num_tokens);
     if (pages + rows == 0) return PEEK_OK;
     hipStream_t st = (hipStream_t)stream;

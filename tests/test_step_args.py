@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 import paper_2607_02525_amd as P
-from tests.test_attention_args import BAD, BAD_POOLS, FAKE, ODD, pool
+from tests.test_attention_args import BAD, BAD_POOLS, FAKE, ODD, decode, pool
 
 torch = pytest.importorskip("torch")
 LIB = P._lib
@@ -186,3 +186,12 @@ def test_the_binding_refuses_other_shapes_and_types():
         P._exact_arg(torch.zeros(3, 4), "x", torch.float32, 4, 3)
     with pytest.raises(TypeError, match="must be"):
         P._exact_arg(torch.zeros(4, 3), "x", torch.float16, 4, 3)
+
+
+def test_rotations_that_no_launch_can_hold_are_refused():
+    """Workgroups of one launch times their threads stay below 2^32, whichever of its parts they are for."""
+    small = dict(kv_heads=1, block_size=4, head_dim=64)
+    one = dict(h=1, d=64, ks=(64, 64), vs=(64, 64), kos=(64, 64), qs=(64, 64), qos=(64, 64), hq=1)
+    # 14 million blocks' workgroups (K and V) beside 7 million of four rows each
+    assert rotate(pool(**small), tokens=28_000_000, rot=rotary(rot_dim=64), **one) == BAD
+    assert "too many" in P.peek_last_error()
