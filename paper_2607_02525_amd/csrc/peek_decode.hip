@@ -467,7 +467,8 @@ peek_status decode(Decode& a, const peek_kv_pool* pool, int32_t n, int32_t type,
   const int32_t threads = many ? 1024 : kThreads, rows = many ? 1 : kWaves;      // of a joining workgroup
   const int64_t outs = p.splits > 1 ? ((int64_t)n * q_heads + rows - 1) / rows : 0;
   const int64_t masses = a.mass ? (int64_t)n * a.pool.heads * ((max_blocks + threads - 1) / threads) : 0;
-  if (groups >= (1 << 24) || outs + masses >= (1 << 24))
+  // (launches have fewer than 2^32 threads)
+  if (groups >= (1 << 24) || (outs + masses) * threads >= (int64_t)1 << 32)
     return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
   // (with a table for every head, these are sequences of their own)
   const bool by_head = a.context_head != 0;

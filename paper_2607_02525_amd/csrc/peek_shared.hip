@@ -1205,7 +1205,9 @@ peek_status peek_shared_decode_attention(const peek_kv_pool* pool, int32_t n, in
     // a workgroup to a row where rows are few or may have many parts of their own
     const bool many = p.own_splits >= kManyParts || (groups > 0 && (int64_t)n * q_heads <= kFewJoins);
     const int64_t joins = ((int64_t)n * q_heads + (many ? 0 : kWaves - 1)) / (many ? 1 : kWaves);
-    if (own_groups >= (1 << 24) || joins >= (1 << 24))
+    // (launches have fewer than 2^32 threads; blocks of 16 or more: shared keys' workgroups are beside the own ones)
+    const int64_t beside = pool->block_size >= 16 ? prefix_groups : 0;
+    if (own_groups + beside >= (1 << 24) || joins * (many ? 1024 : kThreads) >= (int64_t)1 << 32)
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
     hipStream_t st = (hipStream_t)stream;
     a.q = Rows{d_q, q_token_stride, q_head_stride};

@@ -195,3 +195,18 @@ def test_rotations_that_no_launch_can_hold_are_refused():
     # 14 million blocks' workgroups (K and V) beside 7 million of four rows each
     assert rotate(pool(**small), tokens=28_000_000, rot=rotary(rot_dim=64), **one) == BAD
     assert "too many" in P.peek_last_error()
+
+
+def test_decodes_that_no_launch_can_hold_are_refused():
+    # own keys' workgroups and those of shared keys beside them
+    wide = dict(qs=(64, 64), os=(64, 64), hq=1)
+    most = (1 << 24) - 1
+    assert shared(pool(kv_heads=1, block_size=16, head_dim=64), n=most, blocks=1, stride=1, groups=1, size=1 << 50,
+                  **wide) == BAD
+    assert "too many" in P.peek_last_error()
+    # joins by 16 wavefronts to a row: 2^22 rows
+    heads = dict(n=24576, hq=256, qs=(256 * 64, 64), os=(256 * 64, 64), size=1 << 60)
+    width = dict(blocks=8192, stride=8192)
+    for call, kw in ((shared, width), (decode, width), (sparse, dict(keep=8192))):
+        assert call(pool(kv_heads=1, block_size=16, head_dim=64), **kw, **heads) == BAD
+        assert "too many" in P.peek_last_error()
