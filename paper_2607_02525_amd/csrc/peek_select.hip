@@ -561,7 +561,8 @@ peek_status peek_block_select(const peek_kv_pool* pool, const int8_t* d_bounds, 
     const int32_t spans = (max_blocks + kSpan - 1) / kSpan;
     const int32_t waves = (int32_t)std::max<int64_t>(1, std::min<int64_t>(spans, kScoreWaves / units));
     const int64_t groups = (units * waves + kWaves - 1) / kWaves;
-    if (groups >= (1 << 24) || units >= (1 << 24))
+    const int threads = max_blocks <= kHeld * 256 ? 256 : max_blocks <= kHeld * 512 ? 512 : 1024;      // of a choice
+    if (groups >= (1 << 24) || units * threads >= (int64_t)1 << 32)      // (launches have fewer than 2^32 threads)
       return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
     hipStream_t st = (hipStream_t)stream;
     s = validate_kv(n, nullptr, 0, d_context, false, d_block_table, max_blocks, table_stride, pool->block_size, &a.pool,
@@ -586,12 +587,12 @@ peek_status peek_block_select(const peek_kv_pool* pool, const int8_t* d_bounds, 
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess) {
-      auto go = [&](auto kernel, int threads) {
+      auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3((unsigned)threads), 0, st, a);
       };
-      if (max_blocks <= kHeld * 256) go(k_block_select<256>, 256);
-      else if (max_blocks <= kHeld * 512) go(k_block_select<512>, 512);
-      else go(k_block_select<1024>, 1024);
+      if (threads == 256) go(k_block_select<256>);
+      else if (threads == 512) go(k_block_select<512>);
+      else go(k_block_select<1024>);
       e = hipGetLastError();
     }
     if (e != hipSuccess) return fail(PEEK_ERR_DEVICE, "selection launch failed: %s", hipGetErrorString(e));

@@ -210,3 +210,10 @@ def test_decodes_that_no_launch_can_hold_are_refused():
     for call, kw in ((shared, width), (decode, width), (sparse, dict(keep=8192))):
         assert call(pool(kv_heads=1, block_size=16, head_dim=64), **kw, **heads) == BAD
         assert "too many" in P.peek_last_error()
+
+
+def test_choices_that_no_launch_can_hold_are_refused():
+    # choices by 16 wavefronts to a (sequence, kv head)
+    assert select(pool(kv_heads=1024, block_size=4, head_dim=64), n=4096, hq=1024, qs=(1024 * 64, 64), blocks=5000,
+                  stride=5000, size=1 << 60) == BAD
+    assert "too many" in P.peek_last_error()
