@@ -678,21 +678,29 @@ def peek_rotate_append(q, k, v, offsets, context, freq, q_out, k_out=None, pool:
     [tokens, q_heads, head_dim] (both None: only K and V), k, v, k_out [tokens, kv_heads, head_dim] (any token and head
     strides; an output may be its own input), offsets int64[n+1], context int32[n] (tokens before), freq float64
     [rot_dim / 2] or None, q_norm, k_norm [head_dim] of the rows' type or None. Without a pool (v and block_table None)
-    only q_out and k_out are written."""
+    only q_out and k_out are written; without k (None, as k_out) only q_out."""
     n = _queue_n(offsets)
-    kind, dtype = _row_type(k, "k"), k.dtype
-    if k.dim() != 3:
-        raise ValueError("k must be [tokens, heads, head_dim]")
-    tokens, kv_heads, dim = k.shape
+    if k is None and q is None:
+        raise ValueError("k and q are both None")
+    if k is None and (pool is not None or k_out is not None):
+        raise ValueError("k must be given with a pool or k_out")
+    of, name = (q, "q") if k is None else (k, "k")
+    kind, dtype = _row_type(of, name), of.dtype
+    if of.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, head_dim]")
+    tokens, kv_heads, dim = of.shape
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out must be given together")
     if (pool is None) != (v is None) or (pool is None) != (block_table is None):
         raise ValueError("pool, v and block_table must be given together")
-    if pool is None and k_out is None:
+    if pool is None and k_out is None and k is not None:
         raise ValueError("k needs a pool or k_out")
     q_heads = 0 if q is None else q.shape[1] if q.dim() == 3 else -1
-    rows_q = rows_q_out = rows_v = rows_k_out = table = (None, 0, 0)
-    rows_k = _rows(k, "k", dtype)
+    rows_q = rows_q_out = rows_k = rows_v = rows_k_out = table = (None, 0, 0)
+    if k is None:
+        kv_heads = 1                    # (of no rows)
+    else:
+        rows_k = _rows(k, "k", dtype)
     if q is not None:
         rows_q = _rows(q, "q", dtype, None, dim, tokens)
         rows_q_out = _rows(q_out, "q_out", dtype, q_heads, dim, tokens)

@@ -250,3 +250,23 @@ def test_rotation_captured_and_replayed():
         for a, b in zip(outs, eager):
             assert torch.equal(a, b)
         assert torch.equal(pool.pages.view(torch.uint8), other.pages.view(torch.uint8))
+
+
+@pytest.mark.parametrize("layout", ["plain", "fused", "heads first"])
+def test_queries_alone(layout):
+    """Without keys: as beside them."""
+    import paper_2607_02525_amd as P
+    gen = torch.Generator().manual_seed(12)
+    T, Hq, D = 9, 6, 128
+    q, dq = rows_of(gen, (T, Hq, D), BF, layout)
+    _, dk = rows_of(gen, (T, 2, D), BF, "plain")
+    at, ctx = torch.tensor([1, 4, 8]).cuda(), torch.tensor([7, 0], dtype=torch.int32).cuda()
+    freq = torch.tensor([10000.0 ** (-i / 64) for i in range(64)], dtype=torch.float64).cuda()
+    norm = (1 + 0.3 * torch.randn(D, generator=gen)).to(BF).cuda()
+    alone, beside = torch.full_like(dq, math.nan), torch.full_like(dq, math.nan)
+    P.peek_rotate_append(dq, None, None, at, ctx, freq, alone, q_norm=norm)
+    P.peek_rotate_append(dq, dk, None, at, ctx, freq, beside, k_out=torch.empty_like(dk), q_norm=norm)
+    assert torch.equal(alone.view(torch.int16), beside.view(torch.int16))
+    for t, p in S.positions([1, 4, 8], [7, 0]):
+        want, size = S.rotate(q[t], p, freq.tolist(), False, 1.0, norm.cpu(), 1e-6)
+        near(alone[t], want, S.rotate_bound(want, size, BF, D, p), f"token {t} at {p}")

@@ -188,6 +188,22 @@ def test_the_binding_refuses_other_shapes_and_types():
         P._exact_arg(torch.zeros(4, 3), "x", torch.float16, 4, 3)
 
 
+def test_the_binding_takes_queries_alone_and_refuses_neither():
+    f16, i32 = torch.float16, torch.int32
+    q = torch.zeros(3, 2, 64, dtype=f16)
+    at, ctx = torch.zeros(2, dtype=torch.int64), torch.zeros(1, dtype=i32)
+    with pytest.raises(ValueError, match="k and q"):
+        P.peek_rotate_append(None, None, None, at, ctx, None, None)
+    with pytest.raises(ValueError, match="k must be given"):
+        P.peek_rotate_append(q, None, None, at, ctx, None, q, k_out=q)
+    with pytest.raises(TypeError, match="float32"):
+        P.peek_rotate_append(q.float(), None, None, at, ctx, None, q.float())
+    # as far as the tensors' place, which is not a GPU here
+    with pytest.raises(Exception, match="GPU|CUDA|cuda|device"):
+        P.peek_rotate_append(q, None, None, at, ctx, None, q)
+
+
+# ------------------------------------------------- launches of 2^32 threads or more
 def test_rotations_that_no_launch_can_hold_are_refused():
     """Workgroups of one launch times their threads stay below 2^32, whichever of its parts they are for."""
     small = dict(kv_heads=1, block_size=4, head_dim=64)
