@@ -56,9 +56,9 @@ constexpr int kMaxChunk = 4096;                  // tokens of a workgroup, at mo
 struct Decode {
   Pool pool;
   Rows q;
-  const int32_t* context;      // of sequence r and kv head h at r * context_row + h * context_head
-  Table table;                 // kv head h's row `table_head` entries after the one before
-  int64_t context_row, context_head, table_head;
+  const int32_t* context;
+  Table table;
+  int32_t by_head;             // lengths, and rows of the table, are those of (sequence, kv head), not of sequences
   uint16_t* out;
   int64_t out_token, out_head;
   float* lse;
@@ -80,6 +80,12 @@ struct alignas(16) Block {
   float scale, log_v, inv_v;
   uint32_t page;
 };
+
+// Where a kv head's length and row of the table are. (As two products with strides of either kind this took decode of
+// one sequence 0.3 us more.)
+__device__ __forceinline__ int32_t line_of(const Decode& a, int32_t r, int32_t head) {
+  return a.by_head ? r * a.pool.heads + head : r;
+}
 
 // Chunks of a sequence (lengths up to 2^31 - 1).
 __device__ __forceinline__ int32_t parts_of(int32_t tokens, int32_t chunk) {
@@ -108,7 +114,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
   unit /= a.row_tiles;
   const int32_t split = unit % a.splits, r = unit / a.splits;
   const int32_t q_heads = a.group * a.pool.heads, lb = a.pool.log_block;
-  const int32_t held = kv::clip_tokens(a.context[r * a.context_row + head * a.context_head], a.table.width, lb);
+  const int32_t line = line_of(a, r, head), held = kv::clip_tokens(a.context[line], a.table.width, lb);
   const int32_t from = split * a.chunk, to = from + min(a.chunk, held - from);   // (no sum passes `held`, nor 2^31)
   const int32_t row = row_tile * kRows + (lane & 15), rows = min(kRows, a.group - row_tile * kRows);
   if (from >= to) {
@@ -122,7 +128,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(WIDE ?
   }
 
   const int32_t block0 = from >> lb;
-  const int32_t* const row_ids = a.table.ids + r * a.table.stride + head * a.table_head;
+  const int32_t* const row_ids = a.table.ids + line * a.table.stride;
   if constexpr (!WIDE) {
     const int32_t blocks = ((to - 1) >> lb) - block0 + 1;
     for (int32_t i = tid; i < blocks; i += kThreads) {
@@ -360,7 +366,7 @@ __global__ __launch_bounds__(THREADS) void k_decode_join(Decode a, uint32_t outs
     const int64_t at = (int64_t)blockIdx.x * (kWaves / WAVES) + wave / WAVES;
     if (at >= (int64_t)a.n * q_heads) return;
     const int32_t r = (int32_t)(at / q_heads), q_head = (int32_t)(at % q_heads);
-    const int32_t tokens = a.context[r * a.context_row + q_head / a.group * a.context_head];
+    const int32_t tokens = a.context[a.by_head ? line_of(a, r, q_head / a.group) : r];
     const int32_t held = kv::clip_tokens(tokens, a.table.width, lb), parts = parts_of(held, a.chunk);
     if (parts < 2) return;
     float l2;
@@ -470,10 +476,8 @@ peek_status decode(Decode& a, const peek_kv_pool* pool, int32_t n, int32_t type,
   // (launches have fewer than 2^32 threads)
   if (groups >= (1 << 24) || (outs + masses) * threads >= (int64_t)1 << 32)
     return fail(PEEK_ERR_INVALID_ARGUMENT, "too many sequences for one call (%d)", n);
-  // (with a table for every head, these are sequences of their own)
-  const bool by_head = a.context_head != 0;
-  s = validate_kv(by_head ? n * a.pool.heads : n, nullptr, 0, a.context, false, a.table.ids, max_blocks,
-                  by_head ? a.table_head : a.table.stride, pool->block_size, &a.pool, st);
+  s = validate_kv(a.by_head ? n * a.pool.heads : n, nullptr, 0, a.context, false, a.table.ids, max_blocks,
+                  a.table.stride, pool->block_size, &a.pool, st);
   if (s != PEEK_OK) return s;
   char* ws = (char*)d_workspace;
   a.q = Rows{d_q, q_token_stride, q_head_stride};
@@ -535,7 +539,6 @@ peek_status peek_decode_attention(const peek_kv_pool* pool, int32_t n, int32_t t
     clear_error();
     Decode a{};
     a.context = d_context;
-    a.context_row = 1;
     a.table = Table{d_block_table, table_stride, max_blocks};
     a.mass_in = d_mass_in;
     a.mass = d_mass;
@@ -556,12 +559,9 @@ peek_status peek_sparse_decode_attention(const peek_kv_pool* pool, int32_t n, in
   return guarded([&]() -> peek_status {
     clear_error();
     Decode a{};
-    const int64_t heads = pool ? pool->kv_heads : 0;
     a.context = d_context;
-    a.context_row = heads;
-    a.context_head = 1;
-    a.table = Table{d_block_table, keep * heads, keep};
-    a.table_head = keep;
+    a.table = Table{d_block_table, keep, keep};
+    a.by_head = 1;
     return decode(a, pool, n, type, q_heads, d_q, q_token_stride, q_head_stride, scale, d_out, out_token_stride,
                   out_head_stride, d_lse, d_workspace, workspace_bytes, (hipStream_t)stream);
   });
