@@ -696,7 +696,7 @@ __device__ __forceinline__ void stream_keys(const Shared& a, uint32_t block, uin
   }
 }
 
-// ---------------------------------------------------------------- own keys
+// ----------------------------------------------------------------- kernels
 template <int TYPE, int FMT, int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_shared_tiles(Shared a) {
   __shared__ __attribute__((aligned(1024))) uint8_t s_memory[kMemory<D>];
@@ -715,7 +715,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   else stream_keys<TYPE, FMT, D, ROWS>(a, blockIdx.x - shared_groups, 0, s_memory);
 }
 
-// In blocks of 4 or 8 tokens: 16 rows of one sequence over a chunk of its own keys, as
+// ------------------------------------------- own keys in blocks of 4 or 8
+// 16 rows of one sequence over a chunk of its own keys, as
 // in the decode of single sequences. Blocks are looked up in LDS.
 template <int TYPE, int FMT, int D>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void k_shared_own(Shared a) {
