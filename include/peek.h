@@ -38,9 +38,10 @@
  *    inputs on the device (offsets non-decreasing from >= 0, prompt lengths
  *    < 2^31, last nodes inside the cache, match lengths inside their
  *    prompts) and return INVALID_ARGUMENT before any other work if one
- *    fails; so do peek_kv_append, peek_prefill_attention,
- *    peek_decode_attention and peek_kv_evict (offsets, lengths, page ids,
- *    scales).
+ *    fails; so do peek_kv_append, peek_rotate_append, peek_kv_read,
+ *    peek_prefill_attention, peek_kv_evict, the decode attentions (dense,
+ *    shared, sparse), peek_kv_bounds and peek_block_select (offsets, lengths,
+ *    page ids, scales).
  *    The check adds a small allocation, a launch and a stream
  *    synchronization per call, so it is not for use under graph capture.
  */
